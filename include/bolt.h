@@ -2,7 +2,9 @@
  * bolt.h -- C ABI of the MI355X (gfx950) implementation of Bolt's hardware-native kernel family
  * (arxiv 2110.15238): FP16 GEMM and implicit-GEMM NHWC conv2d with fused bias + activation
  * epilogues, persistent back-to-back (b2b) GEMM / conv fusion, channel padding, and the
- * light-weight profiler that picks template parameters per shape.
+ * light-weight profiler that picks template parameters per shape; and next to them the operators of
+ * language models that an FP16 GEMM alone does not cover: products with 4-bit weights, routing to
+ * experts, the experts' products.
  *
  * Conventions for every call
  *   - All tensor pointers are DEVICE pointers to IEEE binary16 data unless stated otherwise.
@@ -50,7 +52,8 @@ typedef enum {
   BOLT_ACT_RELU = 1,
   BOLT_ACT_GELU = 2,       /* 0.5 v (1 + erf(v / sqrt 2)) */
   BOLT_ACT_HARDSWISH = 3,  /* v * clamp(v + 3, 0, 6) / 6   */
-  BOLT_ACT_SOFTPLUS = 4    /* log(1 + exp v)               */
+  BOLT_ACT_SOFTPLUS = 4,   /* log(1 + exp v)               */
+  BOLT_ACT_SILU = 5        /* v / (1 + exp(-v)): bolt_gemm_w4 and bolt_moe_experts only */
 } bolt_act;
 
 typedef enum {
@@ -311,6 +314,90 @@ int32_t bolt_num_instances(bolt_op op);
 bolt_status bolt_instance_config(bolt_op op, int32_t kernel_id, bolt_config* out);
 /* Whether instance kernel_id can run the described problem (1) or not (0). */
 int32_t bolt_instance_supports(bolt_op op, int32_t kernel_id, const void* desc0, const void* desc1);
+
+/* ---- Operators of language models: 4-bit weights, routing to experts, the experts' products ------------------
+ * They follow the conventions above (borrowed device pointers, FP16 activations, FP32 accumulation, validation before any
+ * launch, nothing allocated); they take any size, so M and tokens may be 0 (BOLT_OK, and only `offsets` is written).  They
+ * have no instance tables: the kernel is chosen by a rule on the sizes. */
+
+/* Weights held in 4 bits: W[n][k] = scales[n][k / group] * (q[n][k] - zeros[n][k / group]), q and zeros in 0 .. 15; group 32, 64
+ * or 128; the last group of a row may be short.  N and K multiples of 8.
+ * bolt_w4_pack lays `count` matrices of one shape (one, or one per expert) out for the matrix core, once for a program's
+ * weights: q is [count][N][K / 2] bytes, even k in the low four bits; scales [count][N][ceil(K / group)] FP16; zeros
+ * [count][N][ceil(K / group)] bytes, or NULL (8 everywhere).  `packed` holds bolt_w4_packed_bytes(...) bytes (0 for a shape that
+ * is not accepted) and is all that the products below read. */
+size_t bolt_w4_packed_bytes(int32_t N, int32_t K, int32_t group, int32_t count);
+bolt_status bolt_w4_pack(int32_t N, int32_t K, int32_t group, int32_t count, const void* q, const void* scales, const void* zeros, void* packed,
+                         size_t packed_bytes, void* stream);
+
+/* D[M x N] = act(alpha * A[M x K] . W^T + beta * bias[N]), W of 4 bits with the given group. */
+typedef struct {
+  int32_t M, N, K;
+  int32_t lda, ldd; /* in elements; A and D are row-major */
+  int32_t group;
+  float alpha, beta;
+  int32_t act;      /* bolt_act, SiLU included */
+} bolt_gemm_w4_desc;
+
+/* A: M x K (lda), packed: bolt_w4_pack(N, K, group, 1), bias: N halves or NULL, D: M x N (ldd).  K, N, lda, ldd multiples of 8. */
+bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const void* packed, const void* bias, void* D, void* workspace,
+                         size_t workspace_bytes, void* stream);
+size_t bolt_gemm_w4_workspace_bytes(const bolt_gemm_w4_desc* desc);
+
+typedef enum { BOLT_TYPE_F16 = 0, BOLT_TYPE_F32 = 1 } bolt_type;
+typedef enum { BOLT_SCORE_SOFTMAX = 0, BOLT_SCORE_SIGMOID = 1 } bolt_score;
+
+/* Routing: for each token the top_k experts of `experts`, their weights, and the lists of tokens by expert.
+ *   score = softmax or sigmoid of the token's logits, in FP32.
+ *   key = the logit, or score + bias[e] where there is a bias; keys decide the choice, scores the weights.
+ *   groups > top_groups: the experts form `groups` equal runs; a run's value is its largest key (softmax) or the sum of its two
+ *   largest scores, bias included (sigmoid); the choice is among the top_groups runs of the largest values.
+ *   ids = the top_k largest keys, largest first; equal keys (and runs of equal value) by the lower index.
+ *   weights = scale * score of the chosen, with renormalize divided by their sum (0 if that is 0).
+ * A NaN logit counts as the lowest finite value, infinities as the largest ones of their sign, so that a row of nothing but
+ * masked experts still has a choice (the first experts). */
+typedef struct {
+  int32_t tokens, experts; /* experts <= 512 */
+  int32_t ld_logits;       /* elements from one token's logits to the next's, >= experts */
+  int32_t top_k;           /* <= 16, and no more than the experts of top_groups runs */
+  int32_t logits_type;     /* bolt_type */
+  int32_t score;           /* bolt_score */
+  int32_t groups, top_groups; /* 1, 1: none; experts % groups == 0, groups <= 16 */
+  int32_t renormalize;
+  float scale;
+} bolt_moe_route_desc;
+
+/* logits: tokens x experts (ld_logits); bias: `experts` floats or NULL; mask: `tokens` bytes or NULL, a zero takes the token out (ids
+ * -1, weights 0, in no list).  Outputs: ids [tokens][top_k] int32, weights [tokens][top_k] float, offsets [experts + 1] int32, order
+ * [tokens * top_k] int32: the slots t * top_k + j by expert, within an expert ascending; expert e's are order[offsets[e]] ..
+ * order[offsets[e + 1] - 1], and -1 follows the last list.  The same inputs always give the same lists. */
+bolt_status bolt_moe_route(const bolt_moe_route_desc* desc, const void* logits, const void* bias, const void* mask, void* ids, void* weights,
+                           void* offsets, void* order, void* workspace, size_t workspace_bytes, void* stream);
+size_t bolt_moe_route_workspace_bytes(const bolt_moe_route_desc* desc);
+
+typedef enum { BOLT_WEIGHTS_F16 = 0, BOLT_WEIGHTS_W4 = 1 } bolt_weights;
+
+/* The experts' products, y[t] = sum over the token's slots of weights[slot] * expert(x[t]):
+ *   u = x[t] . w_up[e]^T + b_up[e];  h = act(u), or with `gated` act(u[0 : hidden]) * u[hidden : 2 hidden];
+ *   expert(x) = h . w_down[e]^T + b_down[e].
+ * h is rounded to FP16 (the next product's operand), and so is each slot's weighted row before the FP32 sum over slots. */
+typedef struct {
+  int32_t tokens, experts, top_k;
+  int32_t width, hidden; /* multiples of 8 */
+  int32_t ldx, ldy;      /* row strides of x and y in elements, multiples of 8 */
+  int32_t act;           /* bolt_act, SiLU included */
+  int32_t gated;         /* 0 or 1 */
+  int32_t weights;       /* bolt_weights */
+  int32_t group;         /* of 4-bit weights */
+} bolt_moe_desc;
+
+/* x: tokens x width (ldx); w_up: [experts][hidden or 2 hidden][width], w_down: [experts][width][hidden], FP16 or packed by
+ * bolt_w4_pack with count = experts; b_up: [experts][hidden or 2 hidden], b_down: [experts][width], FP16 or NULL; ids, weights,
+ * offsets, order: as bolt_moe_route writes them; y: tokens x width (ldy), zero for tokens without an expert. */
+bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const void* w_up, const void* b_up, const void* w_down, const void* b_down,
+                             const void* ids, const void* weights, const void* offsets, const void* order, void* y, void* workspace,
+                             size_t workspace_bytes, void* stream);
+size_t bolt_moe_workspace_bytes(const bolt_moe_desc* desc);
 
 /* Measured roofline denominators: runs an MFMA-only loop of v_mfma_f32_16x16x32_f16 on pseudo-random FP16
  * operands, `iterations` x 16 instructions per wave, 8 waves per compute unit (returns the sustained FP16 TFLOP/s

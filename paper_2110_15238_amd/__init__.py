@@ -5,7 +5,8 @@ The Python layer only marshals arguments; importing it fails if the HIP library 
 """
 from . import binding
 from .binding import (ACT, LAYOUT_KN, LAYOUT_NK, OP_B2B_CONV, OP_B2B_CONV_RES, OP_B2B_GEMM, OP_B2B_GEMM_RES, OP_CONV2D, OP_CONV_CHAIN3, OP_GEMM, OP_GEMM_CHAIN3, BoltConfig, BoltError,
-                      ConvDesc, GemmDesc, TENSOR_NCHW, TENSOR_NHWC, TuneResult, conv_desc, conv_out_hw, gemm_desc)
+                      ConvDesc, GemmDesc, GemmW4Desc, MoeDesc, MoeRouteDesc, TENSOR_NCHW, TENSOR_NHWC, TuneResult, conv_desc,
+                      conv_out_hw, gemm_desc, gemm_w4_desc, moe_desc, moe_route_desc)
 
 # the C ABI's entry points under their own names
 bolt_gemm_epilogue = binding.gemm_epilogue
@@ -29,6 +30,14 @@ bolt_pad_channels_nhwc = binding.pad_channels_nhwc
 bolt_nchw_to_nhwc = binding.nchw_to_nhwc
 bolt_nhwc_to_nchw = binding.nhwc_to_nchw
 bolt_bias_act = binding.bias_act
+bolt_w4_packed_bytes = binding.w4_packed_bytes
+bolt_w4_pack = binding.w4_pack
+bolt_gemm_w4 = binding.gemm_w4
+bolt_gemm_w4_workspace_bytes = binding.gemm_w4_workspace_bytes
+bolt_moe_route = binding.moe_route
+bolt_moe_route_workspace_bytes = binding.moe_route_workspace_bytes
+bolt_moe_experts = binding.moe_experts
+bolt_moe_workspace_bytes = binding.moe_workspace_bytes
 bolt_workspace_bytes = binding.workspace_bytes
 bolt_check = binding.check
 bolt_status_string = binding.status_string

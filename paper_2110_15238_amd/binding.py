@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libbolt.so")
 
 OP_GEMM, OP_CONV2D, OP_B2B_GEMM, OP_B2B_CONV, OP_GEMM_CHAIN3, OP_CONV_CHAIN3 = 0, 1, 2, 3, 4, 5
 OP_B2B_GEMM_RES, OP_B2B_CONV_RES = 6, 7
-ACT = {"none": 0, "relu": 1, "gelu": 2, "hardswish": 3, "softplus": 4}
+ACT = {"none": 0, "relu": 1, "gelu": 2, "hardswish": 3, "softplus": 4, "silu": 5}
 LAYOUT_KN, LAYOUT_NK = 0, 1
 STATUS_NAMES = ["BOLT_OK", "BOLT_ERR_INVALID_ARG", "BOLT_ERR_UNSUPPORTED", "BOLT_ERR_ALIGNMENT",
                 "BOLT_ERR_WORKSPACE", "BOLT_ERR_LAUNCH", "BOLT_ERR_ILLEGAL_FUSION"]
@@ -54,6 +54,26 @@ class ConvDesc(C.Structure):
 
 
 TENSOR_NHWC, TENSOR_NCHW = 0, 1
+
+
+class GemmW4Desc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("lda", C.c_int32), ("ldd", C.c_int32),
+                ("group", C.c_int32), ("alpha", C.c_float), ("beta", C.c_float), ("act", C.c_int32)]
+
+
+class MoeRouteDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("tokens", "experts", "ld_logits", "top_k", "logits_type", "score", "groups",
+                                         "top_groups", "renormalize")] + [("scale", C.c_float)]
+
+
+class MoeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("tokens", "experts", "top_k", "width", "hidden", "ldx", "ldy", "act", "gated",
+                                         "weights", "group")]
+
+
+LOGITS = {"f16": 0, "f32": 1}
+SCORE = {"softmax": 0, "sigmoid": 1}
+WEIGHTS = {"f16": 0, "w4": 1}
 
 
 class BoltError(RuntimeError):
@@ -131,6 +151,22 @@ _lib.bolt_nchw_to_nhwc.restype = C.c_int
 _lib.bolt_nchw_to_nhwc.argtypes = [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp]
 _lib.bolt_nhwc_to_nchw.restype = C.c_int
 _lib.bolt_nhwc_to_nchw.argtypes = [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp]
+_lib.bolt_w4_packed_bytes.restype = _sz
+_lib.bolt_w4_packed_bytes.argtypes = [_i32, _i32, _i32, _i32]
+_lib.bolt_w4_pack.restype = C.c_int
+_lib.bolt_w4_pack.argtypes = [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.bolt_gemm_w4.restype = C.c_int
+_lib.bolt_gemm_w4.argtypes = [C.POINTER(GemmW4Desc), _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.bolt_gemm_w4_workspace_bytes.restype = _sz
+_lib.bolt_gemm_w4_workspace_bytes.argtypes = [C.POINTER(GemmW4Desc)]
+_lib.bolt_moe_route.restype = C.c_int
+_lib.bolt_moe_route.argtypes = [C.POINTER(MoeRouteDesc)] + [_vp] * 8 + [_sz, _vp]
+_lib.bolt_moe_route_workspace_bytes.restype = _sz
+_lib.bolt_moe_route_workspace_bytes.argtypes = [C.POINTER(MoeRouteDesc)]
+_lib.bolt_moe_experts.restype = C.c_int
+_lib.bolt_moe_experts.argtypes = [C.POINTER(MoeDesc)] + [_vp] * 11 + [_sz, _vp]
+_lib.bolt_moe_workspace_bytes.restype = _sz
+_lib.bolt_moe_workspace_bytes.argtypes = [C.POINTER(MoeDesc)]
 _lib.bolt_probe_mfma_peak.restype = C.c_int
 _lib.bolt_probe_mfma_peak.argtypes = [_i32, _vp, C.POINTER(C.c_float)]
 _lib.bolt_probe_copy_bandwidth.restype = C.c_int
@@ -141,7 +177,9 @@ EXPORTED = ["bolt_gemm_epilogue", "bolt_gemm_epilogue_noalloc", "bolt_conv2d_fpr
             "bolt_b2b_conv_residual", "bolt_b2b_gemm_chain", "bolt_b2b_conv_chain",
             "bolt_b2b_gemm_chain_residual", "bolt_b2b_conv_chain_residual", "bolt_tune_chain", "bolt_check_chain",
             "bolt_chain_instance_supports",
-            "bolt_pad_channels_nhwc", "bolt_nchw_to_nhwc", "bolt_nhwc_to_nchw", "bolt_bias_act", "bolt_workspace_bytes", "bolt_check", "bolt_status_string",
+            "bolt_pad_channels_nhwc", "bolt_nchw_to_nhwc", "bolt_nhwc_to_nchw", "bolt_bias_act", "bolt_w4_packed_bytes", "bolt_w4_pack",
+            "bolt_gemm_w4", "bolt_gemm_w4_workspace_bytes", "bolt_moe_route", "bolt_moe_route_workspace_bytes", "bolt_moe_experts",
+            "bolt_moe_workspace_bytes", "bolt_workspace_bytes", "bolt_check", "bolt_status_string",
             "bolt_num_instances", "bolt_instance_config", "bolt_instance_supports", "bolt_probe_mfma_peak",
             "bolt_probe_copy_bandwidth"]
 
@@ -499,6 +537,118 @@ def bias_act(D, bias=None, alpha: float = 1.0, beta: float = 1.0, act="relu"):
     _check(_lib.bolt_bias_act(_ptr(D), _ptr(bias), M, N, D.stride(0) if M > 1 else N, alpha, beta, a, _stream()),
            "bolt_bias_act")
     return D
+
+
+# ---- 4-bit weights, routing to experts, the experts' products -----------------------------------------------------
+# These take rows of any stride that their descriptor names, so each tensor is checked to hold what the descriptor asks for.
+
+
+def _buffer(t, dtype: str, count: int, name: str) -> int:
+    """Address of a contiguous CUDA tensor of `dtype` with at least `count` elements."""
+    torch = _torch or _load_torch()
+    assert t.is_cuda and t.dtype is getattr(torch, dtype) and t.is_contiguous(), \
+        "%s: expects a contiguous CUDA %s tensor" % (name, dtype)
+    assert t.numel() >= count, "%s: %d elements, the descriptor asks for %d" % (name, t.numel(), count)
+    return t.data_ptr()
+
+
+def _buffer_or_none(t, dtype: str, count: int, name: str) -> Optional[int]:
+    return None if t is None else _buffer(t, dtype, count, name)
+
+
+def _span(rows: int, ld: int, cols: int) -> int:
+    return (rows - 1) * ld + cols if rows > 0 else 0
+
+
+def w4_packed_bytes(N: int, K: int, group: int, count: int = 1) -> int:
+    """Bytes that `count` packed matrices take (0 for a shape that is not accepted)."""
+    return int(_lib.bolt_w4_packed_bytes(N, K, group, count))
+
+
+def w4_pack(N: int, K: int, group: int, q, scales, zeros, packed, count: Optional[int] = None):
+    """q: uint8 [count][N][K / 2] (even k in the low half), scales: float16 [count][N][ceil(K / group)], zeros: uint8 like scales
+    or None -> packed: uint8, w4_packed_bytes(...) elements.  `count` is q's leading extent unless given."""
+    if count is None:
+        count = q.shape[0] if q.dim() == 3 else 1
+    groups = -(-K // group) if group > 0 else 0
+    _check(_lib.bolt_w4_pack(N, K, group, count, _buffer(q, "uint8", count * N * K // 2, "q"),
+                             _buffer(scales, "float16", count * N * groups, "scales"),
+                             _buffer_or_none(zeros, "uint8", count * N * groups, "zeros"), _buffer(packed, "uint8", 0, "packed"),
+                             packed.numel(), _stream()), "bolt_w4_pack")
+    return packed
+
+
+def gemm_w4_desc(M, N, K, group, lda=None, ldd=None, alpha=1.0, beta=1.0, act="none") -> GemmW4Desc:
+    return GemmW4Desc(M, N, K, K if lda is None else lda, N if ldd is None else ldd, group, alpha, beta, ACT[act])
+
+
+def gemm_w4_workspace_bytes(desc: GemmW4Desc) -> int:
+    return int(_lib.bolt_gemm_w4_workspace_bytes(C.byref(desc)))
+
+
+def gemm_w4(desc: GemmW4Desc, A, packed, bias, D, workspace=None):
+    """D = act(alpha A.W^T + beta bias), W packed by w4_pack(desc.N, desc.K, desc.group, ...)."""
+    d = desc
+    wp, wb = _ws(workspace)
+    _check(_lib.bolt_gemm_w4(C.byref(d), _buffer(A, "float16", _span(d.M, d.lda, d.K), "A"),
+                             _buffer(packed, "uint8", w4_packed_bytes(d.N, d.K, d.group), "packed"),
+                             _buffer_or_none(bias, "float16", d.N, "bias"), _buffer(D, "float16", _span(d.M, d.ldd, d.N), "D"),
+                             wp, wb, _stream()), "bolt_gemm_w4")
+    return D
+
+
+def moe_route_desc(tokens, experts, top_k, score="softmax", groups=1, top_groups=1, renormalize=True, scale=1.0, logits="f16",
+                   ld=None) -> MoeRouteDesc:
+    return MoeRouteDesc(tokens, experts, experts if ld is None else ld, top_k, LOGITS[logits], SCORE[score], groups, top_groups,
+                        int(renormalize), scale)
+
+
+def moe_route_workspace_bytes(desc: MoeRouteDesc) -> int:
+    return int(_lib.bolt_moe_route_workspace_bytes(C.byref(desc)))
+
+
+def moe_route(desc: MoeRouteDesc, logits, bias, mask, ids, weights, offsets, order, workspace=None):
+    """logits: float16 or float32 as the descriptor says; bias: float32 or None; mask: uint8 or None (0 takes a token out);
+    writes ids, offsets, order (int32) and weights (float32)."""
+    d = desc
+    slots = d.tokens * d.top_k
+    wp, wb = _ws(workspace)
+    _check(_lib.bolt_moe_route(C.byref(d), _buffer(logits, "float32" if d.logits_type == LOGITS["f32"] else "float16",
+                                                   _span(d.tokens, d.ld_logits, d.experts), "logits"),
+                               _buffer_or_none(bias, "float32", d.experts, "bias"), _buffer_or_none(mask, "uint8", d.tokens, "mask"),
+                               _buffer(ids, "int32", slots, "ids"), _buffer(weights, "float32", slots, "weights"),
+                               _buffer(offsets, "int32", d.experts + 1, "offsets"), _buffer(order, "int32", slots, "order"),
+                               wp, wb, _stream()), "bolt_moe_route")
+    return ids, weights, offsets, order
+
+
+def moe_desc(tokens, experts, top_k, width, hidden, act="silu", gated=True, weights="f16", group=0, ldx=None, ldy=None) -> MoeDesc:
+    return MoeDesc(tokens, experts, top_k, width, hidden, width if ldx is None else ldx, width if ldy is None else ldy, ACT[act],
+                   int(gated), WEIGHTS[weights], group)
+
+
+def moe_workspace_bytes(desc: MoeDesc) -> int:
+    return int(_lib.bolt_moe_workspace_bytes(C.byref(desc)))
+
+
+def moe_experts(desc: MoeDesc, x, w_up, b_up, w_down, b_down, ids, weights, offsets, order, y, workspace):
+    """The routed experts' products into y; w_up and w_down are float16, or packed by w4_pack (uint8) with count = experts."""
+    d = desc
+    slots, up = d.tokens * d.top_k, (2 if d.gated else 1) * d.hidden
+    if d.weights == WEIGHTS["w4"]:
+        up_at = _buffer(w_up, "uint8", w4_packed_bytes(up, d.width, d.group, d.experts), "w_up")
+        down_at = _buffer(w_down, "uint8", w4_packed_bytes(d.width, d.hidden, d.group, d.experts), "w_down")
+    else:
+        up_at = _buffer(w_up, "float16", d.experts * up * d.width, "w_up")
+        down_at = _buffer(w_down, "float16", d.experts * d.width * d.hidden, "w_down")
+    wp, wb = _ws(workspace)
+    _check(_lib.bolt_moe_experts(C.byref(d), _buffer(x, "float16", _span(d.tokens, d.ldx, d.width), "x"), up_at,
+                                 _buffer_or_none(b_up, "float16", d.experts * up, "b_up"), down_at,
+                                 _buffer_or_none(b_down, "float16", d.experts * d.width, "b_down"),
+                                 _buffer(ids, "int32", slots, "ids"), _buffer(weights, "float32", slots, "weights"),
+                                 _buffer(offsets, "int32", d.experts + 1, "offsets"), _buffer(order, "int32", slots, "order"),
+                                 _buffer(y, "float16", _span(d.tokens, d.ldy, d.width), "y"), wp, wb, _stream()), "bolt_moe_experts")
+    return y
 
 
 def probe_mfma_peak(iterations: int = 20000) -> float:
