@@ -222,7 +222,7 @@ def _load_fast():
     _load_torch()
     try:
         from . import _fastcall
-        _fastcall.types(GemmDesc, ConvDesc, BoltConfig)
+        _fastcall.types(GemmDesc, ConvDesc, BoltConfig, GemmW4Desc, MoeRouteDesc, MoeDesc)
         _fast = _fastcall
     except ImportError as e:
         warnings.warn("calls are marshalled through ctypes, a microsecond slower: %s (make -C paper_2110_15238_amd/csrc "
@@ -588,6 +588,11 @@ def gemm_w4_workspace_bytes(desc: GemmW4Desc) -> int:
 
 def gemm_w4(desc: GemmW4Desc, A, packed, bias, D, workspace=None):
     """D = act(alpha A.W^T + beta bias), W packed by w4_pack(desc.N, desc.K, desc.group, ...)."""
+    status = (_fast or _load_fast()).gemm_w4(desc, A, packed, bias, D, workspace)
+    if status == 0:
+        return D
+    if status is not None:
+        raise BoltError(status, "bolt_gemm_w4")
     d = desc
     wp, wb = _ws(workspace)
     _check(_lib.bolt_gemm_w4(C.byref(d), _buffer(A, "float16", _span(d.M, d.lda, d.K), "A"),
@@ -610,6 +615,11 @@ def moe_route_workspace_bytes(desc: MoeRouteDesc) -> int:
 def moe_route(desc: MoeRouteDesc, logits, bias, mask, ids, weights, offsets, order, workspace=None):
     """logits: float16 or float32 as the descriptor says; bias: float32 or None; mask: uint8 or None (0 takes a token out);
     writes ids, offsets, order (int32) and weights (float32)."""
+    status = (_fast or _load_fast()).moe_route(desc, logits, bias, mask, ids, weights, offsets, order, workspace)
+    if status == 0:
+        return ids, weights, offsets, order
+    if status is not None:
+        raise BoltError(status, "bolt_moe_route")
     d = desc
     slots = d.tokens * d.top_k
     wp, wb = _ws(workspace)
@@ -633,6 +643,11 @@ def moe_workspace_bytes(desc: MoeDesc) -> int:
 
 def moe_experts(desc: MoeDesc, x, w_up, b_up, w_down, b_down, ids, weights, offsets, order, y, workspace):
     """The routed experts' products into y; w_up and w_down are float16, or packed by w4_pack (uint8) with count = experts."""
+    status = (_fast or _load_fast()).moe_experts(desc, x, w_up, b_up, w_down, b_down, ids, weights, offsets, order, y, workspace)
+    if status == 0:
+        return y
+    if status is not None:
+        raise BoltError(status, "bolt_moe_experts")
     d = desc
     slots, up = d.tokens * d.top_k, (2 if d.gated else 1) * d.hidden
     if d.weights == WEIGHTS["w4"]:

@@ -11,7 +11,7 @@
 
 namespace {
 
-PyObject *g_gemm_desc, *g_conv_desc, *g_config;  // the ctypes structure types of binding.py
+PyObject *g_gemm_desc, *g_conv_desc, *g_config, *g_gemm_w4_desc, *g_route_desc, *g_moe_desc;  // the ctypes structure types of binding.py
 
 // A structure's bytes, copied: the call below runs without the interpreter lock.
 template <typename T>
@@ -29,6 +29,9 @@ bool read_struct(PyObject* o, PyObject* type, T* out) {
 }
 bool read(PyObject* o, bolt_gemm_desc* d) { return read_struct(o, g_gemm_desc, d); }
 bool read(PyObject* o, bolt_conv_desc* d) { return read_struct(o, g_conv_desc, d); }
+bool read(PyObject* o, bolt_gemm_w4_desc* d) { return read_struct(o, g_gemm_w4_desc, d); }
+bool read(PyObject* o, bolt_moe_route_desc* d) { return read_struct(o, g_route_desc, d); }
+bool read(PyObject* o, bolt_moe_desc* d) { return read_struct(o, g_moe_desc, d); }
 
 struct Config {
   bolt_config value;
@@ -162,6 +165,70 @@ PyObject* chain(PyObject* const* a) {
   return call([&](void* s) { return FN(N, dp, x, w, b, y, c.ptr, s); });
 }
 
+// A tensor of `type` with at least `count` elements, as binding.py's _buffer asks for.
+bool buffer(PyObject* o, at::ScalarType type, int64_t count, void** p) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || t.scalar_type() != type || !t.is_contiguous() || t.numel() < count) return false;
+  *p = t.data_ptr();
+  return true;
+}
+bool buffer_or_none(PyObject* o, at::ScalarType type, int64_t count, void** p) {
+  *p = nullptr;
+  return o == Py_None || buffer(o, type, count, p);
+}
+int64_t span(int64_t rows, int64_t ld, int64_t cols) { return rows > 0 ? (rows - 1) * ld + cols : 0; }
+
+// (desc, A, packed, bias, D, workspace)
+PyObject* product_w4(PyObject* const* a) {
+  bolt_gemm_w4_desc d;
+  void *x, *w, *b, *y;
+  Workspace ws;
+  if (!read(a[0], &d) || !buffer(a[1], at::kHalf, span(d.M, d.lda, d.K), &x) ||
+      !buffer(a[2], at::kByte, (int64_t)bolt_w4_packed_bytes(d.N, d.K, d.group, 1), &w) || !buffer_or_none(a[3], at::kHalf, d.N, &b) ||
+      !buffer(a[4], at::kHalf, span(d.M, d.ldd, d.N), &y) || !ws.read(a[5]))
+    return nullptr;
+  return call([&](void* s) { return bolt_gemm_w4(&d, x, w, b, y, ws.ptr, ws.bytes, s); });
+}
+
+// (desc, logits, bias, mask, ids, weights, offsets, order, workspace)
+PyObject* route(PyObject* const* a) {
+  bolt_moe_route_desc d;
+  void *logits, *bias, *mask, *ids, *weights, *offsets, *order;
+  Workspace ws;
+  if (!read(a[0], &d)) return nullptr;
+  const int64_t slots = (int64_t)d.tokens * d.top_k;
+  if (!buffer(a[1], d.logits_type == BOLT_TYPE_F32 ? at::kFloat : at::kHalf, span(d.tokens, d.ld_logits, d.experts), &logits) ||
+      !buffer_or_none(a[2], at::kFloat, d.experts, &bias) || !buffer_or_none(a[3], at::kByte, d.tokens, &mask) ||
+      !buffer(a[4], at::kInt, slots, &ids) || !buffer(a[5], at::kFloat, slots, &weights) ||
+      !buffer(a[6], at::kInt, (int64_t)d.experts + 1, &offsets) || !buffer(a[7], at::kInt, slots, &order) || !ws.read(a[8]))
+    return nullptr;
+  return call([&](void* s) { return bolt_moe_route(&d, logits, bias, mask, ids, weights, offsets, order, ws.ptr, ws.bytes, s); });
+}
+
+// (desc, x, w_up, b_up, w_down, b_down, ids, weights, offsets, order, y, workspace)
+PyObject* experts(PyObject* const* a) {
+  bolt_moe_desc d;
+  void *x, *wu, *bu, *wd, *bd, *ids, *weights, *offsets, *order, *y;
+  Workspace ws;
+  if (!read(a[0], &d)) return nullptr;
+  const int64_t slots = (int64_t)d.tokens * d.top_k, up = (d.gated ? 2 : 1) * (int64_t)d.hidden;
+  if (up > INT32_MAX) return nullptr;
+  const bool w4 = d.weights == BOLT_WEIGHTS_W4;
+  const at::ScalarType type = w4 ? at::kByte : at::kHalf;
+  const int64_t up_count = w4 ? (int64_t)bolt_w4_packed_bytes((int32_t)up, d.width, d.group, d.experts) : d.experts * up * d.width;
+  const int64_t down_count = w4 ? (int64_t)bolt_w4_packed_bytes(d.width, d.hidden, d.group, d.experts) : (int64_t)d.experts * d.width * d.hidden;
+  if (!buffer(a[1], at::kHalf, span(d.tokens, d.ldx, d.width), &x) || !buffer(a[2], type, up_count, &wu) ||
+      !buffer_or_none(a[3], at::kHalf, d.experts * up, &bu) || !buffer(a[4], type, down_count, &wd) ||
+      !buffer_or_none(a[5], at::kHalf, (int64_t)d.experts * d.width, &bd) || !buffer(a[6], at::kInt, slots, &ids) ||
+      !buffer(a[7], at::kFloat, slots, &weights) || !buffer(a[8], at::kInt, (int64_t)d.experts + 1, &offsets) ||
+      !buffer(a[9], at::kInt, slots, &order) || !buffer(a[10], at::kHalf, span(d.tokens, d.ldy, d.width), &y) || !ws.read(a[11]))
+    return nullptr;
+  return call([&](void* s) {
+    return bolt_moe_experts(&d, x, wu, bu, wd, bd, ids, weights, offsets, order, y, ws.ptr, ws.bytes, s);
+  });
+}
+
 #define FASTCALL(NAME, WANT, ...) \
   PyObject* NAME(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded<&__VA_ARGS__>(a, n, WANT); }
 FASTCALL(gemm, 7, single<bolt_gemm_desc, &bolt_gemm_epilogue>)
@@ -172,15 +239,18 @@ FASTCALL(gemm_pair, 9, pair<bolt_gemm_desc, &bolt_b2b_gemm>)
 FASTCALL(conv_pair, 9, pair<bolt_conv_desc, &bolt_b2b_conv>)
 FASTCALL(gemm_chain, 6, chain<bolt_gemm_desc, &bolt_b2b_gemm_chain>)
 FASTCALL(conv_chain, 6, chain<bolt_conv_desc, &bolt_b2b_conv_chain>)
+FASTCALL(gemm_w4, 6, product_w4)
+FASTCALL(moe_route, 9, route)
+FASTCALL(moe_experts, 12, experts)
 
-// The structure types, once: GemmDesc, ConvDesc, BoltConfig.
+// The structure types, once: GemmDesc, ConvDesc, BoltConfig, GemmW4Desc, MoeRouteDesc, MoeDesc.
 PyObject* types(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 3) {
-    PyErr_SetString(PyExc_TypeError, "types(GemmDesc, ConvDesc, BoltConfig)");
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "types(GemmDesc, ConvDesc, BoltConfig, GemmW4Desc, MoeRouteDesc, MoeDesc)");
     return nullptr;
   }
-  PyObject** const at[3] = {&g_gemm_desc, &g_conv_desc, &g_config};
-  for (int i = 0; i < 3; ++i) {
+  PyObject** const at[6] = {&g_gemm_desc, &g_conv_desc, &g_config, &g_gemm_w4_desc, &g_route_desc, &g_moe_desc};
+  for (int i = 0; i < 6; ++i) {
     Py_INCREF(a[i]);
     *at[i] = a[i];
   }
@@ -189,7 +259,7 @@ PyObject* types(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {METHOD(gemm), METHOD(conv), METHOD(gemm_residual), METHOD(conv_residual), METHOD(gemm_pair), METHOD(conv_pair),
-                           METHOD(gemm_chain), METHOD(conv_chain), METHOD(types), {nullptr, nullptr, 0, nullptr}};
+                           METHOD(gemm_chain), METHOD(conv_chain), METHOD(gemm_w4), METHOD(moe_route), METHOD(moe_experts), METHOD(types), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

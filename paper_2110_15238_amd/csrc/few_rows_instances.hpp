@@ -1,9 +1,16 @@
-// What launches the products of a few rows: one function per kind of weights (csrc/inst_few_rows_*.hip).
+// What launches the products of rows with packed or FP16 weights: one function per family (csrc/inst_few_rows_*.hip,
+// csrc/inst_shared_rows_*.hip, csrc/inst_moe_tile.hip).  mode: ROWS_*.
 #pragma once
-#include "few_rows_kernel.hpp"
+#include "routed_rows.hpp"
 
 namespace bolt {
-// mode: ROWS_*; mb: 16-row blocks of activations per workgroup, 1, 2 or 4.
-hipError_t launch_few_rows_f16(const RowsParams& p, int mode, bool gated, int mb, hipStream_t stream);
-hipError_t launch_few_rows_w4(const RowsParams& p, int mode, bool gated, int group, int mb, hipStream_t stream);
+// Activation rows x weight rows of a workgroup's tile (a gated product has half as many output columns).
+enum class SharedTile { ROWS16_COLS64, ROWS16_COLS128, ROWS32_COLS32, ROWS32_COLS64, ROWS32_COLS128, ROWS64_COLS128, ROWS128_COLS256 };
+enum class ManyTile { ROWS64, ROWS128, ROWS256 };
+
+hipError_t launch_few_rows_f16(const RowsParams& p, int mode, bool gated, hipStream_t stream);
+hipError_t launch_few_rows_w4(const RowsParams& p, int mode, bool gated, int group, hipStream_t stream);
+hipError_t launch_shared_rows_f16(const RowsParams& p, int mode, bool gated, hipStream_t stream);
+hipError_t launch_shared_rows_w4(const RowsParams& p, int mode, bool gated, int group, SharedTile tile, hipStream_t stream);
+hipError_t launch_many_rows_f16(const RowsParams& p, int mode, bool gated, ManyTile tile, hipStream_t stream);
 }  // namespace bolt

@@ -11,313 +11,346 @@
 //   Activation rows beyond the last repeat the last: their columns of the result are not stored.  Columns beyond K are zero on
 //   both sides.
 #pragma once
-#include "fprop_dma_kernel.hpp"
+#include "routed_rows.hpp"
 #include "w4_format.hpp"
 
 namespace bolt {
 
-enum { WEIGHTS_F16 = 0, WEIGHTS_W4 = 1 };
-// Where a product's rows come from and go to.
-//   DENSE: row m of x, to row m of y.
-//   UP:    rows of the routed list: token order[i] / top_k of x, to row i of y (the list's order).
-//   DOWN:  row i of x, times the slot's weight, to row order[i] of y.
-enum { ROWS_DENSE = 0, ROWS_UP = 1, ROWS_DOWN = 2 };
-
-enum { ACT_SILU = 5 };
-// v / (1 + exp(-v)) with the hardware exp2 and reciprocal units: relative error about 1e-6 from the argument's rounding, far under a half's.
-__device__ __forceinline__ float silu_fast(float v) {
-  return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504088896340736f));
-}
-__device__ __forceinline__ float apply_act_or_silu(float v, int act) { return act == ACT_SILU ? silu_fast(v) : apply_act(v, act); }
-
-struct RowsParams {
-  const half_t* x;
-  int64_t ldx;
-  const unsigned char* w;      // FP16: [count][N][K]; 4 bits: the packed weights
-  int64_t w_stride;            // bytes from one expert's to the next's
-  const half_t* scales;        // 4 bits only
-  const unsigned char* zeros;
-  int64_t scale_stride;        // scales from one expert's to the next's
-  const half_t* bias;          // [count][N]; eight zeros if there is none
-  int bias_on;
-  half_t* y;
-  int64_t ldy;
-  int M, N, K, steps;          // N: weight rows; steps of the reduction, the last may be ragged
-  int hidden;                  // gated: weight rows [0, hidden) are the gate, [hidden, 2 hidden) the values
-  float alpha, beta;
-  int act;
-  const int* offsets;          // routed lists, see bolt_moe_route
-  const int* order;
-  const float* slot_weights;
-  int experts, top_k;
-  int row_blocks, col_blocks;  // grid: row_blocks * col_blocks workgroups
-};
-
-// The want-th block of B list rows, blocks counted expert by expert: its expert, first list row and row count.  Every lane of
-// a wave calls it; lane l adds up the blocks of `per` neighbouring experts.  False beyond the last block.
-template <int B>
-__device__ __forceinline__ bool find_row_block(const int* __restrict__ offsets, int experts, int want, int lane, int* expert, int* row0, int* rows) {
-  const int per = (experts + 63) >> 6, first = lane * per;
-  int mine = 0;
-  int at = first <= experts ? offsets[first] : 0;
-  for (int i = 0; i < per; ++i) {
-    if (first + i < experts) {
-      const int next = offsets[first + i + 1];
-      mine += (next - at + B - 1) / B;
-      at = next;
-    }
-  }
-  int upto = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(upto, d);
-    if (lane >= d) upto += o;
-  }
-  const unsigned long long past = __ballot(upto > want);
-  if (past == 0) return false;
-  const int owner = __builtin_ctzll(past);
-  int left = want - __builtin_amdgcn_readlane(upto - mine, owner);
-  int e = owner * per;
-  while (true) {  // ends: the owner's experts hold more than `left` blocks
-    const int lo = offsets[e], n = offsets[e + 1] - lo, blocks = (n + B - 1) / B;
-    if (left < blocks) {
-      *expert = e;
-      *row0 = lo + left * B;
-      *rows = n - left * B < B ? n - left * B : B;
-      return true;
-    }
-    left -= blocks;
-    ++e;
-  }
-}
-
-template <int WT, int MODE, bool GATED, int NG, int MB, int R, int NW, int NB>
-__global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
+// What both kernels below do alike, for one wave of a workgroup: B = 16 MB activation rows, R tiles of 16 weight rows.
+//   WT, NG: kind of weights, groups of a 128-column step (4 bits)
+template <int WT, int MODE, bool GATED, int NG, int MB, int R>
+struct RowsWave {
+  static constexpr int KS = WT == WEIGHTS_W4 ? 4 : 2, STEP = 32 * KS;  // matrix instructions and columns of a step
+  static constexpr int MPG = KS / NG;                                  // matrix instructions of a group (4 bits)
+  static constexpr int B = 16 * MB, COLS = GATED ? 8 * R : 16 * R;     // rows and outputs of a workgroup's tile
+  static constexpr int PIECES = WT == WEIGHTS_W4 ? 1 : KS;             // 16-byte pieces of weights per tile and step
   static_assert(!GATED || R % 2 == 0, "gated: tiles come in pairs");
-  constexpr int KS = WT == WEIGHTS_W4 ? 4 : 2, STEP = 32 * KS;  // matrix instructions and columns of a step
-  constexpr int MPG = KS / NG;                                  // matrix instructions of a group (4 bits)
-  constexpr int B = 16 * MB, COLS = GATED ? 8 * R : 16 * R;     // rows and outputs of a workgroup
-  extern __shared__ __attribute__((aligned(16))) float part[];  // [NW][R * MB][64 lanes][4]
-  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // Workgroups: the row blocks of one stretch of weights follow one another on one XCD (ids are dealt round-robin over 8), so the
-  // weights come from memory once.  Routed lists: a row block is an expert's, so its stretches follow one another instead.
-  int rb, cb, expert = 0, row0, rows;
-  if constexpr (MODE == ROWS_DENSE) {
-    const int total = (int)gridDim.x, xcd = (int)blockIdx.x & 7, per = total >> 3, rem = total & 7;
-    const int id = xcd * per + (xcd < rem ? xcd : rem) + ((int)blockIdx.x >> 3);
-    cb = id / p.row_blocks;
-    rb = id - cb * p.row_blocks;
-    row0 = rb * B;
-    rows = p.M - row0 < B ? p.M - row0 : B;
-  } else {
-    rb = (int)blockIdx.x / p.col_blocks;
-    cb = (int)blockIdx.x - rb * p.col_blocks;
-    if (!find_row_block<B>(p.offsets, p.experts, rb, lane, &expert, &row0, &rows)) return;
-    expert = __builtin_amdgcn_readfirstlane(expert);
-    row0 = __builtin_amdgcn_readfirstlane(row0);
-    rows = __builtin_amdgcn_readfirstlane(rows);
-  }
-  const int col0 = cb * COLS;
+  struct Weights {  // one step
+    uintx4 piece[R][PIECES];
+    half4 scale[R][NG];
+    unsigned zero[R];
+  };
+  struct Rows {  // one step
+    half8 part[KS][MB];
+  };
 
-  // this lane's activation rows and weight rows
+  const RowsParams& p;
+  int lane, g, l16, expert, row0, rows;
   const half_t* xrow[MB];
-#pragma unroll
-  for (int b = 0; b < MB; ++b) {
-    const int j = b * 16 + l16, row = row0 + (j < rows ? j : rows - 1);
-    const int64_t from = MODE == ROWS_UP ? p.order[row] / p.top_k : row;
-    xrow[b] = p.x + from * p.ldx + g * 8;
-  }
-  const unsigned char* const w = p.w + expert * p.w_stride;
-  auto first_row = [&](int t) { return GATED ? (t & 1) * p.hidden + col0 + (t >> 1) * 16 : col0 + t * 16; };
-  const int last_row = p.N - 1;
   const unsigned char* wrow[R];
-  int64_t scale_at[R], zero_at[R];
+  const half_t* scale_at[R];
+  const unsigned char* zero_at[R];
+
+  __device__ __forceinline__ RowsWave(const RowsParams& p_, int lane_) : p(p_), lane(lane_), g(lane_ >> 4), l16(lane_ & 15), expert(0) {}
+
+  // A routed list's block of rows; false beyond the last.
+  __device__ __forceinline__ bool take_block(int block) {
+    RowBlock at;
+    if (!find_row_block<B>(p.offsets, count_row_blocks<B>(p.offsets, p.experts, lane), block, &at)) return false;
+    const int done = (block - at.first) * B;
+    expert = at.expert;
+    row0 = at.lo + done;
+    rows = at.n - done < B ? at.n - done : B;
+    return true;
+  }
+  // Rows beyond the last repeat the last: their columns of the result are not stored.
+  __device__ __forceinline__ void take_rows() {
 #pragma unroll
-  for (int t = 0; t < R; ++t) {
-    int row = first_row(t) + l16;
-    row = row < last_row ? row : last_row;
-    if constexpr (WT == WEIGHTS_W4) {
-      wrow[t] = w + (int64_t)(row >> 4) * p.steps * W4Format::BLOCK_BYTES + (g * 16 + (row & 15)) * 16;
-      int quad = first_row(t) + g * 4;  // a multiple of 4, so the quad lies in one tile
-      quad = quad < last_row ? quad : last_row & ~3;
-      const int64_t base = expert * p.scale_stride;
-      scale_at[t] = base + ((int64_t)(quad >> 4) * p.steps * 4 + ((quad & 15) >> 2)) * (NG * 4);
-      zero_at[t] = base + ((int64_t)(row >> 4) * p.steps * 16 + (row & 15)) * NG;
-    } else {
-      wrow[t] = w + ((int64_t)row * p.K + g * 8) * 2;
+    for (int b = 0; b < MB; ++b) {
+      const int j = b * 16 + l16, row = row0 + (j < rows ? j : rows - 1);
+      const int64_t from = MODE == ROWS_UP ? p.order[row] / p.top_k : row;
+      xrow[b] = p.x + from * p.ldx + g * 8;
     }
   }
-
-  constexpr int WREGS = WT == WEIGHTS_W4 ? 1 : KS;  // 16-byte pieces of weights per tile and step
-  uintx4 wf[NB][R][WREGS];
-  half4 sc[NB][R][NG];
-  unsigned zp[NB][R];
-  half8 xf[NB][KS][MB];
-  floatx4 acc[R][MB];
+  // First weight row of tile t.
+  __device__ __forceinline__ int first_row(int col0, int t) const { return GATED ? (t & 1) * p.hidden + col0 + (t >> 1) * 16 : col0 + t * 16; }
+  // The tiles of output columns col0 .. col0 + COLS - 1.  Rows beyond the last repeat it.
+  __device__ __forceinline__ void take_columns(int col0) {
+    const unsigned char* const w = p.w + expert * p.w_stride;
+    const int64_t scales = expert * p.scale_stride;
+    const int last = p.N - 1;
 #pragma unroll
-  for (int t = 0; t < R; ++t)
-#pragma unroll
-    for (int b = 0; b < MB; ++b) acc[t][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-
-  // Step `step` into register set S; RAGGED: columns at or beyond K are zero (4-bit weights need no such check, zero activations do).
-  auto load = [&](int step, auto sc_, auto ragged) {
-    constexpr int S = decltype(sc_)::value;
-    constexpr bool RAGGED = decltype(ragged)::value;
+    for (int t = 0; t < R; ++t) {
+      const int first = first_row(col0, t);
+      const int row = first + l16 < last ? first + l16 : last;
+      if constexpr (WT == WEIGHTS_W4) {
+        wrow[t] = w + (int64_t)(row >> 4) * p.steps * W4Format::BLOCK_BYTES + (g * 16 + (row & 15)) * 16;
+        const int quad = first + g * 4 < last ? first + g * 4 : last & ~3;  // (a multiple of 4: the quad lies in one tile)
+        scale_at[t] = p.scales + scales + ((int64_t)(quad >> 4) * p.steps * 4 + ((quad & 15) >> 2)) * (NG * 4);
+        zero_at[t] = p.zeros + scales + ((int64_t)(row >> 4) * p.steps * 16 + (row & 15)) * NG;
+      } else {
+        wrow[t] = w + ((int64_t)row * p.K + g * 8) * 2;
+      }
+    }
+  }
+  // Step `step` of the weights.  4-bit weights are padded to whole steps.  FP16, RAGGED: beyond column K a lane reads its row's first
+  // columns instead, which meet zeros.
+  template <bool RAGGED>
+  __device__ __forceinline__ void load_weights(int step, Weights& out) const {
 #pragma unroll
     for (int t = 0; t < R; ++t) {
       if constexpr (WT == WEIGHTS_W4) {
-        wf[S][t][0] = *(const uintx4*)(wrow[t] + (int64_t)step * W4Format::BLOCK_BYTES);
-        const half_t* s = p.scales + scale_at[t] + (int64_t)step * (NG * 16);
+        out.piece[t][0] = *(const uintx4*)(wrow[t] + (int64_t)step * W4Format::BLOCK_BYTES);
+        const half_t* s = scale_at[t] + (int64_t)step * (NG * 16);
 #pragma unroll
-        for (int i = 0; i < NG; ++i) sc[S][t][i] = *(const half4*)(s + i * 4);
-        const unsigned char* z = p.zeros + zero_at[t] + (int64_t)step * (NG * 16);
-        if constexpr (NG == 4) zp[S][t] = *(const unsigned*)z;
-        else if constexpr (NG == 2) zp[S][t] = *(const unsigned short*)z;
-        else zp[S][t] = *z;
+        for (int i = 0; i < NG; ++i) out.scale[t][i] = *(const half4*)(s + i * 4);
+        const unsigned char* z = zero_at[t] + (int64_t)step * (NG * 16);
+        if constexpr (NG == 4) out.zero[t] = *(const unsigned*)z;
+        else if constexpr (NG == 2) out.zero[t] = *(const unsigned short*)z;
+        else out.zero[t] = *z;
       } else {
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-          const bool in = !RAGGED || step * STEP + s * 32 + g * 8 < p.K;
-          wf[S][t][s] = in ? *(const uintx4*)(wrow[t] + ((int64_t)step * STEP + s * 32) * 2) : uintx4{0, 0, 0, 0};
+          const int k = step * STEP + s * 32;
+          out.piece[t][s] = *(const uintx4*)(wrow[t] + (int64_t)(RAGGED && k + g * 8 >= p.K ? -g * 8 : k) * 2);
         }
       }
     }
+  }
+  template <bool RAGGED>
+  __device__ __forceinline__ void load_rows(int step, Rows& out) const {
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
-        const bool in = !RAGGED || step * STEP + s * 32 + g * 8 < p.K;
-        xf[S][s][b] = in ? *(const half8*)(xrow[b] + (int64_t)step * STEP + s * 32) : half8{0, 0, 0, 0, 0, 0, 0, 0};
+        const int k = step * STEP + s * 32;
+        const bool in = !RAGGED || k + g * 8 < p.K;
+        const half8 v = *(const half8*)(xrow[b] + (in ? k : -g * 8));
+        out.part[s][b] = in ? v : half8{0, 0, 0, 0, 0, 0, 0, 0};
       }
-  };
-  auto multiply = [&](auto sc_) {
-    constexpr int S = decltype(sc_)::value;
+  }
+  __device__ __forceinline__ void multiply(const Weights& w, const Rows& x, floatx4 (&acc)[R][MB]) const {
 #pragma unroll
     for (int t = 0; t < R; ++t) {
       if constexpr (WT == WEIGHTS_W4) {
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const unsigned z = NG == 1 ? zp[S][t] : (zp[S][t] >> (i * 8)) & 0xffu;
+          const unsigned z = NG == 1 ? w.zero[t] : (w.zero[t] >> (i * 8)) & 0xffu;
           const half2v m1 = w4_minus1(z), m16 = w4_minus16(z);
           floatx4 sum[MB];
 #pragma unroll
           for (int b = 0; b < MB; ++b) sum[b] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int s = i * MPG; s < (i + 1) * MPG; ++s) {
-            const half8 a = w4_values(wf[S][t][0][s], m1, m16);
+            const half8 a = w4_values(w.piece[t][0][s], m1, m16);
 #pragma unroll
-            for (int b = 0; b < MB; ++b) sum[b] = mfma_16x16x32(a, xf[S][s][b], sum[b]);
+            for (int b = 0; b < MB; ++b) sum[b] = mfma_16x16x32(a, x.part[s][b], sum[b]);
           }
 #pragma unroll
           for (int b = 0; b < MB; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[t][b][e] += (float)sc[S][t][i][e] * sum[b][e];
+            for (int e = 0; e < 4; ++e) acc[t][b][e] += (float)w.scale[t][i][e] * sum[b][e];
         }
       } else {
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-          for (int b = 0; b < MB; ++b) acc[t][b] = mfma_16x16x32(__builtin_bit_cast(half8, wf[S][t][s]), xf[S][s][b], acc[t][b]);
+          for (int b = 0; b < MB; ++b) acc[t][b] = mfma_16x16x32(__builtin_bit_cast(half8, w.piece[t][s]), x.part[s][b], acc[t][b]);
       }
     }
-  };
+  }
+  // part: [waves][R * MB][64 lanes][4] floats
+  __device__ __forceinline__ void put_sums(float* part, int wave, const floatx4 (&acc)[R][MB]) const {
+#pragma unroll
+    for (int t = 0; t < R; ++t)
+#pragma unroll
+      for (int b = 0; b < MB; ++b) *(floatx4*)(part + ((wave * R * MB + t * MB + b) * 64 + lane) * 4) = acc[t][b];
+  }
+  // The waves' sums, added in the order of the waves, through the epilogue and out: one thread for a quad of columns of one row.
+  template <int NW>
+  __device__ __forceinline__ void finish(const float* part, int col0, int tid) const {
+    auto sum_of = [&](int t, int b, int at) {
+      floatx4 v = *(const floatx4*)(part + ((t * MB + b) * 64 + at) * 4);
+#pragma unroll
+      for (int k = 1; k < NW; ++k) v += *(const floatx4*)(part + ((k * R * MB + t * MB + b) * 64 + at) * 4);
+      return v;
+    };
+    auto with_bias = [&](floatx4 v, int n) {  // n: weight row of the quad
+      const half4 hb = *(const half4*)(p.bias + (expert * (int64_t)p.N + n) * p.bias_on);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = p.alpha * v[e] + p.beta * (float)hb[e];
+      return v;
+    };
+    constexpr int OUT = (GATED ? R / 2 : R) * MB;
+    const int outputs = GATED ? p.hidden : p.N;
+    for (int i = tid; i < OUT * 64; i += 64 * NW) {
+      const int at = i & 63, b = (i >> 6) % MB, t = (i >> 6) / MB;
+      const int j = b * 16 + (at & 15), col = col0 + t * 16 + (at >> 4) * 4;
+      if (j >= rows || col >= outputs) continue;
+      floatx4 v = with_bias(sum_of(GATED ? 2 * t : t, b, at), col);
+v = apply_act4(v, p.act);
+      if constexpr (GATED) v *= with_bias(sum_of(2 * t + 1, b, at), p.hidden + col);
+      if constexpr (MODE == ROWS_DOWN) {
+        *(floatx4*)((float*)p.y + (int64_t)p.order[row0 + j] * p.ldy + col) = v;
+      } else {
+        half4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (half_t)v[e];
+        *(half4*)((half_t*)p.y + (int64_t)(row0 + j) * p.ldy + col) = o;
+      }
+    }
+  }
+};
 
+// Deep reductions: a wave's steps pass through NB register sets, one tile of columns per workgroup.
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NB>
+__global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
+  using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
+  extern __shared__ __attribute__((aligned(16))) float part[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Wave w(p, tid & 63);
+  int cb;
+  if constexpr (MODE == ROWS_DENSE) {
+    const int id = xcd_run((int)blockIdx.x, (int)gridDim.x);
+    cb = id / p.row_blocks;
+    w.row0 = (id - cb * p.row_blocks) * Wave::B;
+    w.rows = p.M - w.row0 < Wave::B ? p.M - w.row0 : Wave::B;
+  } else {
+    const int block = (int)blockIdx.x / p.col_blocks;
+    cb = (int)blockIdx.x - block * p.col_blocks;
+    if (!w.take_block(block)) return;
+  }
+  const int col0 = cb * Wave::COLS;
+  w.take_rows();
+  w.take_columns(col0);
+  typename Wave::Weights wf[NB];
+  typename Wave::Rows xf[NB];
+  floatx4 acc[R][1] = {};
   // This wave's steps: wave, wave + NW, ...; a ragged last step is one wave's, behind its whole ones.
-  const int whole = p.K / STEP;
+  const int whole = p.K / Wave::STEP;
   const int n = whole > wave ? (whole - wave + NW - 1) / NW : 0;
-  auto step_of = [&](int i) { return wave + i * NW; };
-  using False = std::integral_constant<bool, false>;
-  using True = std::integral_constant<bool, true>;
+  auto load = [&](int i, auto b) {
+    w.template load_weights<false>(wave + i * NW, wf[decltype(b)::value]);
+    w.template load_rows<false>(wave + i * NW, xf[decltype(b)::value]);
+  };
+  auto multiply = [&](auto b) { w.multiply(wf[decltype(b)::value], xf[decltype(b)::value], acc); };
   if (n >= NB) {
-    for_constants<NB>([&](auto b) { load(step_of(decltype(b)::value), b, False{}); });
+    for_constants<NB>([&](auto b) { load(decltype(b)::value, b); });
     int c = 0;
     for (; c + 2 * NB <= n; c += NB)
       for_constants<NB>([&](auto b) {
         multiply(b);
-        load(step_of(c + NB + decltype(b)::value), b, False{});
+        load(c + NB + decltype(b)::value, b);
       });
     const int left = n - c - NB;  // steps not requested yet, fewer than NB
     for_constants<NB>([&](auto b) {
       multiply(b);
-      if (decltype(b)::value < left) load(step_of(c + NB + decltype(b)::value), b, False{});
+      if (decltype(b)::value < left) load(c + NB + decltype(b)::value, b);
     });
     for_constants<NB>([&](auto b) {
       if (decltype(b)::value < left) multiply(b);
     });
   } else {
     for_constants<NB>([&](auto b) {
-      if (decltype(b)::value < n) load(step_of(decltype(b)::value), b, False{});
+      if (decltype(b)::value < n) load(decltype(b)::value, b);
     });
     for_constants<NB>([&](auto b) {
       if (decltype(b)::value < n) multiply(b);
     });
   }
   if (whole < p.steps && whole % NW == wave) {
-    load(whole, std::integral_constant<int, 0>{}, True{});
-    multiply(std::integral_constant<int, 0>{});
+    w.template load_weights<true>(whole, wf[0]);
+    w.template load_rows<true>(whole, xf[0]);
+    w.multiply(wf[0], xf[0], acc);
   }
-
-  // the waves' sums, in the order of the waves
-#pragma unroll
-  for (int t = 0; t < R; ++t)
-#pragma unroll
-    for (int b = 0; b < MB; ++b) *(floatx4*)(part + ((wave * R * MB + t * MB + b) * 64 + lane) * 4) = acc[t][b];
+  w.put_sums(part, wave, acc);
   __syncthreads();
-  auto sum_of = [&](int t, int b, int at) {
-    floatx4 v = *(const floatx4*)(part + ((t * MB + b) * 64 + at) * 4);
-#pragma unroll
-    for (int k = 1; k < NW; ++k) v += *(const floatx4*)(part + ((k * R * MB + t * MB + b) * 64 + at) * 4);
-    return v;
+  w.template finish<NW>(part, col0, tid);
+}
+
+// Reductions of at most NX steps per wave: the wave's share of the activations stays in registers while the workgroup walks over
+// p.walk tiles of columns.  The weights of the next tile are on their way while a tile is multiplied, summed and stored, so the
+// cost of finding the rows and of the first round trip to memory is paid once per walk, and the waves' sums have two places, so one
+// barrier per tile is enough.  Steps that a wave does not have meet zero activations (and read its last step's weights again).
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
+__global__ __launch_bounds__(64 * NW) void few_rows_walk_kernel(const RowsParams p) {
+  using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
+  constexpr int PART = NW * R * 64 * 4;
+  extern __shared__ __attribute__((aligned(16))) float part[];  // [2][PART]
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Wave w(p, tid & 63);
+  const int walks = (p.col_blocks + p.walk - 1) / p.walk;
+  int cb;
+  if constexpr (MODE == ROWS_DENSE) {
+    const int id = xcd_run((int)blockIdx.x, (int)gridDim.x), walk = id / p.row_blocks;
+    cb = walk * p.walk;
+    w.row0 = (id - walk * p.row_blocks) * Wave::B;
+    w.rows = p.M - w.row0 < Wave::B ? p.M - w.row0 : Wave::B;
+  } else {
+    const int block = (int)blockIdx.x / walks;
+    cb = ((int)blockIdx.x - block * walks) * p.walk;
+    if (!w.take_block(block)) return;
+  }
+  const int tiles = p.col_blocks - cb < p.walk ? p.col_blocks - cb : p.walk;
+  typename Wave::Weights wf[2][NX];
+  typename Wave::Rows xf[NX];
+  const int last_step = p.steps - 1;
+  auto load = [&](int tile, auto set) {
+    w.take_columns((cb + tile) * Wave::COLS);
+    for_constants<NX>([&](auto i) {
+      const int step = wave + decltype(i)::value * NW;
+      w.template load_weights<true>(step < last_step ? step : last_step, wf[decltype(set)::value][decltype(i)::value]);
+    });
   };
-  auto with_bias = [&](floatx4 v, int n_) {  // n_: weight row of the quad
-    const half4 hb = *(const half4*)(p.bias + (expert * (int64_t)p.N + n_) * p.bias_on);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = p.alpha * v[e] + p.beta * (float)hb[e];
-    return v;
+  using S0 = std::integral_constant<int, 0>;
+  using S1 = std::integral_constant<int, 1>;
+  load(0, S0{});
+  w.take_rows();
+  for_constants<NX>([&](auto i) { w.template load_rows<true>(wave + decltype(i)::value * NW, xf[decltype(i)::value]); });
+  auto tile = [&](int it, auto set) {
+    floatx4 acc[R][1] = {};
+    for_constants<NX>([&](auto i) { w.multiply(wf[decltype(set)::value][decltype(i)::value], xf[decltype(i)::value], acc); });
+    float* const mine = part + decltype(set)::value * PART;
+    w.put_sums(mine, wave, acc);
+    barrier_after_lds_writes();
+    w.template finish<NW>(mine, (cb + it) * Wave::COLS, tid);
   };
-  constexpr int OUT = (GATED ? R / 2 : R) * MB;
-  for (int i = tid; i < OUT * 64; i += 64 * NW) {
-    const int at = i & 63, b = (i >> 6) % MB, t = (i >> 6) / MB;
-    const int j = b * 16 + (at & 15), col = col0 + t * 16 + (at >> 4) * 4;
-    const int outputs = GATED ? p.hidden : p.N;
-    if (j >= rows || col >= outputs) continue;
-    floatx4 v;
-    if constexpr (GATED) {
-      v = with_bias(sum_of(2 * t, b, at), col);
-      const floatx4 u = with_bias(sum_of(2 * t + 1, b, at), p.hidden + col);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = apply_act_or_silu(v[e], p.act) * u[e];
-    } else {
-      v = with_bias(sum_of(t, b, at), col);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = apply_act_or_silu(v[e], p.act);
-    }
-    int64_t to = row0 + j;
-    if constexpr (MODE == ROWS_DOWN) {
-      to = p.order[row0 + j];
-      const float s = p.slot_weights[to];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] *= s;
-    }
-    half4 o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (half_t)v[e];
-    *(half4*)(p.y + to * p.ldy + col) = o;
+  int it = 0;
+  for (; it + 2 < tiles; it += 2) {
+    load(it + 1, S1{});
+    tile(it, S0{});
+    load(it + 2, S0{});
+    tile(it + 1, S1{});
+  }
+  if (it + 1 < tiles) {
+    load(it + 1, S1{});
+    tile(it, S0{});
+    tile(it + 1, S1{});
+  } else {
+    tile(it, S0{});
   }
 }
 
-template <int WT, int MODE, bool GATED, int NG, int MB, int R, int NW, int NB>
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NB>
 hipError_t launch_few_rows(RowsParams p, hipStream_t stream) {
-  auto kern = few_rows_kernel<WT, MODE, GATED, NG, MB, R, NW, NB>;
-  constexpr int LDS_BYTES = NW * R * MB * 64 * 16, COLS = GATED ? 8 * R : 16 * R;
+  auto kern = few_rows_kernel<WT, MODE, GATED, NG, R, NW, NB>;
+  using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
+  constexpr int LDS_BYTES = NW * R * 64 * 16;
   static LdsOptIn opt_in;
   if (hipError_t e = opt_in.ensure((const void*)kern, LDS_BYTES); e != hipSuccess) return e;
-  p.col_blocks = ((GATED ? p.hidden : p.N) + COLS - 1) / COLS;
-  // an expert's last block of rows may be short: at most one such block for each expert that has rows
-  p.row_blocks = MODE == ROWS_DENSE ? (p.M + 16 * MB - 1) / (16 * MB) : p.M / (16 * MB) + (p.M < p.experts ? p.M : p.experts);
+  p.col_blocks = ((GATED ? p.hidden : p.N) + Wave::COLS - 1) / Wave::COLS;
+  p.row_blocks = row_blocks<Wave::B>(p, MODE);
   hipLaunchKernelGGL(kern, dim3(p.row_blocks * p.col_blocks), dim3(64 * NW), LDS_BYTES, stream, p);
+  return hipGetLastError();
+}
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
+hipError_t launch_few_rows_walk(RowsParams p, hipStream_t stream) {
+  auto kern = few_rows_walk_kernel<WT, MODE, GATED, NG, R, NW, NX>;
+  using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
+  constexpr int LDS_BYTES = 2 * NW * R * 64 * 16;
+  static LdsOptIn opt_in;
+  if (hipError_t e = opt_in.ensure((const void*)kern, LDS_BYTES); e != hipSuccess) return e;
+  p.col_blocks = ((GATED ? p.hidden : p.N) + Wave::COLS - 1) / Wave::COLS;
+  p.row_blocks = row_blocks<Wave::B>(p, MODE);
+  // As many walks as the compute units hold at once (two workgroups each).  Routed lists: four times as many, since part of the row
+  // blocks that are counted here do not exist (29 tokens to 8 of 128 experts, 2048 x 768 in 4 bits: 112 us so, 96, 92 and 100 with
+  // 2, 4 and 8 times).
+  const int64_t tiles = (int64_t)p.row_blocks * p.col_blocks, want = 512 * (MODE == ROWS_DENSE ? 1 : 4);
+  const int64_t walk = (tiles + want - 1) / want;
+  p.walk = (int)(walk < p.col_blocks ? walk : p.col_blocks);
+  const int walks = (p.col_blocks + p.walk - 1) / p.walk;
+  hipLaunchKernelGGL(kern, dim3(p.row_blocks * walks), dim3(64 * NW), LDS_BYTES, stream, p);
   return hipGetLastError();
 }
 

@@ -1,9 +1,11 @@
 // C ABI of the operators of language models: linear layers with weights in 4 bits, routing to experts, the experts' products.
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "../../include/bolt.h"
 #include "few_rows_instances.hpp"
+#include "w4_format.hpp"
 #include "moe_route_kernel.hpp"
 
 namespace bolt {
@@ -51,9 +53,42 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const unsigned char* q, co
 }
 
 
-// y[t] = sum of the slots' rows (which carry their weights already), in FP32, in the order of the slots: one thread for eight columns.
+// A packed 4-bit matrix as [N][K] halves, scale * (q - z) rounded once: for problems of so many rows that the matrix cores bound
+// them, where decoding once and running on operands in FP16 costs less than decoding in every tile.  The rounding is that of a weight
+// held in FP16.  One thread for 16 packed bytes.
+template <int NG>
+__global__ __launch_bounds__(256) void w4_unpack_kernel(const unsigned char* packed, half_t* out, const W4Format f) {
+  const half_t* const scales = (const half_t*)(packed + f.scales_at(1));
+  const unsigned char* const zeros = packed + f.zeros_at(1);
+  const int64_t pieces = f.weight_bytes / 16;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
+    const int lane = (int)(i & 63), g = lane >> 4, r = lane & 15;
+    const int64_t block = i >> 6, tile = block / f.steps;
+    const int step = (int)(block - tile * f.steps), row = (int)tile * 16 + r;
+    if (row >= f.N) continue;
+    const uintx4 w = *(const uintx4*)(packed + i * 16);
+    half_t* const to = out + (int64_t)row * f.K;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int k = step * W4Format::STEP + s * 32 + g * 8, j = s * NG / 4;
+      if (k >= f.K) continue;
+      const unsigned z = zeros[(block * 16 + r) * NG + j];
+      const half_t scale = scales[((block * 4 + (r >> 2)) * NG + j) * 4 + (r & 3)];
+      *(half8*)(to + k) = w4_values(w[s], w4_minus1(z), w4_minus16(z)) * scale;
+    }
+  }
+}
+hipError_t launch_w4_unpack(const void* packed, half_t* out, const W4Format& f, hipStream_t stream) {
+  const int64_t pieces = f.weight_bytes / 16;
+  const dim3 grid((unsigned)std::min<int64_t>((pieces + 255) / 256, 256 * 32));
+  auto kern = f.ng == 1 ? w4_unpack_kernel<1> : f.ng == 2 ? w4_unpack_kernel<2> : w4_unpack_kernel<4>;
+  hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, (const unsigned char*)packed, out, f);
+  return hipGetLastError();
+}
+
+// y[t] = sum of weight times row over the token's slots, in FP32, in the order of the slots: one thread for eight columns.
 // Slots without an expert have no row.
-__global__ __launch_bounds__(256) void moe_combine_kernel(const half_t* rows, const int* ids, half_t* y, int tokens, int top_k, int width, int64_t ldy) {
+__global__ __launch_bounds__(256) void moe_combine_kernel(const float* rows, const int* ids, const float* weights, half_t* y, int tokens, int top_k, int width, int64_t ldy) {
   const int chunks = width / 8;
   const int64_t total = (int64_t)tokens * chunks;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
@@ -63,9 +98,10 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const half_t* rows, co
     for (int j = 0; j < top_k; ++j) {
       const int64_t slot = t * top_k + j;
       if (ids[slot] < 0) continue;
-      const half8 v = *(const half8*)(rows + slot * width + c);
+      const float w = weights[slot];
+      const floatx4 lo = *(const floatx4*)(rows + slot * width + c), hi = *(const floatx4*)(rows + slot * width + c + 4);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += (float)v[e];
+      for (int e = 0; e < 4; ++e) sum[e] += w * lo[e], sum[4 + e] += w * hi[e];
     }
     half8 o;
 #pragma unroll
@@ -119,42 +155,42 @@ bolt_status check_route(const bolt_moe_route_desc* d) {
   return BOLT_OK;
 }
 
-// Tokens per workgroup of the routing kernel.  One workgroup makes the lists in the same launch.
+// Workgroups of the routing kernel.  Up to 256 tokens one workgroup routes them, a wave for a token, and makes the lists in the same launch;
+// beyond, 16 lanes take a token, and each workgroup of the second launch adds up the counts of all.
 struct RoutePlan {
-  int blocks, block_tokens;
+  int blocks, block_tokens, threads;
 };
 RoutePlan route_plan(const bolt_moe_route_desc& d) {
-  if (d.tokens <= 256) return {1, d.tokens};
-  const int blocks = std::min(256, (d.tokens + 63) / 64), per = (d.tokens + blocks - 1) / blocks;
-  return {(d.tokens + per - 1) / per, per};
+  if (d.tokens <= 256) return {1, d.tokens, kRouteThreads};
+  const int threads = d.tokens <= 8192 ? 512 : 1024, at_once = threads / 16;
+  const int rounds = std::max(1, (d.tokens + at_once * 256 - 1) / (at_once * 256)), per = rounds * at_once;
+  return {(d.tokens + per - 1) / per, per, threads};
 }
 
-template <typename T, bool SIGMOID, int L, int V>
+template <typename T, bool SIGMOID, int L, int V, int NT, bool ONE>
 hipError_t launch_route(const RouteParams& p, int blocks, hipStream_t stream) {
-  constexpr int TEAMS = kRouteThreads / L;
-  const int groups = p.top_groups < p.groups ? TEAMS * (kRouteMaxGroups + p.experts) : 0;
-  const int lists = kRouteWaves * p.experts, head = kRouteMaxExperts + 1 + kRouteWaves;
-  constexpr int MOST = 160 * 1024;
-  auto one = moe_route_kernel<T, SIGMOID, L, V, true>;
-  auto many = moe_route_kernel<T, SIGMOID, L, V, false>;
-  static LdsOptIn opt_in[2];
-  if (hipError_t e = opt_in[0].ensure((const void*)one, MOST); e != hipSuccess) return e;
-  if (hipError_t e = opt_in[1].ensure((const void*)many, MOST); e != hipSuccess) return e;
-  if (blocks == 1) {
-    hipLaunchKernelGGL(one, dim3(1), dim3(kRouteThreads), (head + std::max(groups, lists)) * 4, stream, p);
-    return hipGetLastError();
-  }
-  hipLaunchKernelGGL(many, dim3(blocks), dim3(kRouteThreads), (head + groups) * 4, stream, p);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  auto kern = moe_route_kernel<T, SIGMOID, L, V, NT, ONE>;
+  static LdsOptIn opt_in;
+  if (hipError_t e = opt_in.ensure((const void*)kern, 160 * 1024); e != hipSuccess) return e;
+  const int groups = p.top_groups < p.groups ? NT / L * (kRouteMaxGroups + p.experts) : 0;
+  const int lists = kRouteWaves * std::max(p.experts, 2 * 64), head = kRouteMaxExperts + 1 + kRouteWaves;
+  hipLaunchKernelGGL(kern, dim3(blocks), dim3(NT), (head + (ONE ? std::max(groups, lists) : groups)) * 4, stream, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || ONE) return e;
   hipLaunchKernelGGL(moe_list_kernel, dim3(blocks), dim3(kRouteThreads), (head + lists) * 4, stream, p);
   return hipGetLastError();
 }
 template <typename T, bool SIGMOID>
-hipError_t launch_route_keys(const RouteParams& p, int blocks, hipStream_t stream) {
-  if (p.experts <= 64) return launch_route<T, SIGMOID, 64, 1>(p, blocks, stream);
-  if (p.experts <= 128) return launch_route<T, SIGMOID, 64, 2>(p, blocks, stream);
-  if (p.experts <= 256) return launch_route<T, SIGMOID, 64, 4>(p, blocks, stream);
-  return launch_route<T, SIGMOID, 64, 8>(p, blocks, stream);
+hipError_t launch_route_keys(const RouteParams& p, const RoutePlan& plan, hipStream_t stream) {
+  auto keys = [&](auto v64) {
+    constexpr int V = decltype(v64)::value;
+    if (plan.blocks == 1) return launch_route<T, SIGMOID, 64, V, 1024, true>(p, 1, stream);
+    if (plan.threads == 512) return launch_route<T, SIGMOID, 16, 4 * V, 512, false>(p, plan.blocks, stream);
+    return launch_route<T, SIGMOID, 16, 4 * V, 1024, false>(p, plan.blocks, stream);
+  };
+  if (p.experts <= 64) return keys(std::integral_constant<int, 1>{});
+  if (p.experts <= 128) return keys(std::integral_constant<int, 2>{});
+  if (p.experts <= 256) return keys(std::integral_constant<int, 4>{});
+  return keys(std::integral_constant<int, 8>{});
 }
 
 bolt_status check_moe(const bolt_moe_desc* d) {
@@ -170,18 +206,93 @@ bolt_status check_moe(const bolt_moe_desc* d) {
   return BOLT_OK;
 }
 
-// Rows of a workgroup in 16s, from the rows that share a weight matrix.
-int row_blocks_of(double rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+int64_t blocks_of(int64_t v, int64_t by) { return (v + by - 1) / by; }
+
+// ---- which kernel runs a linear layer with 4-bit weights --------------------------------------------------------------------
+// Estimated time in us: a fit to 6 shapes x 13 row counts, one workgroup's step in us times its steps and its rounds of 256 workgroups.  Two
+// workgroups that share a compute unit (LDS of 78 KB) take 1.55 to 1.6 times as long as one alone.  Measured, rows of A x tile 32 x
+// 32, 32 x 64, 64 x 128, 128 x 256 and unpacked: N = K = 4096, 64 rows 9.4 / 12.4 / 28 / 59, 256 rows 32 / 20 / 29 / 62, 1024 rows 150 /
+// 77 / 46 / 64 / 78, 2048 rows - / 152 / 92 / 71 / 82; 12288 x 4096, 1024 rows 430 / 225 / 128 / 128 / 108.
+struct DenseTile {
+  SharedTile tile;
+  int rows, cols, sets;  // sets: of waves that split the reduction
+  double step_us;
+  bool pairs;            // two workgroups fit a compute unit
+};
+constexpr DenseTile kDenseTiles[] = {{SharedTile::ROWS32_COLS32, 32, 32, 4, 0.72, false},
+                                     {SharedTile::ROWS32_COLS64, 32, 64, 2, 0.57, true},
+                                     {SharedTile::ROWS64_COLS128, 64, 128, 1, 0.78, true},
+                                     {SharedTile::ROWS128_COLS256, 128, 256, 1, 1.73, false}};
+// Groups of 32 (64) columns: four (two) times as many sums to scale per step.
+double dense_us(const DenseTile& t, int64_t M, int64_t N, int64_t steps, int group) {
+  const double rounds = (double)blocks_of(blocks_of(M, t.rows) * blocks_of(N, t.cols), 256);
+  const double factor = t.pairs ? (rounds <= 1 ? 1.0 : rounds <= 2 ? 1.55 : 0.8 * rounds) : rounds <= 1 ? 1.0 : 1.1 * rounds;
+  return 3.3 + (double)blocks_of(steps, t.sets) * t.step_us * factor * (group == 32 ? 1.4 : group == 64 ? 1.1 : 1.0);
+}
+const DenseTile& dense_tile(int64_t M, int64_t N, int64_t steps, int group) {
+  const DenseTile* best = &kDenseTiles[0];
+  for (const DenseTile& t : kDenseTiles)
+    if (dense_us(t, M, N, steps, group) < dense_us(*best, M, N, steps, group)) best = &t;
+  return *best;
+}
+// Unpacking (10 bytes written and read for 4 weights, 4 TB/s) and a GEMM on FP16 operands, against the best tile on packed ones.
+bool dense_unpacks(int64_t M, int64_t N, int64_t K, int group) {
+  if (M < 512 || N * K * 2 > INT32_MAX) return false;  // (unpacked weights are addressed with 31-bit offsets)
+  const int64_t steps = W4Format(N, K, group).steps;
+  const double unpacked = 9.0 + 2.5 * (double)N * K / 4.0e6 + 2.0 * (double)M * N * K / 1.25e9;
+  return unpacked < dense_us(dense_tile(M, N, steps, group), M, N, steps, group);
+}
+
+// ---- which kernels run the experts ------------------------------------------------------------------------------------
+// The host does not know the lists: it goes by the experts that the slots reach if all are asked for equally often, and the rows of each.
+struct Spread {
+  double experts, rows;
+  explicit Spread(const bolt_moe_desc& d) {
+    const double slots = (double)d.tokens * d.top_k, E = d.experts;
+    experts = std::max(1.0, E * (1.0 - std::pow(1.0 - 1.0 / E, slots)));
+    rows = slots / experts;
+  }
+  // workgroups with blocks of `by` rows: every expert's last block is half full on average
+  double blocks(int by) const { return experts * std::max(1.0, rows / by + 0.5); }
+};
+enum class Family { FEW, SHARED, MANY };
+struct Choice {
+  Family family;
+  SharedTile shared;
+  ManyTile many;
+};
+// 4 bits, us for 2048 wide, 1024 hidden, 32 experts, 4 per token, few rows / 16 x 64 / 16 x 128 / 32 x 128 / 64 x 128 / 128 x 256:
+// 1 token 15 / 19 / 26; 4 tokens 27 / 23 / 26; 32 tokens 42 / 38 / 34 / 37; 128 tokens 67 / 53 / 45 / 49 / 53 / 68; 512 tokens 157 / 120 / 93 /
+// 77 / 90 / 131; 1024 tokens - / - / 162 / 127 / 127 / 143; 2048 tokens - / - / - / - / 246 / 225.
+Choice choose_w4(const Spread& s, int weight_rows) {
+  if (s.experts * blocks_of(weight_rows, 32) <= 512 && s.rows <= 16) return {Family::FEW, {}, {}};
+  SharedTile t = SharedTile::ROWS128_COLS256;
+  if (s.blocks(16) * blocks_of(weight_rows, 64) <= 768) t = SharedTile::ROWS16_COLS64;
+  else if (s.rows <= 16) t = SharedTile::ROWS16_COLS128;
+  else if (s.rows <= 128) t = SharedTile::ROWS32_COLS128;
+  else if (s.rows <= 256) t = SharedTile::ROWS64_COLS128;
+  return {Family::SHARED, t, {}};
+}
+// FP16, us for the same experts, few rows / shared rows / 64 x 128 / 128 x 128 / 256 x 256: 32 tokens 82 / 90; 128 tokens 116 / 109 / 96 / 105 /
+// 115; 512 tokens 183 / 183 / 128 / 126 / 123; 2048 tokens - / - / 215 / 210 / 191; and 1000 wide, 2504 hidden, no gate, 8 experts, 2 per token:
+// 64 tokens 31 / 31 / 47 / 36 / 83, 1024 tokens - / - / 89 / 81 / 117, 4096 tokens - / - / 205 / 208 / 166.
+Choice choose_f16(const Spread& s, int weight_rows, bool offsets_fit) {
+  if (s.rows <= 10 || !offsets_fit) return {Family::FEW, {}, {}};
+  if (s.rows >= 192 && s.blocks(256) * blocks_of(weight_rows, 256) >= 144) return {Family::MANY, {}, ManyTile::ROWS256};
+  if (s.rows <= 48 && s.blocks(32) * blocks_of(weight_rows, 64) <= 768) return {Family::SHARED, {}, {}};
+  if (s.rows >= 48 && s.blocks(128) * blocks_of(weight_rows, 128) <= 512) return {Family::MANY, {}, ManyTile::ROWS128};
+  return {Family::MANY, {}, ManyTile::ROWS64};
+}
 
 struct MoeWorkspace {
-  int64_t hidden_at, rows_at, bytes;  // [slots][hidden] in the lists' order, [slots][width] by slot, halves
+  int64_t hidden_at, rows_at, bytes;  // [slots][hidden] halves in the lists' order, [slots][width] floats by slot
 };
 MoeWorkspace moe_workspace(const bolt_moe_desc& d) {
   const int64_t slots = (int64_t)d.tokens * d.top_k;
   MoeWorkspace w;
   w.hidden_at = 0;
   w.rows_at = round_up(slots * d.hidden * 2, 256);
-  w.bytes = w.rows_at + round_up(slots * d.width * 2, 256);
+  w.bytes = w.rows_at + round_up(slots * d.width * 4, 256);
   return w;
 }
 
@@ -211,8 +322,8 @@ bolt_status bolt_w4_pack(int32_t N, int32_t K, int32_t group, int32_t count, con
 }
 
 size_t bolt_gemm_w4_workspace_bytes(const bolt_gemm_w4_desc* desc) {
-  (void)desc;
-  return 0;
+  if (check_gemm_w4(desc) != BOLT_OK || !dense_unpacks(desc->M, desc->N, desc->K, desc->group)) return 0;
+  return (size_t)desc->N * desc->K * 2;
 }
 
 bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const void* packed, const void* bias, void* D, void* workspace,
@@ -220,10 +331,12 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   if (bolt_status s = check_gemm_w4(desc); s != BOLT_OK) return s;
   if (!A || !packed || !D) return BOLT_ERR_INVALID_ARG;
   if (!aligned16(A) || !aligned16(packed) || !aligned16(D) || (bias && !aligned16(bias))) return BOLT_ERR_ALIGNMENT;
-  (void)workspace;
-  (void)workspace_bytes;
+  const size_t need = bolt_gemm_w4_workspace_bytes(desc);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return BOLT_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return BOLT_ERR_ALIGNMENT;
   if (desc->M == 0) return BOLT_OK;
   const W4Format f(desc->N, desc->K, desc->group);
+  const hipStream_t st = (hipStream_t)stream;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
   RowsParams p{};
@@ -234,13 +347,23 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   p.zeros = (const unsigned char*)packed + f.zeros_at(1);
   p.bias = bias ? (const half_t*)bias : none;
   p.bias_on = bias ? 1 : 0;
-  p.y = (half_t*)D;
+  p.y = D;
   p.ldy = desc->ldd;
   p.M = desc->M; p.N = desc->N; p.K = desc->K; p.steps = f.steps;
   p.alpha = desc->alpha; p.beta = desc->beta; p.act = desc->act;
-  const int mb = row_blocks_of(desc->M);
-  if ((int64_t)((desc->M + 15) / 16) * ((desc->N + 15) / 16) > kMaxGrid) return BOLT_ERR_UNSUPPORTED;
-  return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, desc->group, mb, (hipStream_t)stream));
+  if (blocks_of(desc->M, 16) * blocks_of(desc->N, 16) > kMaxGrid) return BOLT_ERR_UNSUPPORTED;
+  if (desc->M <= 16) return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, desc->group, st));
+  // (alpha 0: the kernels of many rows start their sums at beta / alpha times the bias)
+  if (need == 0 || desc->alpha == 0.f)
+    return status_of(launch_shared_rows_w4(p, ROWS_DENSE, false, desc->group, dense_tile(desc->M, desc->N, f.steps, desc->group).tile, st));
+  if (launch_w4_unpack(packed, (half_t*)workspace, f, st) != hipSuccess) return BOLT_ERR_LAUNCH;
+  if (desc->act != BOLT_ACT_SILU) {
+    const bolt_gemm_desc g = {desc->M, desc->N, desc->K, desc->lda, desc->K, desc->ldd, desc->alpha, desc->beta, desc->act, BOLT_LAYOUT_NK};
+    return bolt_gemm_epilogue(&g, A, workspace, bias, D, nullptr, nullptr, 0, stream);
+  }
+  p.w = (const unsigned char*)workspace;
+  p.w_stride = (int64_t)p.N * p.K * 2;
+  return status_of(launch_many_rows_f16(p, ROWS_DENSE, false, ManyTile::ROWS256, st));
 }
 
 size_t bolt_moe_route_workspace_bytes(const bolt_moe_route_desc* desc) {
@@ -267,8 +390,8 @@ bolt_status bolt_moe_route(const bolt_moe_route_desc* desc, const void* logits, 
   const bool sigmoid = desc->score == BOLT_SCORE_SIGMOID;
   const hipStream_t st = (hipStream_t)stream;
   if (desc->logits_type == BOLT_TYPE_F16)
-    return status_of(sigmoid ? launch_route_keys<half_t, true>(p, plan.blocks, st) : launch_route_keys<half_t, false>(p, plan.blocks, st));
-  return status_of(sigmoid ? launch_route_keys<float, true>(p, plan.blocks, st) : launch_route_keys<float, false>(p, plan.blocks, st));
+    return status_of(sigmoid ? launch_route_keys<half_t, true>(p, plan, st) : launch_route_keys<half_t, false>(p, plan, st));
+  return status_of(sigmoid ? launch_route_keys<float, true>(p, plan, st) : launch_route_keys<float, false>(p, plan, st));
 }
 
 size_t bolt_moe_workspace_bytes(const bolt_moe_desc* desc) {
@@ -290,16 +413,22 @@ bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const voi
   if (!none) return BOLT_ERR_LAUNCH;
   const bool w4 = desc->weights == BOLT_WEIGHTS_W4, gated = desc->gated != 0;
   const int slots = desc->tokens * desc->top_k, E = desc->experts;
-  const int mb = row_blocks_of((double)slots / E);
   const int up_rows = gated ? 2 * desc->hidden : desc->hidden;
-  if (((int64_t)slots / 16 + E) * ((std::max(desc->hidden, desc->width) + 15) / 16) > kMaxGrid) return BOLT_ERR_UNSUPPORTED;
+  if ((blocks_of(slots, 16) + E) * blocks_of(std::max(up_rows, desc->width), 16) > kMaxGrid) return BOLT_ERR_UNSUPPORTED;
+  // the kernels that stage rows address x, an expert's weights and a tile's rows with 31-bit byte offsets
+  const int64_t most = (1ll << 31) - 1;
+  const bool offsets_fit = (int64_t)desc->tokens * desc->ldx * 2 <= most && (int64_t)up_rows * desc->width * 2 <= most &&
+                           (int64_t)desc->width * desc->hidden * 2 <= most && (int64_t)256 * desc->hidden * 2 <= most;
+  const Spread spread(*desc);
+  const hipStream_t st = (hipStream_t)stream;
 
   RowsParams p{};
   p.M = slots;
-  p.offsets = (const int*)offsets; p.order = (const int*)order; p.slot_weights = (const float*)weights;
+  p.offsets = (const int*)offsets; p.order = (const int*)order;
   p.experts = E; p.top_k = desc->top_k;
   p.alpha = p.beta = 1.f;
   auto product = [&](int N, int K, const void* w, const void* b, int mode) {
+    const bool gate = mode == ROWS_UP && gated;
     p.N = N; p.K = K;
     p.w = (const unsigned char*)w;
     p.bias = b ? (const half_t*)b : none;
@@ -309,20 +438,25 @@ bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const voi
       p.w_stride = f.weight_bytes; p.scale_stride = f.scale_count; p.steps = f.steps;
       p.scales = (const half_t*)((const char*)w + f.scales_at(E));
       p.zeros = (const unsigned char*)w + f.zeros_at(E);
-      return launch_few_rows_w4(p, mode, mode == ROWS_UP && gated, desc->group, mb, (hipStream_t)stream);
+      const Choice c = choose_w4(spread, N);
+      if (c.family == Family::FEW || !offsets_fit) return launch_few_rows_w4(p, mode, gate, desc->group, st);
+      return launch_shared_rows_w4(p, mode, gate, desc->group, c.shared, st);
     }
     p.w_stride = (int64_t)N * K * 2; p.steps = (K + 63) / 64;
-    return launch_few_rows_f16(p, mode, mode == ROWS_UP && gated, mb, (hipStream_t)stream);
+    const Choice c = choose_f16(spread, N, offsets_fit);
+    if (c.family == Family::FEW) return launch_few_rows_f16(p, mode, gate, st);
+    if (c.family == Family::SHARED) return launch_shared_rows_f16(p, mode, gate, st);
+    return launch_many_rows_f16(p, mode, gate, c.many, st);
   };
   half_t* const hidden = (half_t*)((char*)workspace + ws.hidden_at);
-  half_t* const rows = (half_t*)((char*)workspace + ws.rows_at);
+  float* const rows = (float*)((char*)workspace + ws.rows_at);
   p.x = (const half_t*)x; p.ldx = desc->ldx; p.y = hidden; p.ldy = desc->hidden; p.hidden = desc->hidden; p.act = desc->act;
   if (hipError_t e = product(up_rows, desc->width, w_up, b_up, ROWS_UP); e != hipSuccess) return BOLT_ERR_LAUNCH;
   p.x = hidden; p.ldx = desc->hidden; p.y = rows; p.ldy = desc->width; p.act = BOLT_ACT_NONE;
   if (hipError_t e = product(desc->width, desc->hidden, w_down, b_down, ROWS_DOWN); e != hipSuccess) return BOLT_ERR_LAUNCH;
   const int64_t chunks = (int64_t)desc->tokens * (desc->width / 8);
-  hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)std::min<int64_t>((chunks + 255) / 256, 256 * 32)), dim3(256), 0, (hipStream_t)stream, rows,
-                     (const int*)ids, (half_t*)y, desc->tokens, desc->top_k, desc->width, desc->ldy);
+  hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)std::min<int64_t>((chunks + 255) / 256, 256 * 32)), dim3(256), 0, st, rows,
+                     (const int*)ids, (const float*)weights, (half_t*)y, desc->tokens, desc->top_k, desc->width, desc->ldy);
   return status_of(hipGetLastError());
 }
 

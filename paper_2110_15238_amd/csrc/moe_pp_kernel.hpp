@@ -1,0 +1,292 @@
+// The experts' products over many rows, on the two-wave-group ("ping-pong"), persistent scheme of fprop_pp_kernel: a 256 x 256 tile
+// on 8 waves, group 0 (waves 0-3) and group 1 (waves 4-7) sharing the SIMDs pairwise; a wave alternates between a phase that reads
+// fragments and issues direct-to-LDS loads and a phase of nothing but MFMAs, a workgroup barrier after every phase, group 1 one phase
+// behind.  Stages, waits and the epilogue's LDS are as described there: W(t + 1) is loaded by group 0 in phase M(t), X(t + 2) by group 1;
+// the first k-tiles of the next output tile go out before a tile's epilogue, which uses the stages they leave free.
+//
+// What differs: a workgroup finds its tiles from `offsets` (the host knows a bound of their number only); the activation rows may be
+// gathered; with a gate the weight tile alternates 16 gate rows and the 16 value rows of the same columns, so that neighbouring
+// fragments of a wave are the two factors of an output; results leave as halves in the list's order or as FP32 rows by slot.
+// Tiles run in bands of 8 row blocks of an expert, and an XCD's 32 workgroups walk neighbouring tiles: a band's rows stay in its L2 while
+// the expert's weights stream through.
+#pragma once
+#include <type_traits>
+#include <utility>
+
+#include "fprop_pp_kernel.hpp"
+#include "routed_rows.hpp"
+
+namespace bolt {
+
+template <int MODE, bool GATED>
+__global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
+  using T = FpropPpTraits;
+  constexpr int BM = 256, BN = T::BN, BK = T::BK, WTM = BM / 2, WTN = T::WTN;
+  constexpr int FM = WTM / 16, FN = WTN / 16, KS = BK / 32;
+  constexpr int L = 8;  // load instructions per k-tile of a wave: 4 waves x 8 rows of 256 each
+  constexpr int COLS = GATED ? BN / 2 : BN;
+  constexpr bool FLOATS = MODE == ROWS_DOWN;
+
+  extern __shared__ __attribute__((aligned(16))) half_t lds[];
+  half_t* const wring = lds;
+  half_t* const xring = lds + T::W_STAGES * T::W_HALVES;
+  half_t* const free0 = wring + T::W_HALVES;
+  half_t* const free1 = xring + 2 * T::X_HALVES;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = wave >> 2, wq = wave & 3;
+  const int g = lane >> 4, lr = lane & 15;
+  const int n_tiles = (p.K + BK - 1) / BK;
+  const int outputs = GATED ? p.hidden : p.N;
+
+  BlockCounts counts;
+  if constexpr (MODE != ROWS_DENSE) counts = count_row_blocks<BM>(p.offsets, p.experts, lane);
+  const int total = (MODE == ROWS_DENSE ? p.row_blocks : counts.total()) * p.col_blocks;
+
+  // ---- this wave's loader: rows (j * 4 + wq) * 8 + lane / 8 of ONE operand tile, one byte offset per row ---------------------
+  const int lrow = lane >> 3;
+  const int lc16 = ((lane & 7) ^ dma_swizzle<BK>(wq * 8 + lrow)) << 4;
+  unsigned st[L];
+  __amdgpu_buffer_rsrc_t rsrc;
+  const int k_limit_bytes = p.K * 2;
+  int expert, row0, rows, c0;  // the output tile whose operands the loader addresses
+
+  auto setup_tile = [&](int id) {
+    const int tile = xcd_run(id, total);
+    RowBlock at = {0, 0, p.M, 0, p.row_blocks};
+    if constexpr (MODE != ROWS_DENSE) find_row_block<BM>(p.offsets, counts, tile / p.col_blocks, &at);  // (tile < total)
+    // bands of 8 row blocks, in a band the row block fastest
+    const int local = tile - at.first * p.col_blocks, band = local / (8 * p.col_blocks), in_band = local - band * 8 * p.col_blocks;
+    const int height = at.count - band * 8 < 8 ? at.count - band * 8 : 8;
+    const int cb = in_band / height, block = band * 8 + in_band - cb * height;
+    expert = at.expert;
+    row0 = at.lo + block * BM;
+    rows = at.n - block * BM < BM ? at.n - block * BM : BM;
+    c0 = cb * COLS;
+    if (grp == 0) {
+      rsrc = make_rsrc(p.w + expert * p.w_stride, (unsigned)p.w_stride);
+#pragma unroll
+      for (int j = 0; j < L; ++j) {
+        const int r = (j * 4 + wq) * 8 + lrow;
+        const int c = GATED ? c0 + (r >> 5) * 16 + (r & 15) : c0 + r;
+        st[j] = c < outputs ? (unsigned)(c + (GATED && (r & 16) ? p.hidden : 0)) * (unsigned)(p.K * 2) : kInvalidOffset;
+      }
+    } else if (MODE == ROWS_UP) {
+      rsrc = make_rsrc(p.x, 0x7fffffffu);  // (the host keeps x below 2 GiB)
+      int token[L];
+#pragma unroll
+      for (int j = 0; j < L; ++j) {
+        const int r = (j * 4 + wq) * 8 + lrow;
+        token[j] = p.order[row0 + (r < rows ? r : rows - 1)] / p.top_k;
+      }
+#pragma unroll
+      for (int j = 0; j < L; ++j) st[j] = (j * 4 + wq) * 8 + lrow < rows ? (unsigned)token[j] * (unsigned)(p.ldx * 2) : kInvalidOffset;
+    } else {
+      rsrc = make_rsrc(p.x + (int64_t)row0 * p.ldx, (unsigned)(rows * p.ldx * 2));
+#pragma unroll
+      for (int j = 0; j < L; ++j) {
+        const int r = (j * 4 + wq) * 8 + lrow;
+        st[j] = r < rows ? (unsigned)(r * p.ldx * 2) : kInvalidOffset;
+      }
+    }
+  };
+  auto issue_one = [&](auto jc, int kt, half_t* dst) {
+    constexpr int j = decltype(jc)::value;
+    half_t* slot = dst + (j * 4) * 8 * BK + wq * 8 * BK;
+    unsigned sj = st[j];  // (the empty asm: see fprop_pp_kernel, nothing derived from it is to live through the k loop)
+    asm volatile("" : "+v"(sj));
+    const int kb = kt * (BK * 2) + lc16;
+    const unsigned off = (sj + (unsigned)kb) | (kb < k_limit_bytes ? 0u : kInvalidOffset);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, BOLT_LDS_PTR(slot), 16, off, 0, 0, 0);
+  };
+  auto issue_first_tiles = [&]() {
+    if (grp == 0) {
+      for_constants<L>([&](auto jc) { issue_one(jc, 0, wring); });
+    } else {
+      for_constants<L>([&](auto jc) { issue_one(jc, 0, xring); });
+      for_constants<L>([&](auto jc) { issue_one(jc, 1, xring + T::X_HALVES); });
+    }
+  };
+
+  floatx4 acc[FN][FM];
+  half8 xf[KS][FM], wf[KS][FN];
+  constexpr int NREAD = KS * (FM + FN);
+  auto read_one = [&](const half_t* xs, const half_t* ws, auto rc) {
+    constexpr int r = decltype(rc)::value, k = r / (FM + FN), i = r % (FM + FN);
+    const int chunk = k * 4 + g;
+    if constexpr (i < FM) xf[k][i] = *(const half8*)(xs + dma_chunk_offset<BK>(grp * WTM + i * 16 + lr, chunk));
+    else wf[k][i - FM] = *(const half8*)(ws + dma_chunk_offset<BK>(wq * WTN + (i - FM) * 16 + lr, chunk));
+  };
+  auto m_phase = [&](half_t* dst, int kt, const half_t* xs, const half_t* ws) {
+    for_constants<L>([&](auto jc) {
+      constexpr int j = decltype(jc)::value, r0 = j * NREAD / L, r1 = (j + 1) * NREAD / L;
+      issue_one(jc, kt, dst);
+      for_constants<r1 - r0>([&](auto ic) { read_one(xs, ws, std::integral_constant<int, r0 + decltype(ic)::value>{}); });
+    });
+    for_constants<L>([&](auto jc) {
+      constexpr int j = decltype(jc)::value;
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);                                            // one load
+      __builtin_amdgcn_sched_group_barrier(0x100, (j + 1) * NREAD / L - j * NREAD / L, 0);  // its share of reads
+    });
+  };
+  auto c_phase = [&]() {
+    for_constants<KS * FM * FN>([&](auto ic) {
+      constexpr int i = decltype(ic)::value, k = i / (FM * FN), a = (i / FM) % FN, b = i % FM;
+      acc[a][b] = mfma_16x16x32(wf[k][a], xf[k][b], acc[a][b]);
+    });
+  };
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  auto wait_reads = [] { __builtin_amdgcn_s_waitcnt(0xC07F); };          // lgkmcnt(0)
+  auto wait_loads_0 = [] { __builtin_amdgcn_s_waitcnt(0x0F70); };        // vmcnt(0)
+  auto wait_loads_x = [] { __builtin_amdgcn_s_waitcnt(0x0F70 | L); };    // vmcnt(L): all but the newest activation tile
+
+  // The accumulators of a tile start at the bias.
+  half4 bias_q[FN];
+  auto column = [&](int a, int gl) { return GATED ? wq * (WTN / 2) + (a >> 1) * 16 + gl * 4 : wq * WTN + a * 16 + gl * 4; };
+  auto load_bias = [&]() {
+#pragma unroll
+    for (int a = 0; a < FN; ++a) {
+      const int c = c0 + column(a, g), n = (c < outputs ? c : 0) + (GATED && (a & 1) ? p.hidden : 0);
+      bias_q[a] = *(const half4*)(p.bias + (expert * (int64_t)p.N + n) * p.bias_on);
+    }
+  };
+
+  // A wave group moves its rows through its own free stage (32 KB), R at a time: halves in the list's order, or floats by slot.
+  // (FLOATS: lane i holds the slot of the group's row wq + 4 i, which this wave stores.)
+  auto epilogue = [&](int erow0, int erows, int ec0, int slot) {
+    int elane = lane;
+    asm volatile("" : "+v"(elane));  // (as in fprop_pp_kernel: the addresses below are not to live through the k loop)
+    const int eg = elane >> 4, elr = elane & 15, gtid = wq * 64 + elane;
+    half_t* const stage = grp == 0 ? free0 : free1;
+    constexpr int R = FLOATS ? 32 : (GATED ? 128 : 64) < WTM ? (GATED ? 128 : 64) : WTM;
+    constexpr int CPR = COLS * (FLOATS ? 4 : 2) / 16;  // 16-byte chunks of a row
+    const int r_half = grp * WTM;
+    for_constants<WTM / R>([&](auto sc) {
+      constexpr int sp = decltype(sc)::value;
+      barrier_after_lds_writes();
+#pragma unroll
+      for (int a = 0; a < FN; a += GATED ? 2 : 1)
+#pragma unroll
+        for (int bb = 0; bb < R / 16; ++bb) {
+          const int b = sp * (R / 16) + bb, srow = bb * 16 + elr, nl = column(a, eg);
+          floatx4 v = acc[a][b];
+          if constexpr (MODE == ROWS_DENSE) v *= p.alpha;
+          if constexpr (FLOATS) {
+            *(floatx4*)((float*)stage + srow * BN + (((nl >> 2) ^ (srow & 15)) << 2)) = v;
+          } else {
+v = apply_act4(v, p.act);
+            if constexpr (GATED) v *= acc[a + 1][b];
+            half4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = (half_t)v[e];
+            *(half4*)(stage + srow * COLS + (((nl >> 3) ^ ctile_swizzle<CPR>(srow)) << 3) + (nl & 4)) = o;
+          }
+        }
+      barrier_after_lds_writes();
+      if constexpr (FLOATS) {
+        const int c = ec0 + elane * 4;
+        if (c < outputs) {
+#pragma unroll
+          for (int i = 0; i < R / 4; ++i) {  // a wave stores one row of 256 floats at a time
+            const int srow = i * 4 + wq, r = r_half + sp * R + srow;
+            if (r < erows) {
+              const int64_t to = __builtin_amdgcn_readlane(slot, sp * (R / 4) + i);
+              const floatx4 v = *(const floatx4*)((const float*)stage + srow * BN + ((elane ^ (srow & 15)) << 2));
+              __builtin_nontemporal_store(v, (floatx4*)((float*)p.y + to * p.ldy + c));
+            }
+          }
+        }
+      } else {
+        const int chunk = gtid % CPR, first = gtid / CPR, c = ec0 + chunk * 8;
+        if (c < outputs) {
+#pragma unroll
+          for (int i = 0; i < R * CPR / 256; ++i) {
+            const int srow = first + i * (256 / CPR), r = r_half + sp * R + srow;
+            if (r < erows)
+              *(half8*)((half_t*)p.y + (int64_t)(erow0 + r) * p.ldy + c) = *(const half8*)(stage + srow * COLS + ((chunk ^ ctile_swizzle<CPR>(srow)) << 3));
+          }
+        }
+      }
+    });
+  };
+
+  int tile = blockIdx.x;
+  if (tile >= total) return;
+  setup_tile(tile);
+  load_bias();
+  issue_first_tiles();
+  while (true) {
+    if (grp == 0) wait_loads_0();
+    else wait_loads_x();
+    wait_reads();
+    const float bias_scale = MODE == ROWS_DENSE ? p.beta / p.alpha : 1.f;  // (the host keeps alpha from being zero)
+#pragma unroll
+    for (int a = 0; a < FN; ++a)
+#pragma unroll
+      for (int b = 0; b < FM; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[a][b][e] = (float)bias_q[a][e] * bias_scale;
+    raw_barrier();
+    if (grp == 1) raw_barrier();
+    int ws_cur = 0, xs_cur = 0;
+    for (int t = 0; t < n_tiles; ++t) {
+      const int ws_next = ws_cur ^ 1;
+      const int xs_fill = xs_cur == 0 ? 2 : xs_cur - 1;
+      const half_t* xs = xring + xs_cur * T::X_HALVES;
+      const half_t* ws = wring + ws_cur * T::W_HALVES;
+      fence();
+      // both groups run the same code on their own rows, offsets and stage
+      m_phase(grp == 0 ? wring + ws_next * T::W_HALVES : xring + xs_fill * T::X_HALVES, t + 1 + grp, xs, ws);
+      wait_reads();
+      if (grp == 1) wait_loads_x();  // X(t + 1) has landed
+      fence();
+      raw_barrier();
+      fence();
+      __builtin_amdgcn_s_setprio(1);
+      c_phase();
+      __builtin_amdgcn_s_setprio(0);
+      if (grp == 0) wait_loads_0();  // W(t + 1) has landed
+      fence();
+      raw_barrier();
+      ws_cur = ws_next;
+      xs_cur = xs_cur == 2 ? 0 : xs_cur + 1;
+    }
+    if (grp == 0) raw_barrier();
+    // nothing of this workgroup is on its way into LDS any more, and nobody reads a stage
+    wait_loads_0();
+    raw_barrier();
+    const int erow0 = row0, erows = rows, ec0 = c0;
+    int slot = 0;  // (requested ahead of the next tile's operands, which it would have to wait for)
+    if constexpr (FLOATS) {
+      int elane = lane;
+      asm volatile("" : "+v"(elane));
+      const int r = grp * WTM + wq + 4 * (elane & 31);
+      slot = p.order[row0 + (r < rows ? r : rows - 1)];
+    }
+    tile += gridDim.x;
+    const bool more = tile < total;
+    if (more) {
+      setup_tile(tile);
+      load_bias();
+      issue_first_tiles();
+    }
+    epilogue(erow0, erows, ec0, slot);
+    if (!more) break;
+  }
+}
+
+template <int MODE, bool GATED>
+hipError_t launch_moe_pp(RowsParams p, hipStream_t stream) {
+  auto kern = moe_pp_kernel<MODE, GATED>;
+  static LdsOptIn opt_in;
+  if (hipError_t e = opt_in.ensure((const void*)kern, FpropPpTraits::LDS_BYTES); e != hipSuccess) return e;
+  constexpr int COLS = GATED ? FpropPpTraits::BN / 2 : FpropPpTraits::BN, kComputeUnits = 256;
+  p.col_blocks = ((GATED ? p.hidden : p.N) + COLS - 1) / COLS;
+  p.row_blocks = row_blocks<256>(p, MODE);
+  const int64_t most = (int64_t)p.row_blocks * p.col_blocks;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(most < kComputeUnits ? most : kComputeUnits)), dim3(512), FpropPpTraits::LDS_BYTES, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace bolt

@@ -31,7 +31,7 @@ struct RouteParams {
 };
 
 static constexpr int kRouteMaxExperts = 512, kRouteMaxTopK = 16, kRouteMaxGroups = 16;
-static constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;
+static constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;  // of a workgroup that makes lists
 
 // exp(x) for x <= 0 (softmax) or of either sign (sigmoid) to about 2 units in the last place: the product with log2 e in two parts.
 __device__ __forceinline__ float route_exp(float x) {
@@ -46,15 +46,28 @@ __device__ __forceinline__ float route_sigmoid(float x) {
   return x < -88.f ? 0.f : 1.f / (1.f + route_exp(-x));
 }
 
-template <int L, typename T, typename F>
-__device__ __forceinline__ T route_reduce(T v, F f) {
-#pragma unroll
-  for (int d = 1; d < L; d <<= 1) v = f(v, __shfl_xor(v, d));
-  return v;
-}
 struct MaxF { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 struct SumF { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 struct MinI { __device__ __forceinline__ int operator()(int a, int b) const { return a < b ? a : b; } };
+// f over the L lanes of a token, to each of them: lanes exchanged inside rows of 16 (1, 2, 7 and 15 apart by mirroring), then between
+// the four rows.  (Shuffles through LDS take ten times as long as these exchanges, and a token's choice is a chain of them.)
+template <int L, typename T, typename F>
+__device__ __forceinline__ T route_reduce(T v, F f) {
+  static_assert(L == 16 || L == 64, "lanes of a token");
+  auto with = [&](auto ctrl) {
+    const int o = __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, true);
+    v = f(v, __builtin_bit_cast(T, o));
+  };
+  with(std::integral_constant<int, 0xb1>{});   // quad_perm 1 0 3 2
+  with(std::integral_constant<int, 0x4e>{});   // quad_perm 2 3 0 1
+  with(std::integral_constant<int, 0x141>{});  // row_half_mirror
+  with(std::integral_constant<int, 0x140>{});  // row_mirror
+  if constexpr (L == 64) {
+    auto row = [&](int r) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), r * 16)); };
+    v = f(f(row(0), row(1)), f(row(2), row(3)));
+  }
+  return v;
+}
 
 // LDS written by some lanes of a wave is read by others of the same wave.
 __device__ __forceinline__ void route_wave_sync() {
@@ -225,18 +238,19 @@ __device__ __forceinline__ void route_place(F id_of, int s0, int s1, const int* 
   }
 }
 
-// `block_tokens` tokens per workgroup, kRouteThreads / L at a time.  ONE: a single workgroup, which makes the lists as well; otherwise the
+// `block_tokens` tokens per workgroup, NT / L at a time.  ONE: a single workgroup, which makes the lists as well; otherwise the
 // workgroup's counts per expert go to `counts` for moe_list_kernel.
-template <typename T, bool SIGMOID, int L, int V, bool ONE>
-__global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(const RouteParams p) {
+template <typename T, bool SIGMOID, int L, int V, int NT, bool ONE>
+__global__ __launch_bounds__(NT) void moe_route_kernel(const RouteParams p) {
+  static_assert(!ONE || NT == kRouteThreads, "lists");
   extern __shared__ __attribute__((aligned(16))) int route_lds[];
   int* const n = route_lds;                        // [experts + 1]
   int* const wave_sums = n + kRouteMaxExperts + 1;  // [kRouteWaves]
   int* const rest = wave_sums + kRouteWaves;
   const int tid = threadIdx.x, l = tid % L, team = tid / L;
-  constexpr int TEAMS = kRouteThreads / L;
+  constexpr int TEAMS = NT / L;
   float* const shared = (float*)rest + team * (kRouteMaxGroups + p.experts);
-  for (int e = tid; e <= p.experts; e += kRouteThreads) n[e] = 0;
+  for (int e = tid; e <= p.experts; e += NT) n[e] = 0;
   __syncthreads();
   const int64_t t0 = (int64_t)blockIdx.x * p.block_tokens;
   const int64_t t1 = t0 + p.block_tokens < p.tokens ? t0 + p.block_tokens : p.tokens;
@@ -260,7 +274,7 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(const RoutePar
     route_place([&](int s) { return p.ids[s]; }, 0, slots, n, rest, p.experts, p.order, tid);
   } else {
     __syncthreads();
-    for (int e = tid; e < p.experts; e += kRouteThreads) p.counts[(int64_t)blockIdx.x * p.experts + e] = n[e];
+    for (int e = tid; e < p.experts; e += NT) p.counts[(int64_t)blockIdx.x * p.experts + e] = n[e];
   }
 }
 
@@ -272,17 +286,32 @@ __global__ __launch_bounds__(kRouteThreads) void moe_list_kernel(const RoutePara
   int* const wave_sums = n + kRouteMaxExperts + 1;
   int* const rest = wave_sums + kRouteWaves;
   const int tid = threadIdx.x, E = p.experts;
+  // a thread adds up every SLICES-th workgroup's counts of one expert
+  int pad = 64;
+  while (pad < E) pad *= 2;
+  const int slices = kRouteThreads / pad, e = tid & (pad - 1), slice = tid / pad;
   int all = 0, before = 0;
-  if (tid < E)
-    for (int b = 0; b < (int)gridDim.x; ++b) {
-      const int c = p.counts[(int64_t)b * E + tid];
+  if (e < E) {
+#pragma unroll 8
+    for (int b = slice; b < (int)gridDim.x; b += slices) {
+      const int c = p.counts[(int64_t)b * E + e];
       all += c;
       before += b < (int)blockIdx.x ? c : 0;
+    }
+  }
+  rest[tid] = all;
+  rest[kRouteThreads + tid] = before;
+  __syncthreads();
+  all = before = 0;
+  if (tid < E)
+    for (int i = 0; i < slices; ++i) {
+      all += rest[i * pad + tid];
+      before += rest[kRouteThreads + i * pad + tid];
     }
   if (tid < E) n[tid] = all;
   route_scan(n, wave_sums, E, tid);
   if (blockIdx.x == 0)
-    for (int e = tid; e <= E; e += kRouteThreads) p.offsets[e] = n[e];
+    for (int i = tid; i <= E; i += kRouteThreads) p.offsets[i] = n[i];
   const int listed = n[E];
   __syncthreads();
   if (tid < E) n[tid] += before;
