@@ -50,9 +50,11 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
   unsigned st[L];
   __amdgpu_buffer_rsrc_t rsrc;
   const int k_limit_bytes = p.K * 2;
-  int expert, row0, rows, c0;  // the output tile whose operands the loader addresses
-
-  auto setup_tile = [&](int id) {
+  // An output tile.  The next one is looked up while the first loads of a tile are on their way, not between two tiles.
+  struct Tile {
+    int expert, row0, rows, c0;
+  };
+  auto find_tile = [&](int id) {
     const int tile = xcd_run(id, total);
     RowBlock at = {0, 0, p.M, 0, p.row_blocks};
     if constexpr (MODE != ROWS_DENSE) find_row_block<BM>(p.offsets, counts, tile / p.col_blocks, &at);  // (tile < total)
@@ -60,34 +62,35 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
     const int local = tile - at.first * p.col_blocks, band = local / (8 * p.col_blocks), in_band = local - band * 8 * p.col_blocks;
     const int height = at.count - band * 8 < 8 ? at.count - band * 8 : 8;
     const int cb = in_band / height, block = band * 8 + in_band - cb * height;
-    expert = at.expert;
-    row0 = at.lo + block * BM;
-    rows = at.n - block * BM < BM ? at.n - block * BM : BM;
-    c0 = cb * COLS;
+    return Tile{at.expert, at.lo + block * BM, at.n - block * BM < BM ? at.n - block * BM : BM, cb * COLS};
+  };
+  // UP: the byte offset of one row of the tile's tokens per lane, of those this wave loads: row (lane / 8 * 4 + wq) * 8 + lane % 8.
+  auto find_row = [&](const Tile& t) {
+    const int r = (lane >> 3) * 32 + wq * 8 + (lane & 7);
+    const unsigned token = (unsigned)(p.order[t.row0 + (r < t.rows ? r : t.rows - 1)] / p.top_k);
+    return r < t.rows ? token * (unsigned)(p.ldx * 2) : kInvalidOffset;
+  };
+  Tile cur, next;
+  unsigned next_row = 0;
+  auto setup_tile = [&](const Tile& t, unsigned row) {
     if (grp == 0) {
-      rsrc = make_rsrc(p.w + expert * p.w_stride, (unsigned)p.w_stride);
+      rsrc = make_rsrc(p.w + t.expert * p.w_stride, (unsigned)p.w_stride);
 #pragma unroll
       for (int j = 0; j < L; ++j) {
         const int r = (j * 4 + wq) * 8 + lrow;
-        const int c = GATED ? c0 + (r >> 5) * 16 + (r & 15) : c0 + r;
+        const int c = GATED ? t.c0 + (r >> 5) * 16 + (r & 15) : t.c0 + r;
         st[j] = c < outputs ? (unsigned)(c + (GATED && (r & 16) ? p.hidden : 0)) * (unsigned)(p.K * 2) : kInvalidOffset;
       }
     } else if (MODE == ROWS_UP) {
       rsrc = make_rsrc(p.x, 0x7fffffffu);  // (the host keeps x below 2 GiB)
-      int token[L];
 #pragma unroll
-      for (int j = 0; j < L; ++j) {
-        const int r = (j * 4 + wq) * 8 + lrow;
-        token[j] = p.order[row0 + (r < rows ? r : rows - 1)] / p.top_k;
-      }
-#pragma unroll
-      for (int j = 0; j < L; ++j) st[j] = (j * 4 + wq) * 8 + lrow < rows ? (unsigned)token[j] * (unsigned)(p.ldx * 2) : kInvalidOffset;
+      for (int j = 0; j < L; ++j) st[j] = (unsigned)__shfl((int)row, j * 8 + lrow);
     } else {
-      rsrc = make_rsrc(p.x + (int64_t)row0 * p.ldx, (unsigned)(rows * p.ldx * 2));
+      rsrc = make_rsrc(p.x + (int64_t)t.row0 * p.ldx, (unsigned)(((int64_t)(t.rows - 1) * p.ldx + p.K) * 2));
 #pragma unroll
       for (int j = 0; j < L; ++j) {
         const int r = (j * 4 + wq) * 8 + lrow;
-        st[j] = r < rows ? (unsigned)(r * p.ldx * 2) : kInvalidOffset;
+        st[j] = r < t.rows ? (unsigned)(r * p.ldx * 2) : kInvalidOffset;
       }
     }
   };
@@ -144,24 +147,36 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
   // The accumulators of a tile start at the bias.
   half4 bias_q[FN];
   auto column = [&](int a, int gl) { return GATED ? wq * (WTN / 2) + (a >> 1) * 16 + gl * 4 : wq * WTN + a * 16 + gl * 4; };
-  auto load_bias = [&]() {
+  auto load_bias = [&](const Tile& t) {
 #pragma unroll
     for (int a = 0; a < FN; ++a) {
-      const int c = c0 + column(a, g), n = (c < outputs ? c : 0) + (GATED && (a & 1) ? p.hidden : 0);
-      bias_q[a] = *(const half4*)(p.bias + (expert * (int64_t)p.N + n) * p.bias_on);
+      const int c = t.c0 + column(a, g), n = (c < outputs ? c : 0) + (GATED && (a & 1) ? p.hidden : 0);
+      bias_q[a] = *(const half4*)(p.bias + (t.expert * (int64_t)p.N + n) * p.bias_on);
     }
   };
 
-  // A wave group moves its rows through its own free stage (32 KB), R at a time: halves in the list's order, or floats by slot.
-  // (FLOATS: lane i holds the slot of the group's row wq + 4 i, which this wave stores.)
-  auto epilogue = [&](int erow0, int erows, int ec0, int slot) {
+  // Halves: a wave group moves its rows through its own free stage (32 KB), R at a time, so that whole row segments are stored.
+  // Floats (DOWN): a quad per lane straight to the slot's row, 64 bytes of a row by four lanes; slot[b] is that of row 16 b + lane % 16.
+  auto epilogue = [&](const Tile& t, const int (&slot)[FM]) {
     int elane = lane;
     asm volatile("" : "+v"(elane));  // (as in fprop_pp_kernel: the addresses below are not to live through the k loop)
-    const int eg = elane >> 4, elr = elane & 15, gtid = wq * 64 + elane;
+    const int eg = elane >> 4, elr = elane & 15, gtid = wq * 64 + elane, r_half = grp * WTM;
+    if constexpr (FLOATS) {
+#pragma unroll
+      for (int b = 0; b < FM; ++b) {
+        if (r_half + b * 16 + elr >= t.rows) continue;
+        float* const to = (float*)p.y + (int64_t)slot[b] * p.ldy;
+#pragma unroll
+        for (int a = 0; a < FN; ++a) {
+          const int c = t.c0 + column(a, eg);
+          if (c < outputs) *(floatx4*)(to + c) = acc[a][b];
+        }
+      }
+      return;
+    }
     half_t* const stage = grp == 0 ? free0 : free1;
-    constexpr int R = FLOATS ? 32 : (GATED ? 128 : 64) < WTM ? (GATED ? 128 : 64) : WTM;
-    constexpr int CPR = COLS * (FLOATS ? 4 : 2) / 16;  // 16-byte chunks of a row
-    const int r_half = grp * WTM;
+    constexpr int R = (GATED ? 128 : 64) < WTM ? (GATED ? 128 : 64) : WTM;
+    constexpr int CPR = COLS / 8;  // 16-byte chunks of a row
     for_constants<WTM / R>([&](auto sc) {
       constexpr int sp = decltype(sc)::value;
       barrier_after_lds_writes();
@@ -172,40 +187,21 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
           const int b = sp * (R / 16) + bb, srow = bb * 16 + elr, nl = column(a, eg);
           floatx4 v = acc[a][b];
           if constexpr (MODE == ROWS_DENSE) v *= p.alpha;
-          if constexpr (FLOATS) {
-            *(floatx4*)((float*)stage + srow * BN + (((nl >> 2) ^ (srow & 15)) << 2)) = v;
-          } else {
-v = apply_act4(v, p.act);
-            if constexpr (GATED) v *= acc[a + 1][b];
-            half4 o;
+          v = apply_act4(v, p.act);
+          if constexpr (GATED) v *= acc[a + 1][b];
+          half4 o;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = (half_t)v[e];
-            *(half4*)(stage + srow * COLS + (((nl >> 3) ^ ctile_swizzle<CPR>(srow)) << 3) + (nl & 4)) = o;
-          }
+          for (int e = 0; e < 4; ++e) o[e] = (half_t)v[e];
+          *(half4*)(stage + srow * COLS + (((nl >> 3) ^ ctile_swizzle<CPR>(srow)) << 3) + (nl & 4)) = o;
         }
       barrier_after_lds_writes();
-      if constexpr (FLOATS) {
-        const int c = ec0 + elane * 4;
-        if (c < outputs) {
+      const int chunk = gtid % CPR, first = gtid / CPR, c = t.c0 + chunk * 8;
+      if (c < outputs) {
 #pragma unroll
-          for (int i = 0; i < R / 4; ++i) {  // a wave stores one row of 256 floats at a time
-            const int srow = i * 4 + wq, r = r_half + sp * R + srow;
-            if (r < erows) {
-              const int64_t to = __builtin_amdgcn_readlane(slot, sp * (R / 4) + i);
-              const floatx4 v = *(const floatx4*)((const float*)stage + srow * BN + ((elane ^ (srow & 15)) << 2));
-              __builtin_nontemporal_store(v, (floatx4*)((float*)p.y + to * p.ldy + c));
-            }
-          }
-        }
-      } else {
-        const int chunk = gtid % CPR, first = gtid / CPR, c = ec0 + chunk * 8;
-        if (c < outputs) {
-#pragma unroll
-          for (int i = 0; i < R * CPR / 256; ++i) {
-            const int srow = first + i * (256 / CPR), r = r_half + sp * R + srow;
-            if (r < erows)
-              *(half8*)((half_t*)p.y + (int64_t)(erow0 + r) * p.ldy + c) = *(const half8*)(stage + srow * COLS + ((chunk ^ ctile_swizzle<CPR>(srow)) << 3));
-          }
+        for (int i = 0; i < R * CPR / 256; ++i) {
+          const int srow = first + i * (256 / CPR), r = r_half + sp * R + srow;
+          if (r < t.rows)
+            *(half8*)((half_t*)p.y + (int64_t)(t.row0 + r) * p.ldy + c) = *(const half8*)(stage + srow * COLS + ((chunk ^ ctile_swizzle<CPR>(srow)) << 3));
         }
       }
     });
@@ -213,10 +209,16 @@ v = apply_act4(v, p.act);
 
   int tile = blockIdx.x;
   if (tile >= total) return;
-  setup_tile(tile);
-  load_bias();
+  cur = find_tile(tile);
+  setup_tile(cur, MODE == ROWS_UP ? find_row(cur) : 0);
+  load_bias(cur);
   issue_first_tiles();
   while (true) {
+    const bool more = tile + (int)gridDim.x < total;
+    if (more) {
+      next = find_tile(tile + gridDim.x);
+      if (MODE == ROWS_UP && grp == 1) next_row = find_row(next);
+    }
     if (grp == 0) wait_loads_0();
     else wait_loads_x();
     wait_reads();
@@ -256,22 +258,24 @@ v = apply_act4(v, p.act);
     // nothing of this workgroup is on its way into LDS any more, and nobody reads a stage
     wait_loads_0();
     raw_barrier();
-    const int erow0 = row0, erows = rows, ec0 = c0;
-    int slot = 0;  // (requested ahead of the next tile's operands, which it would have to wait for)
+    int slot[FM];  // (requested ahead of the next tile's operands, which they would have to wait for)
     if constexpr (FLOATS) {
       int elane = lane;
       asm volatile("" : "+v"(elane));
-      const int r = grp * WTM + wq + 4 * (elane & 31);
-      slot = p.order[row0 + (r < rows ? r : rows - 1)];
+#pragma unroll
+      for (int b = 0; b < FM; ++b) {
+        const int r = grp * WTM + b * 16 + (elane & 15);
+        slot[b] = p.order[cur.row0 + (r < cur.rows ? r : cur.rows - 1)];
+      }
     }
-    tile += gridDim.x;
-    const bool more = tile < total;
     if (more) {
-      setup_tile(tile);
-      load_bias();
+      setup_tile(next, next_row);
+      load_bias(next);
       issue_first_tiles();
     }
-    epilogue(erow0, erows, ec0, slot);
+    epilogue(cur, slot);
+    tile += gridDim.x;
+    cur = next;
     if (!more) break;
   }
 }

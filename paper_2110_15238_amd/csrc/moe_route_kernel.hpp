@@ -31,6 +31,7 @@ struct RouteParams {
 };
 
 static constexpr int kRouteMaxExperts = 512, kRouteMaxTopK = 16, kRouteMaxGroups = 16;
+static constexpr int kRouteKeptIds = 4096;  // a single workgroup keeps its ids in LDS: 256 tokens of 16 slots
 static constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;  // of a workgroup that makes lists
 
 // exp(x) for x <= 0 (softmax) or of either sign (sigmoid) to about 2 units in the last place: the product with log2 e in two parts.
@@ -149,6 +150,7 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t token,
     route_wave_sync();
   }
   int id = 0;
+  float chosen = 0.f;  // lane j: the key of place j, which is the logit if there is no bias
   for (int j = 0; j < p.top_k; ++j) {
     float best = -INFINITY;
 #pragma unroll
@@ -161,10 +163,11 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t token,
 #pragma unroll
     for (int v = 0; v < V; ++v) key[v] = v * L + l == at ? -INFINITY : key[v];
     id = l == j ? at : id;
+    chosen = l == j ? best : chosen;
   }
   float w = 0.f;
   if (l < p.top_k) {
-    const float x = logit(id);
+    const float x = p.bias ? logit(id) : chosen;
     w = SIGMOID ? route_sigmoid(x) : route_exp(x - top);
   }
   if (p.renormalize) {
@@ -246,7 +249,8 @@ __global__ __launch_bounds__(NT) void moe_route_kernel(const RouteParams p) {
   extern __shared__ __attribute__((aligned(16))) int route_lds[];
   int* const n = route_lds;                        // [experts + 1]
   int* const wave_sums = n + kRouteMaxExperts + 1;  // [kRouteWaves]
-  int* const rest = wave_sums + kRouteWaves;
+  int* const kept = wave_sums + kRouteWaves;       // [kRouteKeptIds], ONE only
+  int* const rest = kept + (ONE ? kRouteKeptIds : 0);
   const int tid = threadIdx.x, l = tid % L, team = tid / L;
   constexpr int TEAMS = NT / L;
   float* const shared = (float*)rest + team * (kRouteMaxGroups + p.experts);
@@ -261,17 +265,17 @@ __global__ __launch_bounds__(NT) void moe_route_kernel(const RouteParams p) {
     if (l < p.top_k) {
       const bool on = !p.mask || p.mask[t];
       p.ids[t * p.top_k + l] = on ? id : -1;
+      if (ONE) kept[t * p.top_k + l] = on ? id : -1;
       p.weights[t * p.top_k + l] = on ? w : 0.f;
       if (on) atomicAdd(&n[id], 1);
     }
   }
   if constexpr (ONE) {
-    route_scan(n, wave_sums, p.experts, tid);  // (its first barrier: the ids of this workgroup are written)
+    route_scan(n, wave_sums, p.experts, tid);  // (its first barrier: the ids are kept)
     for (int e = tid; e <= p.experts; e += kRouteThreads) p.offsets[e] = n[e];
     const int slots = p.tokens * p.top_k;
     for (int s = n[p.experts] + tid; s < slots; s += kRouteThreads) p.order[s] = -1;
-    __threadfence_block();
-    route_place([&](int s) { return p.ids[s]; }, 0, slots, n, rest, p.experts, p.order, tid);
+    route_place([&](int s) { return kept[s]; }, 0, slots, n, rest, p.experts, p.order, tid);
   } else {
     __syncthreads();
     for (int e = tid; e < p.experts; e += NT) p.counts[(int64_t)blockIdx.x * p.experts + e] = n[e];
