@@ -6,8 +6,8 @@
 namespace bolt {
 template <int MODE, bool GATED>
 static hipError_t launch(const RowsParams& p, ManyTile tile, hipStream_t stream) {
-  if (tile == ManyTile::ROWS64) return launch_moe_tiles<64, 128, 2, 2, 2, MODE, GATED>(p, stream);
-  if (tile == ManyTile::ROWS128) return launch_moe_tiles<128, 128, 4, 2, 3, MODE, GATED>(p, stream);
+  if (tile == ManyTile::ROWS64) return launch_moe_tiles<64, 128, 2, 2, 3, MODE, GATED>(p, stream);
+  if (tile == ManyTile::ROWS128) return launch_moe_tiles<128, 128, 4, 2, 2, MODE, GATED>(p, stream);
   return launch_moe_pp<MODE, GATED>(p, stream);
 }
 hipError_t launch_many_rows_f16(const RowsParams& p, int mode, bool gated, ManyTile tile, hipStream_t stream) {

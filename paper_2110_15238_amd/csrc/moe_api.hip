@@ -291,15 +291,15 @@ Choice choose_w4(const Spread& s, int weight_rows) {
   else if (s.rows <= 256) t = SharedTile::ROWS64_COLS128;
   return {Family::SHARED, t, {}};
 }
-// FP16, us for the same experts, few rows / shared rows / 64 x 128 / 128 x 128 / 256 x 256: 32 tokens 82 / 90; 128 tokens 116 / 109 / 96 / 105 /
-// 115; 512 tokens 183 / 183 / 128 / 126 / 123; 2048 tokens - / - / 215 / 210 / 191; and 1000 wide, 2504 hidden, no gate, 8 experts, 2 per token:
-// 64 tokens 31 / 31 / 47 / 36 / 83, 1024 tokens - / - / 89 / 81 / 117, 4096 tokens - / - / 205 / 208 / 166.
+// FP16, us for the same experts, few rows / shared rows / 64 x 128 / 128 x 128 / 256 x 256: 32 tokens 82 / 90; 128 tokens 116 / 109 / 96 / 98 /
+// 109; 512 tokens 183 / 183 / 117 / 140 / 122; 1024 tokens - / - / 142 / 151 / 182; 2048 tokens - / - / 238 / 214 / 189; 4096 tokens - / - / 398 / 348 /
+// 285; and 1000 wide, 2504 hidden, no gate, 8 experts, 2 per token: 64 tokens 31 / 31 / 47, 256 tokens - / 51 / 51 / 70 / 100, 1024 tokens - / - /
+// 90 / 84 / 114, 4096 tokens - / - / 221 / 200 / 160.
 Choice choose_f16(const Spread& s, int weight_rows, bool offsets_fit) {
   if (s.rows <= 10 || !offsets_fit) return {Family::FEW, {}, {}};
   if (s.rows >= 192 && s.blocks(256) * blocks_of(weight_rows, 256) >= 144) return {Family::MANY, {}, ManyTile::ROWS256};
   if (s.rows <= 48 && s.blocks(32) * blocks_of(weight_rows, 64) <= 768) return {Family::SHARED, {}, {}};
-  if (s.rows >= 48 && s.blocks(128) * blocks_of(weight_rows, 128) <= 512) return {Family::MANY, {}, ManyTile::ROWS128};
-  return {Family::MANY, {}, ManyTile::ROWS64};
+  return {Family::MANY, {}, s.rows >= 224 ? ManyTile::ROWS128 : ManyTile::ROWS64};
 }
 
 struct MoeWorkspace {
