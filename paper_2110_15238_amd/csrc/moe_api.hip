@@ -174,20 +174,20 @@ bolt_status check_route(const bolt_moe_route_desc* d) {
 }
 
 // Workgroups of the routing kernel.  Up to 256 tokens one workgroup routes them, a wave for a token, and makes the lists in the same launch;
-// beyond, 16 lanes take a token, and each workgroup of the second launch adds up the counts of all.
+// beyond, 16 lanes take a token (more than 256 experts: 32 keys each, so 512 threads, or registers would run out), and each workgroup of the second launch adds up the counts of all.
 struct RoutePlan {
   int blocks, block_tokens, threads;
 };
 RoutePlan route_plan(const bolt_moe_route_desc& d) {
   if (d.tokens <= 256) return {1, d.tokens, kRouteThreads};
-  const int threads = d.tokens <= 8192 ? 512 : 1024, at_once = threads / 16;
+  const int threads = d.tokens <= 8192 || d.experts > 256 ? 512 : 1024, at_once = threads / 16;
   const int rounds = std::max(1, (d.tokens + at_once * 256 - 1) / (at_once * 256)), per = rounds * at_once;
   return {(d.tokens + per - 1) / per, per, threads};
 }
 
-template <typename T, bool SIGMOID, int L, int V, int NT, bool ONE>
+template <typename T, bool SIGMOID, bool PACKED, bool WIDE, int L, int V, int NT, bool ONE>
 hipError_t launch_route(const RouteParams& p, int blocks, hipStream_t stream) {
-  auto kern = moe_route_kernel<T, SIGMOID, L, V, NT, ONE>;
+  auto kern = moe_route_kernel<T, SIGMOID, PACKED, WIDE, L, V, NT, ONE>;
   static LdsOptIn opt_in;
   if (hipError_t e = opt_in.ensure((const void*)kern, 160 * 1024); e != hipSuccess) return e;
   const int groups = p.top_groups < p.groups ? NT / L * (kRouteMaxGroups + p.experts) : 0;
@@ -197,13 +197,20 @@ hipError_t launch_route(const RouteParams& p, int blocks, hipStream_t stream) {
   hipLaunchKernelGGL(moe_list_kernel, dim3(blocks), dim3(kRouteThreads), (head + lists) * 4, stream, p);
   return hipGetLastError();
 }
-template <typename T, bool SIGMOID>
+template <typename T, bool SIGMOID, bool PACKED>
 hipError_t launch_route_keys(const RouteParams& p, const RoutePlan& plan, hipStream_t stream) {
   auto keys = [&](auto v64) {
     constexpr int V = decltype(v64)::value;
-    if (plan.blocks == 1) return launch_route<T, SIGMOID, 64, V, 1024, true>(p, 1, stream);
-    if (plan.threads == 512) return launch_route<T, SIGMOID, 16, 4 * V, 512, false>(p, plan.blocks, stream);
-    return launch_route<T, SIGMOID, 16, 4 * V, 1024, false>(p, plan.blocks, stream);
+    if (plan.blocks == 1) return launch_route<T, SIGMOID, PACKED, false, 64, V, 1024, true>(p, 1, stream);
+    auto many = [&](auto wide) {
+      constexpr bool WIDE = decltype(wide)::value;
+      if constexpr (V <= 4)
+        if (plan.threads == 1024) return launch_route<T, SIGMOID, PACKED, WIDE, 16, 4 * V, 1024, false>(p, plan.blocks, stream);
+      return launch_route<T, SIGMOID, PACKED, WIDE, 16, 4 * V, 512, false>(p, plan.blocks, stream);
+    };
+    if constexpr (4 * V * sizeof(T) >= 16)
+      if (p.experts == 64 * V && p.ld * sizeof(T) % 16 == 0) return many(std::true_type{});  // (logits are 16-byte aligned)
+    return many(std::false_type{});
   };
   if (p.experts <= 64) return keys(std::integral_constant<int, 1>{});
   if (p.experts <= 128) return keys(std::integral_constant<int, 2>{});
@@ -407,9 +414,11 @@ bolt_status bolt_moe_route(const bolt_moe_route_desc* desc, const void* logits, 
   p.renormalize = desc->renormalize; p.scale = desc->scale; p.block_tokens = plan.block_tokens;
   const bool sigmoid = desc->score == BOLT_SCORE_SIGMOID;
   const hipStream_t st = (hipStream_t)stream;
-  if (desc->logits_type == BOLT_TYPE_F16)
-    return status_of(sigmoid ? launch_route_keys<half_t, true>(p, plan, st) : launch_route_keys<half_t, false>(p, plan, st));
-  return status_of(sigmoid ? launch_route_keys<float, true>(p, plan, st) : launch_route_keys<float, false>(p, plan, st));
+  if (desc->logits_type == BOLT_TYPE_F32)
+    return status_of(sigmoid ? launch_route_keys<float, true, false>(p, plan, st) : launch_route_keys<float, false, false>(p, plan, st));
+  if (bias)
+    return status_of(sigmoid ? launch_route_keys<half_t, true, false>(p, plan, st) : launch_route_keys<half_t, false, false>(p, plan, st));
+  return status_of(sigmoid ? launch_route_keys<half_t, true, true>(p, plan, st) : launch_route_keys<half_t, false, true>(p, plan, st));
 }
 
 size_t bolt_moe_workspace_bytes(const bolt_moe_desc* desc) {
