@@ -1,15 +1,17 @@
-// Products of a few rows with a large weight matrix [N][K]: the linear layers of a handful of tokens, with weights in 4 bits
+// Products of up to 16 rows with a large weight matrix [N][K]: the linear layers of a handful of tokens, with weights in 4 bits
 // or in FP16, for one matrix or for the experts that a router chose.
 //
-// With M rows every weight is used M times, so up to about 64 rows the product is bound by reading the weights once.  A
-// workgroup owns 16 R weight rows and up to 16 MB activation rows; its NW waves take the reduction in turns, step by step (a
-// wave's step is 128 columns of 4-bit weights or 64 of FP16 ones), so that the workgroup reads its weights as one stream.  Weights go
-// straight from memory to registers, NB steps ahead, in the operand order of v_mfma_f32_16x16x32_f16, whose 16 columns are the
+// Every weight is used for 16 rows at most, so the product is bound by reading the weights once, and small ones by the launch and one
+// round trip to memory.  A workgroup owns 16 R weight rows; its NW waves take the reduction in turns, step by step (a wave's step
+// is 128 columns of 4-bit weights or 64 of FP16 ones), so that the workgroup reads its weights as one stream.  Weights and activations go
+// straight from memory to registers, several steps ahead, in the operand order of v_mfma_f32_16x16x32_f16, whose 16 columns are the
 // activation rows; nothing passes through LDS but the waves' partial sums, which are added in a fixed order.
 //   4-bit weights: an operand is q - z, exact in a half; the sum over a group of columns comes out of the matrix core in FP32
 //   and is scaled there, so neither scale nor zero point costs accuracy.  (Nine vector instructions make eight operands.)
 //   Activation rows beyond the last repeat the last: their columns of the result are not stored.  Columns beyond K are zero on
 //   both sides.
+// Measured: 4096 x 4096 in 4 bits, one row, 4.2 us (8.7 MB); 6152 x 5000, 13 rows, 7.7 us (17 MB); one token's 8 experts in FP16, 2048 x 1024:
+// 16.8 us for 67 MB of gate and value rows (4.0 TB/s; a large copy moves 5.15), 8 us for 34 MB behind them.
 #pragma once
 #include "routed_rows.hpp"
 #include "w4_format.hpp"

@@ -446,6 +446,8 @@ bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const voi
   const int64_t most = (1ll << 31) - 1;
   const bool offsets_fit = (int64_t)desc->tokens * desc->ldx * 2 <= most && (int64_t)up_rows * desc->width * 2 <= most &&
                            (int64_t)desc->width * desc->hidden * 2 <= most && (int64_t)256 * desc->hidden * 2 <= most;
+  // (beyond them the kernel of few rows runs, whose launch has to stay below 2^32 threads)
+  if (!offsets_fit && (blocks_of(slots, 16) + E) * blocks_of(std::max(up_rows, desc->width), 16) * 512 > UINT32_MAX) return BOLT_ERR_UNSUPPORTED;
   const Spread spread(*desc);
   const hipStream_t st = (hipStream_t)stream;
 

@@ -121,6 +121,8 @@ def test_experts_refusals(bolt):
         assert _experts(bolt, bad) == ALIGNMENT
     for bad in (D(4, 513, 2, 64, 64), D(4, 64, 17, 64, 64), D(1 << 30, 8, 4, 64, 64), D(4, 8, 2, 64, (1 << 20) + 8)):
         assert _experts(bolt, bad) == UNSUPPORTED
+    # x past 2 GiB runs on the kernel of few rows, which has no grid for this many
+    assert _experts(bolt, D(300000, 8, 8, 4096, 4096)) == UNSUPPORTED
     good = D(4, 8, 2, 64, 64)
     for name in ("x", "w_up", "w_down", "ids", "weights", "offsets", "order", "y"):
         assert _experts(bolt, good, **{name: None}) == INVALID
