@@ -360,6 +360,7 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   if (need > 0 && (!workspace || workspace_bytes < need)) return BOLT_ERR_WORKSPACE;
   if (!aligned16(workspace)) return BOLT_ERR_ALIGNMENT;
   if (desc->M == 0) return BOLT_OK;
+  if (blocks_of(desc->M, 16) * blocks_of(desc->N, 16) > kMaxGrid) return BOLT_ERR_UNSUPPORTED;
   const W4Format f(desc->N, desc->K, desc->group);
   const hipStream_t st = (hipStream_t)stream;
   const half_t* none = no_bias();
@@ -376,7 +377,6 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   p.ldy = desc->ldd;
   p.M = desc->M; p.N = desc->N; p.K = desc->K; p.steps = f.steps;
   p.alpha = desc->alpha; p.beta = desc->beta; p.act = desc->act;
-  if (blocks_of(desc->M, 16) * blocks_of(desc->N, 16) > kMaxGrid) return BOLT_ERR_UNSUPPORTED;
   if (desc->M <= 16) return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, desc->group, st));
   // (alpha 0: the kernels of many rows start their sums at beta / alpha times the bias)
   if (need == 0 || desc->alpha == 0.f)
@@ -436,8 +436,6 @@ bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const voi
     if (!aligned16(q)) return BOLT_ERR_ALIGNMENT;
   const MoeWorkspace ws = moe_workspace(*desc);
   if (!workspace || workspace_bytes < (size_t)ws.bytes) return BOLT_ERR_WORKSPACE;
-  const half_t* none = no_bias();
-  if (!none) return BOLT_ERR_LAUNCH;
   const bool w4 = desc->weights == BOLT_WEIGHTS_W4, gated = desc->gated != 0;
   const int slots = desc->tokens * desc->top_k, E = desc->experts;
   const int up_rows = gated ? 2 * desc->hidden : desc->hidden;
@@ -448,6 +446,8 @@ bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const voi
                            (int64_t)desc->width * desc->hidden * 2 <= most && (int64_t)256 * desc->hidden * 2 <= most;
   // (beyond them the kernel of few rows runs, whose launch has to stay below 2^32 threads)
   if (!offsets_fit && (blocks_of(slots, 16) + E) * blocks_of(std::max(up_rows, desc->width), 16) * 512 > UINT32_MAX) return BOLT_ERR_UNSUPPORTED;
+  const half_t* none = no_bias();
+  if (!none) return BOLT_ERR_LAUNCH;
   const Spread spread(*desc);
   const hipStream_t st = (hipStream_t)stream;
 
