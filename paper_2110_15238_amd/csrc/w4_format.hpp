@@ -31,14 +31,21 @@ struct W4Format {
 };
 
 // Eight values q - z as halves, exact: 0x6400 | q is 1024 + q and 0x6400 | q << 4 is 1024 + 16 q as a half; minus1 holds two
-// halves -1024 - z, minus16 two halves -64 - z.
+// halves -1024 - z, minus16 two halves -64 - z.  The empty asm keeps the constants in registers: as literals they would make two
+// instructions of every (w & mask) | exponent.
 __device__ __forceinline__ half8 w4_values(unsigned w, half2v minus1, half2v minus16) {
   const half2v sixteenth = {(half_t)0.0625f, (half_t)0.0625f};
+  unsigned lo = 0x000f000fu, hi = 0x00f000f0u, exponent = 0x64006400u;
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm("" : "+s"(lo));
+  asm("" : "+s"(hi));
+  asm("" : "+v"(exponent));
+#endif
   const unsigned v = w >> 8;
-  const half2v a = __builtin_bit_cast(half2v, (w & 0x000f000fu) | 0x64006400u) + minus1;
-  const half2v b = __builtin_elementwise_fma(__builtin_bit_cast(half2v, (w & 0x00f000f0u) | 0x64006400u), sixteenth, minus16);
-  const half2v c = __builtin_bit_cast(half2v, (v & 0x000f000fu) | 0x64006400u) + minus1;
-  const half2v d = __builtin_elementwise_fma(__builtin_bit_cast(half2v, (v & 0x00f000f0u) | 0x64006400u), sixteenth, minus16);
+  const half2v a = __builtin_bit_cast(half2v, (w & lo) | exponent) + minus1;
+  const half2v b = __builtin_elementwise_fma(__builtin_bit_cast(half2v, (w & hi) | exponent), sixteenth, minus16);
+  const half2v c = __builtin_bit_cast(half2v, (v & lo) | exponent) + minus1;
+  const half2v d = __builtin_elementwise_fma(__builtin_bit_cast(half2v, (v & hi) | exponent), sixteenth, minus16);
   return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 // The two constants for a zero point: -1024 - z is 0xe400 + z as a half, -64 - z is 0xd400 + 16 z.
