@@ -173,16 +173,21 @@ bolt_status check_route(const bolt_moe_route_desc* d) {
   return BOLT_OK;
 }
 
-// Workgroups of the routing kernel.  Up to 256 tokens one workgroup routes them, a wave for a token, and makes the lists in the same launch;
-// beyond, 16 lanes take a token (more than 256 experts: 32 keys each, so 512 threads, or registers would run out), and each workgroup of the second launch adds up the counts of all.
+// Workgroups of the routing kernel.  Few tokens are one workgroup's, which makes the lists in the same launch; beyond, each workgroup of a second
+// launch adds up the counts of all.  One workgroup takes a wave for a token up to 16 tokens and 16 lanes from there, 64 tokens at once.  us, a wave
+// each / 16 lanes, FP16 softmax, 28, 128 and 196 (4 groups) experts: 17 tokens 5.6 / 5.1, 6.0 / 5.9 and 8.1 / 9.2, 32 tokens 6.9 / 5.1, 7.5 / 5.9
+// and 10.1 / 9.0, 64 tokens 9.7 / 6.0, 10.7 / 7.2 and 15.7 / 11.3.  By 16 lanes 96 tokens take 6.5, 8.0 and 12.7, 256 tokens 10.9, 13.9 and 25.9; two
+// launches take 7.9, 8.3 and 12.6 for 257 tokens.  More than 256 experts (32 keys for 16 lanes) keep to waves: 352 and 512 experts in 8 groups, 48 tokens
+// 12.5 and 21.3, two launches 13.7 and 20.1 for 49.
 struct RoutePlan {
-  int blocks, block_tokens, threads;
+  int blocks, block_tokens, threads, lanes;
 };
 RoutePlan route_plan(const bolt_moe_route_desc& d) {
-  if (d.tokens <= 256) return {1, d.tokens, kRouteThreads};
-  const int threads = d.tokens <= 8192 || d.experts > 256 ? 512 : 1024, at_once = threads / 16;
+  const bool wide = d.experts > 256;
+  if (d.tokens <= (wide ? 48 : 64)) return {1, d.tokens, kRouteThreads, wide || d.tokens <= 16 ? 64 : 16};
+  const int threads = d.tokens <= 8192 || wide ? 512 : 1024, at_once = threads / 16;
   const int rounds = std::max(1, (d.tokens + at_once * 256 - 1) / (at_once * 256)), per = rounds * at_once;
-  return {(d.tokens + per - 1) / per, per, threads};
+  return {(d.tokens + per - 1) / per, per, threads, 16};
 }
 
 template <typename T, bool SIGMOID, bool PACKED, bool WIDE, int L, int V, int NT, bool ONE>
@@ -201,7 +206,9 @@ template <typename T, bool SIGMOID, bool PACKED>
 hipError_t launch_route_keys(const RouteParams& p, const RoutePlan& plan, hipStream_t stream) {
   auto keys = [&](auto v64) {
     constexpr int V = decltype(v64)::value;
-    if (plan.blocks == 1) return launch_route<T, SIGMOID, PACKED, false, 64, V, 1024, true>(p, 1, stream);
+    if (plan.lanes == 64) return launch_route<T, SIGMOID, PACKED, false, 64, V, 1024, true>(p, 1, stream);
+    if constexpr (V <= 4)
+      if (plan.blocks == 1) return launch_route<T, SIGMOID, PACKED, false, 16, 4 * V, 1024, true>(p, 1, stream);
     auto many = [&](auto wide) {
       constexpr bool WIDE = decltype(wide)::value;
       if constexpr (V <= 4)

@@ -34,7 +34,7 @@ struct RouteParams {
 };
 
 static constexpr int kRouteMaxExperts = 512, kRouteMaxTopK = 16, kRouteMaxGroups = 16;
-static constexpr int kRouteKeptIds = 4096;  // a single workgroup keeps its ids in LDS: 256 tokens of 16 slots
+static constexpr int kRouteKeptIds = 1024;  // a single workgroup keeps its ids in LDS: 64 tokens of 16 slots
 static constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;  // of a workgroup that makes lists
 
 // exp(x) for x <= 0 (softmax) or of either sign (sigmoid) to about 2 units in the last place: the product with log2 e in two parts.

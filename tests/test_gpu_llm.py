@@ -209,6 +209,20 @@ def test_route_sigmoid(bolt, T, E, k, groups, top_groups, biased):
     _check_route(got, E, False)
 
 
+@pytest.mark.parametrize("T", [16, 17, 48, 49, 64, 65])
+@pytest.mark.parametrize("E,k,groups,top_groups", [(28, 4, 1, 1), (256, 16, 16, 9), (256, 16, 1, 1), (352, 5, 1, 1), (512, 10, 8, 4)])
+@pytest.mark.parametrize("half", [True, False])
+def test_route_around_the_kernels_limits(bolt, T, E, k, groups, top_groups, half):
+    """The numbers of tokens at which lanes per token and launches change; 64 tokens of 16 slots fill what a workgroup keeps."""
+    g = torch.Generator().manual_seed(T * E + groups)
+    logits = torch.randn(T, E, generator=g) * 1.5
+    mask = (torch.rand(T, generator=g) > 0.2).to(torch.uint8) if T % 2 else None
+    if half:
+        return _check_route(_route(bolt, logits.half(), k, mask=mask, groups=groups, top_groups=top_groups), E, True)
+    bias = torch.randn(E, generator=g) * 0.1
+    _check_route(_route(bolt, logits, k, bias=bias, mask=mask, score="sigmoid", groups=groups, top_groups=top_groups), E, False)
+
+
 @pytest.mark.parametrize("T", [5, 700])
 @pytest.mark.parametrize("biased", [True, False])
 def test_route_softmax_groups(bolt, T, biased):
