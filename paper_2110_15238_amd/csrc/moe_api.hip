@@ -295,17 +295,21 @@ struct Choice {
 };
 // 4 bits, us for 2048 wide, 1024 hidden, 32 experts, 4 per token, few rows / 16 x 64 / 16 x 128 / 32 x 128 / 64 x 128 / 128 x 256:
 // 1 token 15 / 19 / 26; 4 tokens 27 / 23 / 26; 32 tokens 42 / 38 / 34 / 37; 128 tokens 67 / 53 / 45 / 49 / 53 / 68; 512 tokens 157 / 120 / 93 /
-// 77 / 90 / 131; 1024 tokens - / - / 162 / 127 / 127 / 143; 2048 tokens - / - / - / - / 246 / 225.
+// 77 / 90 / 131; 1024 tokens - / - / 162 / 127 / 127 / 143; 2048 tokens - / - / - / - / 246 / 225.  A tile that leaves compute units without a
+// workgroup gives way to the next smaller one: groups of 32, no gate, 968 wide, 3592 hidden, 350 tokens, 6 of 6 experts 144 by the rows alone, 114 so;
+// groups of 128, gated, 1264 wide, 4072 hidden, 1104 tokens, 3 of 4 experts 186 and 167.
 Choice choose_w4(const Spread& s, int weight_rows) {
   if (s.experts * blocks_of(weight_rows, 32) <= 512 && s.rows <= 16) return {Family::FEW, {}, {}};
-  SharedTile t = SharedTile::ROWS128_COLS256;
+  const auto fills = [&](int rows, int cols) { return s.blocks(rows) * blocks_of(weight_rows, cols) >= 256; };
+  SharedTile t = SharedTile::ROWS16_COLS64;
   if (s.blocks(16) * blocks_of(weight_rows, 64) <= 768) t = SharedTile::ROWS16_COLS64;
-  else if (s.rows <= 16) t = SharedTile::ROWS16_COLS128;
-  else if (s.rows <= 128) t = SharedTile::ROWS32_COLS128;
-  else if (s.rows <= 256) t = SharedTile::ROWS64_COLS128;
+  else if (s.rows > 256 && fills(128, 256)) t = SharedTile::ROWS128_COLS256;
+  else if (s.rows > 128 && fills(64, 128)) t = SharedTile::ROWS64_COLS128;
+  else if (s.rows > 16 && fills(32, 128)) t = SharedTile::ROWS32_COLS128;
+  else if (fills(16, 128)) t = SharedTile::ROWS16_COLS128;
   return {Family::SHARED, t, {}};
 }
-// FP16, us for the same experts, few rows / shared rows / 64 x 128 / 128 x 128 / 256 x 256: 32 tokens 82 / 90; 128 tokens 116 / 109 / 96 / 98 /
+// FP16, us for the first experts above, few rows / shared rows / 64 x 128 / 128 x 128 / 256 x 256: 32 tokens 82 / 90; 128 tokens 116 / 109 / 96 / 98 /
 // 109; 512 tokens 183 / 183 / 117 / 140 / 122; 1024 tokens - / - / 142 / 151 / 182; 2048 tokens - / - / 238 / 214 / 189; 4096 tokens - / - / 398 / 348 /
 // 285; and 1000 wide, 2504 hidden, no gate, 8 experts, 2 per token: 64 tokens 31 / 31 / 47, 256 tokens - / 51 / 51 / 70 / 100, 1024 tokens - / - /
 // 90 / 84 / 114, 4096 tokens - / - / 221 / 200 / 160.
