@@ -139,10 +139,13 @@ const half_t* no_bias() {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+int64_t blocks_of(int64_t v, int64_t by) { return (v + by - 1) / by; }
 bool known_act(int a) { return a >= BOLT_ACT_NONE && a <= BOLT_ACT_SILU; }
 bolt_status status_of(hipError_t e) { return e == hipSuccess ? BOLT_OK : BOLT_ERR_LAUNCH; }
 constexpr int kMaxLength = 1 << 21;  // of a row, as in the other operators
 constexpr int64_t kMaxGrid = (1ll << 31) - 1;
+// Rows and slots: the kernels count them in 32 bits, as far as the end of the last workgroup's share and one stride past it.
+constexpr int64_t kMaxRows = (1ll << 31) - (1 << 16);
 
 bolt_status check_w4_shape(int32_t N, int32_t K, int32_t group) {
   if (N <= 0 || K <= 0 || (group != 32 && group != 64 && group != 128)) return BOLT_ERR_INVALID_ARG;
@@ -156,7 +159,7 @@ bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d) {
   if (bolt_status s = check_w4_shape(d->N, d->K, d->group); s == BOLT_ERR_INVALID_ARG) return s;
   if (d->M < 0 || !known_act(d->act) || d->lda < d->K || d->ldd < d->N) return BOLT_ERR_INVALID_ARG;
   if ((d->N | d->K | d->lda | d->ldd) & 7) return BOLT_ERR_ALIGNMENT;
-  if (d->lda > kMaxLength || d->ldd > kMaxLength || d->N > kMaxLength) return BOLT_ERR_UNSUPPORTED;
+  if (d->lda > kMaxLength || d->ldd > kMaxLength || d->N > kMaxLength || d->M > kMaxRows) return BOLT_ERR_UNSUPPORTED;
   return BOLT_OK;
 }
 
@@ -169,7 +172,7 @@ bolt_status check_route(const bolt_moe_route_desc* d) {
   if (d->logits_type != BOLT_TYPE_F16 && d->logits_type != BOLT_TYPE_F32) return BOLT_ERR_INVALID_ARG;
   if ((int64_t)d->top_k > (int64_t)(d->experts / d->groups) * d->top_groups) return BOLT_ERR_INVALID_ARG;
   if (d->experts > kRouteMaxExperts || d->top_k > kRouteMaxTopK || d->groups > kRouteMaxGroups) return BOLT_ERR_UNSUPPORTED;
-  if ((int64_t)d->tokens * d->top_k > INT32_MAX) return BOLT_ERR_UNSUPPORTED;
+  if ((int64_t)d->tokens * d->top_k > kMaxRows) return BOLT_ERR_UNSUPPORTED;
   return BOLT_OK;
 }
 
@@ -186,8 +189,8 @@ RoutePlan route_plan(const bolt_moe_route_desc& d) {
   const bool wide = d.experts > 256;
   if (d.tokens <= (wide ? 48 : 64)) return {1, d.tokens, kRouteThreads, wide || d.tokens <= 16 ? 64 : 16};
   const int threads = d.tokens <= 8192 || wide ? 512 : 1024, at_once = threads / 16;
-  const int rounds = std::max(1, (d.tokens + at_once * 256 - 1) / (at_once * 256)), per = rounds * at_once;
-  return {(d.tokens + per - 1) / per, per, threads, 16};
+  const int per = (int)blocks_of(d.tokens, at_once * 256) * at_once;
+  return {(int)blocks_of(d.tokens, per), per, threads, 16};
 }
 
 template <typename T, bool SIGMOID, bool PACKED, bool WIDE, int L, int V, int NT, bool ONE>
@@ -234,11 +237,9 @@ bolt_status check_moe(const bolt_moe_desc* d) {
   if ((d->width | d->hidden | d->ldx | d->ldy) & 7) return BOLT_ERR_ALIGNMENT;
   if (d->experts > kRouteMaxExperts || d->top_k > kRouteMaxTopK) return BOLT_ERR_UNSUPPORTED;
   if (d->ldx > kMaxLength || d->ldy > kMaxLength || d->width > kMaxLength || d->hidden > kMaxLength / 2) return BOLT_ERR_UNSUPPORTED;
-  if ((int64_t)d->tokens * d->top_k > INT32_MAX) return BOLT_ERR_UNSUPPORTED;
+  if ((int64_t)d->tokens * d->top_k > kMaxRows) return BOLT_ERR_UNSUPPORTED;
   return BOLT_OK;
 }
-
-int64_t blocks_of(int64_t v, int64_t by) { return (v + by - 1) / by; }
 
 // ---- which kernel runs a linear layer with 4-bit weights --------------------------------------------------------------------
 // Estimated time in us: a fit to 6 shapes x 13 row counts, one workgroup's step in us times its steps and its rounds of 256 workgroups.  Two

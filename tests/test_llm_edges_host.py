@@ -1,0 +1,49 @@
+"""CPU-only: sizes at the edge of what the operators of language models accept.  Every call is one that is refused or has nothing to do, so
+no address is read."""
+import ctypes as C
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2110_15238_amd", "libbolt.so")
+pytestmark = pytest.mark.skipif(not os.path.exists(LIB), reason="libbolt.so not built (run __graft_entry__.build())")
+
+OK, INVALID, UNSUPPORTED, ALIGNMENT, WORKSPACE, LAUNCH, ILLEGAL = range(7)
+A16, MUCH = 0x1000, 1 << 50
+MOST = (1 << 31) - (1 << 16)  # rows, or slots
+
+
+@pytest.fixture(scope="module")
+def bolt():
+    import paper_2110_15238_amd as b
+    return b
+
+
+def _route(bolt, d):
+    return bolt.binding.raw().bolt_moe_route(C.byref(d), A16, None, None, A16, A16, A16, A16, A16, MUCH, None)
+
+
+def _experts(bolt, d):
+    return bolt.binding.raw().bolt_moe_experts(C.byref(d), A16, A16, None, A16, None, A16, A16, A16, A16, A16, A16, MUCH, None)
+
+
+def _gemm(bolt, d):
+    return bolt.binding.raw().bolt_gemm_w4(C.byref(d), A16, A16, None, A16, A16, MUCH, None)
+
+
+def test_slots_that_32_bits_cannot_count_past_are_refused(bolt):
+    """2^31 - 16 slots: the last wave's share of the lists would end at 2^31.  The most that is accepted leaves room for it."""
+    for tokens, k in ((134217727, 16), ((1 << 31) - 1, 1), (MOST + 1, 1)):
+        assert _route(bolt, bolt.moe_route_desc(tokens, 16, k)) == UNSUPPORTED
+        assert bolt.bolt_moe_route_workspace_bytes(bolt.moe_route_desc(tokens, 16, k)) == 0
+        assert _experts(bolt, bolt.moe_desc(tokens, 16, k, 8, 8)) == UNSUPPORTED
+        assert bolt.bolt_moe_workspace_bytes(bolt.moe_desc(tokens, 16, k, 8, 8)) == 0
+    for tokens, k in ((MOST // 16, 16), (MOST, 1)):
+        assert 256 * 16 * 4 >= bolt.bolt_moe_route_workspace_bytes(bolt.moe_route_desc(tokens, 16, k)) > 0
+        assert bolt.bolt_moe_workspace_bytes(bolt.moe_desc(tokens, 16, k, 8, 8)) >= tokens * k * (8 * 2 + 8 * 4)
+
+
+def test_rows_that_32_bits_cannot_count_past_are_refused(bolt):
+    for rows in ((1 << 31) - 1, MOST + 1):
+        assert _gemm(bolt, bolt.gemm_w4_desc(rows, 8, 8, 32)) == UNSUPPORTED
