@@ -6,6 +6,20 @@
 namespace bolt {
 // Activation rows x weight rows of a workgroup's tile (a gated product has half as many output columns).
 enum class SharedTile { ROWS16_COLS64, ROWS16_COLS128, ROWS32_COLS32, ROWS32_COLS64, ROWS32_COLS128, ROWS64_COLS128, ROWS128_COLS256 };
+struct TileSize {
+  int rows, cols;
+};
+inline TileSize tile_size(SharedTile t) {
+  switch (t) {
+    case SharedTile::ROWS16_COLS64: return {16, 64};
+    case SharedTile::ROWS16_COLS128: return {16, 128};
+    case SharedTile::ROWS32_COLS32: return {32, 32};
+    case SharedTile::ROWS32_COLS64: return {32, 64};
+    case SharedTile::ROWS32_COLS128: return {32, 128};
+    case SharedTile::ROWS64_COLS128: return {64, 128};
+    default: return {128, 256};
+  }
+}
 enum class ManyTile { ROWS64, ROWS128, ROWS256 };
 
 hipError_t launch_few_rows_f16(const RowsParams& p, int mode, bool gated, hipStream_t stream);

@@ -143,9 +143,10 @@ int64_t blocks_of(int64_t v, int64_t by) { return (v + by - 1) / by; }
 bool known_act(int a) { return a >= BOLT_ACT_NONE && a <= BOLT_ACT_SILU; }
 bolt_status status_of(hipError_t e) { return e == hipSuccess ? BOLT_OK : BOLT_ERR_LAUNCH; }
 constexpr int kMaxLength = 1 << 21;  // of a row, as in the other operators
-constexpr int64_t kMaxGrid = (1ll << 31) - 1;
 // Rows and slots: the kernels count them in 32 bits, as far as the end of the last workgroup's share and one stride past it.
 constexpr int64_t kMaxRows = (1ll << 31) - (1 << 16);
+// Threads of a launch: the runtime counts them in 32 bits, and no workgroup here has more than 512.
+bool launches(int64_t blocks) { return blocks <= UINT32_MAX / 512; }
 
 bolt_status check_w4_shape(int32_t N, int32_t K, int32_t group) {
   if (N <= 0 || K <= 0 || (group != 32 && group != 64 && group != 128)) return BOLT_ERR_INVALID_ARG;
@@ -321,6 +322,23 @@ Choice choose_f16(const Spread& s, int weight_rows, bool offsets_fit) {
   return {Family::MANY, {}, s.rows >= 224 ? ManyTile::ROWS128 : ManyTile::ROWS64};
 }
 
+// Whether the launch of a product with N weight rows of K columns can be made; the number of row blocks is the host's bound of it.
+bool product_launches(const bolt_moe_desc& d, const Spread& s, int N, int K, bool offsets_fit) {
+  const bool w4 = d.weights == BOLT_WEIGHTS_W4;
+  const Choice c = w4 ? choose_w4(s, N) : choose_f16(s, N, offsets_fit);
+  const int64_t slots = (int64_t)d.tokens * d.top_k, short_blocks = std::min<int64_t>(slots, d.experts);
+  if (c.family == Family::FEW || !offsets_fit) {
+    const int64_t blocks = slots / 16 + short_blocks;
+    const bool walks = blocks_of(K, w4 ? W4Format::STEP : 64) <= 32;  // (each row block once at least, some thousand workgroups otherwise)
+    return launches(walks ? 2 * blocks + 2048 : blocks * blocks_of(N, 32));
+  }
+  if (c.family == Family::MANY && c.many == ManyTile::ROWS256) return true;  // (one workgroup per compute unit)
+  TileSize t = {32, 64};
+  if (w4) t = tile_size(c.shared);
+  else if (c.family == Family::MANY) t = c.many == ManyTile::ROWS64 ? TileSize{64, 128} : TileSize{128, 128};
+  return launches((slots / t.rows + short_blocks) * blocks_of(N, t.cols));
+}
+
 struct MoeWorkspace {
   int64_t hidden_at, rows_at, bytes;  // [slots][hidden] halves in the lists' order, [slots][width] floats by slot
 };
@@ -372,8 +390,11 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   if (need > 0 && (!workspace || workspace_bytes < need)) return BOLT_ERR_WORKSPACE;
   if (!aligned16(workspace)) return BOLT_ERR_ALIGNMENT;
   if (desc->M == 0) return BOLT_OK;
-  if (blocks_of(desc->M, 16) * blocks_of(desc->N, 16) > kMaxGrid) return BOLT_ERR_UNSUPPORTED;
   const W4Format f(desc->N, desc->K, desc->group);
+  const DenseTile& tile = dense_tile(desc->M, desc->N, f.steps, desc->group);
+  // (alpha 0: the kernels of many rows start their sums at beta / alpha times the bias)
+  const bool packed_tiles = desc->M > 16 && (need == 0 || desc->alpha == 0.f);
+  if (packed_tiles && !launches(blocks_of(desc->M, tile.rows) * blocks_of(desc->N, tile.cols))) return BOLT_ERR_UNSUPPORTED;
   const hipStream_t st = (hipStream_t)stream;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
@@ -390,9 +411,7 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   p.M = desc->M; p.N = desc->N; p.K = desc->K; p.steps = f.steps;
   p.alpha = desc->alpha; p.beta = desc->beta; p.act = desc->act;
   if (desc->M <= 16) return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, desc->group, st));
-  // (alpha 0: the kernels of many rows start their sums at beta / alpha times the bias)
-  if (need == 0 || desc->alpha == 0.f)
-    return status_of(launch_shared_rows_w4(p, ROWS_DENSE, false, desc->group, dense_tile(desc->M, desc->N, f.steps, desc->group).tile, st));
+  if (packed_tiles) return status_of(launch_shared_rows_w4(p, ROWS_DENSE, false, desc->group, tile.tile, st));
   if (launch_w4_unpack(packed, (half_t*)workspace, f, st) != hipSuccess) return BOLT_ERR_LAUNCH;
   if (desc->act != BOLT_ACT_SILU) {
     const bolt_gemm_desc g = {desc->M, desc->N, desc->K, desc->lda, desc->K, desc->ldd, desc->alpha, desc->beta, desc->act, BOLT_LAYOUT_NK};
@@ -451,16 +470,16 @@ bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const voi
   const bool w4 = desc->weights == BOLT_WEIGHTS_W4, gated = desc->gated != 0;
   const int slots = desc->tokens * desc->top_k, E = desc->experts;
   const int up_rows = gated ? 2 * desc->hidden : desc->hidden;
-  if ((blocks_of(slots, 16) + E) * blocks_of(std::max(up_rows, desc->width), 16) > kMaxGrid) return BOLT_ERR_UNSUPPORTED;
   // the kernels that stage rows address x, an expert's weights and a tile's rows with 31-bit byte offsets
   const int64_t most = (1ll << 31) - 1;
   const bool offsets_fit = (int64_t)desc->tokens * desc->ldx * 2 <= most && (int64_t)up_rows * desc->width * 2 <= most &&
                            (int64_t)desc->width * desc->hidden * 2 <= most && (int64_t)256 * desc->hidden * 2 <= most;
-  // (beyond them the kernel of few rows runs, whose launch has to stay below 2^32 threads)
-  if (!offsets_fit && (blocks_of(slots, 16) + E) * blocks_of(std::max(up_rows, desc->width), 16) * 512 > UINT32_MAX) return BOLT_ERR_UNSUPPORTED;
+  // (beyond them the kernel of few rows runs)
+  const Spread spread(*desc);
+  if (!product_launches(*desc, spread, up_rows, desc->width, offsets_fit) || !product_launches(*desc, spread, desc->width, desc->hidden, offsets_fit))
+    return BOLT_ERR_UNSUPPORTED;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
-  const Spread spread(*desc);
   const hipStream_t st = (hipStream_t)stream;
 
   RowsParams p{};
