@@ -206,30 +206,17 @@ __global__ __launch_bounds__(256) void copy_kernel(const floatx4* src, floatx4* 
 __device__ __attribute__((aligned(16))) half_t g_zero_bias[8];
 
 static const half_t* zero_bias() {
-  static const half_t* ptr = [] {
-    void* q = nullptr;
-    return hipGetSymbolAddress(&q, HIP_SYMBOL(g_zero_bias)) == hipSuccess ? (const half_t*)q : nullptr;
-  }();
-  return ptr;
+  static PerDevice known;
+  return (const half_t*)address_on_device(known, g_zero_bias);
 }
 
 // Split-K partial sums of bolt_gemm_epilogue_noalloc: a file-scope device array, so that entry point never
 // allocates.  Every GPU the library runs on holds its own copy (at its own address) until the process ends.
 static __device__ __align__(256) unsigned char scratch[BOLT_NOALLOC_SCRATCH_BYTES];
 
-// The array's name is a host-side stand-in, not a device address: host code only ever uses the pointer that
-// hipGetSymbolAddress returns for the current device, looked up once per device.
-static constexpr int kMaxDevices = 64;
 static void* scratch_of_current_device() {
-  static std::once_flag once[kMaxDevices];
-  static void* ptr[kMaxDevices] = {};
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;
-  std::call_once(once[dev], [dev] {
-    void* q = nullptr;
-    if (hipGetSymbolAddress(&q, HIP_SYMBOL(scratch)) == hipSuccess) ptr[dev] = q;
-  });
-  return ptr[dev];
+  static PerDevice known;
+  return address_on_device(known, scratch);
 }
 
 // ------------------------------------------------------------------------------------------

@@ -10,6 +10,8 @@
 #include <mutex>
 #include <utility>
 
+#include "per_device.hpp"
+
 namespace bolt {
 
 typedef _Float16 half_t;
@@ -238,6 +240,17 @@ template <int CPR>
 __device__ __forceinline__ int ctile_swizzle(int row) {
   static_assert(CPR == 4 || CPR == 8 || CPR == 16 || CPR == 32, "chunks per C-tile row");
   return CPR >= 16 ? (row & 15) : CPR == 8 ? ((row >> 1) & 7) : ((row >> 2) & 3);
+}
+
+// Address of a device variable on the current device; a variable's name is only a host-side stand-in.
+template <typename T>
+inline void* address_on_device(PerDevice& known, const T& variable) {
+  int device = -1;
+  if (hipGetDevice(&device) != hipSuccess) return nullptr;
+  return known.get(device, [&]() -> void* {
+    void* q = nullptr;
+    return hipGetSymbolAddress(&q, HIP_SYMBOL(variable)) == hipSuccess ? q : nullptr;
+  });
 }
 
 // Host side: a kernel that wants more than 64 KiB of dynamic LDS has to opt in once per process.  Every launcher

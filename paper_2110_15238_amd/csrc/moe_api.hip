@@ -130,11 +130,8 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const float* rows, con
 
 __device__ __attribute__((aligned(16))) half_t g_no_bias[8];
 const half_t* no_bias() {
-  static const half_t* ptr = [] {
-    void* q = nullptr;
-    return hipGetSymbolAddress(&q, HIP_SYMBOL(g_no_bias)) == hipSuccess ? (const half_t*)q : nullptr;
-  }();
-  return ptr;
+  static PerDevice known;
+  return (const half_t*)address_on_device(known, g_no_bias);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

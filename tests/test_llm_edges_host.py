@@ -2,6 +2,8 @@
 no address is read."""
 import ctypes as C
 import os
+import re
+import subprocess
 
 import pytest
 
@@ -54,3 +56,24 @@ def test_launches_of_two_to_the_32_threads_are_refused(bolt):
     2^23 of 128 x 256."""
     assert _gemm(bolt, bolt.gemm_w4_desc(1 << 30, 8, 8, 32, alpha=0.0)) == UNSUPPORTED  # (alpha 0: weights as they are packed)
     assert _experts(bolt, bolt.moe_desc(1 << 26, 16, 16, 8, 8, weights="w4", group=32)) == UNSUPPORTED
+
+
+def test_addresses_of_device_variables_are_looked_up_for_each_device(tmp_path):
+    """The zeros that stand for a missing bias lie elsewhere on every GPU of a process.  The lookup on the host alone, with made-up devices; and
+    nothing in the library asks for such an address but through it."""
+    csrc = os.path.join(ROOT, "paper_2110_15238_amd", "csrc")
+    (tmp_path / "t.cpp").write_text("""
+#include "per_device.hpp"
+int main() {
+  static bolt::PerDevice known;
+  int asked = 0, zeros[3];
+  auto get = [&](int device) { return known.get(device, [&]() -> void* { ++asked; return device == 2 ? nullptr : &zeros[device]; }); };
+  for (int i = 0; i < 3; ++i)
+    if (get(0) != &zeros[0] || get(1) != &zeros[1] || get(2)) return 1;
+  return asked != 3 || get(-1) || get(bolt::PerDevice::kMaxDevices);
+}
+""")
+    subprocess.run(["g++", "-std=c++17", "-I" + csrc, "-o", str(tmp_path / "t"), str(tmp_path / "t.cpp"), "-pthread"], check=True)
+    subprocess.run([str(tmp_path / "t")], check=True)
+    calls = [f for f in sorted(os.listdir(csrc)) if f.endswith((".hip", ".hpp")) for _ in re.findall("hipGetSymbolAddress[(]", open(os.path.join(csrc, f)).read())]
+    assert calls == ["bolt_device.hpp"]
