@@ -381,12 +381,12 @@ size_t bolt_gemm_w4_workspace_bytes(const bolt_gemm_w4_desc* desc) {
 bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const void* packed, const void* bias, void* D, void* workspace,
                          size_t workspace_bytes, void* stream) {
   if (bolt_status s = check_gemm_w4(desc); s != BOLT_OK) return s;
+  if (desc->M == 0) return BOLT_OK;
   if (!A || !packed || !D) return BOLT_ERR_INVALID_ARG;
   if (!aligned16(A) || !aligned16(packed) || !aligned16(D) || (bias && !aligned16(bias))) return BOLT_ERR_ALIGNMENT;
   const size_t need = bolt_gemm_w4_workspace_bytes(desc);
   if (need > 0 && (!workspace || workspace_bytes < need)) return BOLT_ERR_WORKSPACE;
   if (!aligned16(workspace)) return BOLT_ERR_ALIGNMENT;
-  if (desc->M == 0) return BOLT_OK;
   const W4Format f(desc->N, desc->K, desc->group);
   const DenseTile& tile = dense_tile(desc->M, desc->N, f.steps, desc->group);
   // (alpha 0: the kernels of many rows start their sums at beta / alpha times the bias)

@@ -77,3 +77,10 @@ int main() {
     subprocess.run([str(tmp_path / "t")], check=True)
     calls = [f for f in sorted(os.listdir(csrc)) if f.endswith((".hip", ".hpp")) for _ in re.findall("hipGetSymbolAddress[(]", open(os.path.join(csrc, f)).read())]
     assert calls == ["bolt_device.hpp"]
+
+
+def test_without_rows_no_address_is_asked_for(bolt):
+    """A tensor without elements has a null address."""
+    raw = bolt.binding.raw()
+    assert raw.bolt_gemm_w4(C.byref(bolt.gemm_w4_desc(0, 64, 128, 64)), None, None, None, None, None, 0, None) == OK
+    assert raw.bolt_moe_experts(C.byref(bolt.moe_desc(0, 8, 2, 64, 64)), *[None] * 11, 0, None) == OK
