@@ -318,7 +318,8 @@ int32_t bolt_instance_supports(bolt_op op, int32_t kernel_id, const void* desc0,
 /* ---- Operators of language models: 4-bit weights, routing to experts, the experts' products ------------------
  * They follow the conventions above (borrowed device pointers, FP16 activations, FP32 accumulation, validation before any
  * launch, nothing allocated); they take any size, so M and tokens may be 0 (BOLT_OK, and only `offsets` is written), up to
- * 2^31 - 65536 rows, or slots (tokens * top_k).  They have no instance tables: the kernel is chosen by a rule on the sizes. */
+ * 2^31 - 65536 rows, or slots (tokens * top_k).  The bytes of workspace do not fall as M or tokens grow, everything else the
+ * same, so a buffer for the largest batch serves all.  They have no instance tables: the kernel is chosen by a rule on the sizes. */
 
 /* Weights held in 4 bits: W[n][k] = scales[n][k / group] * (q[n][k] - zeros[n][k / group]), q and zeros in 0 .. 15; group 32, 64
  * or 128; the last group of a row may be short.  N and K multiples of 8.

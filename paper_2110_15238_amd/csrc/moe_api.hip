@@ -421,8 +421,9 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
 
 size_t bolt_moe_route_workspace_bytes(const bolt_moe_route_desc* desc) {
   if (check_route(desc) != BOLT_OK) return 0;
-  const RoutePlan plan = route_plan(*desc);
-  return plan.blocks == 1 ? 0 : (size_t)plan.blocks * desc->experts * sizeof(int);
+  if (route_plan(*desc).blocks == 1) return 0;
+  // a bound of the plan's workgroups that does not fall as tokens grow: a buffer for the largest batch is enough for all
+  return (size_t)std::min<int64_t>(256, blocks_of(desc->tokens, 32)) * desc->experts * sizeof(int);
 }
 
 bolt_status bolt_moe_route(const bolt_moe_route_desc* desc, const void* logits, const void* bias, const void* mask, void* ids, void* weights,

@@ -84,3 +84,16 @@ def test_without_rows_no_address_is_asked_for(bolt):
     raw = bolt.binding.raw()
     assert raw.bolt_gemm_w4(C.byref(bolt.gemm_w4_desc(0, 64, 128, 64)), None, None, None, None, None, 0, None) == OK
     assert raw.bolt_moe_experts(C.byref(bolt.moe_desc(0, 8, 2, 64, 64)), *[None] * 11, 0, None) == OK
+
+
+@pytest.mark.parametrize("experts", [8, 128, 256, 257, 512])
+def test_workspace_of_the_routing_does_not_fall_as_tokens_grow(bolt, experts):
+    near = {n + d for n in (16, 48, 64, 512, 8192, 16384, 24576, 65536, 1 << 20, 1 << 26) for d in range(-65, 66, 13)} | {1, 48, 49, 64, 65, 8192, 8193, 16384, 16385}
+    tokens = sorted(n for n in near if n > 0)
+    held = [bolt.bolt_moe_route_workspace_bytes(bolt.moe_route_desc(n, experts, 4)) for n in tokens]
+    assert held == sorted(held) and held[0] == 0 and held[-1] == 256 * experts * 4
+
+
+def test_workspace_of_the_experts_does_not_fall_as_tokens_grow(bolt):
+    held = [bolt.bolt_moe_workspace_bytes(bolt.moe_desc(n, 16, 4, 264, 136)) for n in range(0, 3000, 7)]
+    assert held == sorted(held)
