@@ -340,7 +340,9 @@ typedef struct {
   int32_t act;      /* bolt_act, SiLU included */
 } bolt_gemm_w4_desc;
 
-/* A: M x K (lda), packed: bolt_w4_pack(N, K, group, 1), bias: N halves or NULL, D: M x N (ldd).  K, N, lda, ldd multiples of 8. */
+/* A: M x K (lda), packed: bolt_w4_pack(N, K, group, 1), bias: N halves or NULL, D: M x N (ldd).  K, N, lda, ldd multiples of 8.
+ * From M = 512 and M * N = 2^19 on the workspace has room for N x K halves (none, and no unpacking, where those are 2 GiB or more): such
+ * layers may be unpacked and run on weights in FP16. */
 bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const void* packed, const void* bias, void* D, void* workspace,
                          size_t workspace_bytes, void* stream);
 size_t bolt_gemm_w4_workspace_bytes(const bolt_gemm_w4_desc* desc);

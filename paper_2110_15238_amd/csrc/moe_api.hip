@@ -266,9 +266,12 @@ const DenseTile& dense_tile(int64_t M, int64_t N, int64_t steps, int group) {
     if (dense_us(t, M, N, steps, group) < dense_us(*best, M, N, steps, group)) best = &t;
   return *best;
 }
+// Rows from which unpacking can pay: the caller's buffer for unpacked weights goes by this alone, so that it does not come and go as M grows.
+// (Unpacked weights are addressed with 31-bit offsets.)
+bool dense_may_unpack(int64_t M, int64_t N, int64_t K) { return M >= 512 && M * N >= 1 << 19 && N * K * 2 <= INT32_MAX; }
 // Unpacking (10 bytes written and read for 4 weights, 4 TB/s) and a GEMM on FP16 operands, against the best tile on packed ones.
 bool dense_unpacks(int64_t M, int64_t N, int64_t K, int group) {
-  if (M < 512 || N * K * 2 > INT32_MAX) return false;  // (unpacked weights are addressed with 31-bit offsets)
+  if (!dense_may_unpack(M, N, K)) return false;
   const int64_t steps = W4Format(N, K, group).steps;
   const double unpacked = 9.0 + 2.5 * (double)N * K / 4.0e6 + 2.0 * (double)M * N * K / 1.25e9;
   return unpacked < dense_us(dense_tile(M, N, steps, group), M, N, steps, group);
@@ -374,7 +377,7 @@ bolt_status bolt_w4_pack(int32_t N, int32_t K, int32_t group, int32_t count, con
 }
 
 size_t bolt_gemm_w4_workspace_bytes(const bolt_gemm_w4_desc* desc) {
-  if (check_gemm_w4(desc) != BOLT_OK || !dense_unpacks(desc->M, desc->N, desc->K, desc->group)) return 0;
+  if (check_gemm_w4(desc) != BOLT_OK || !dense_may_unpack(desc->M, desc->N, desc->K)) return 0;
   return (size_t)desc->N * desc->K * 2;
 }
 
@@ -390,7 +393,7 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   const W4Format f(desc->N, desc->K, desc->group);
   const DenseTile& tile = dense_tile(desc->M, desc->N, f.steps, desc->group);
   // (alpha 0: the kernels of many rows start their sums at beta / alpha times the bias)
-  const bool packed_tiles = desc->M > 16 && (need == 0 || desc->alpha == 0.f);
+  const bool packed_tiles = desc->M > 16 && (desc->alpha == 0.f || !dense_unpacks(desc->M, desc->N, desc->K, desc->group));
   if (packed_tiles && !launches(blocks_of(desc->M, tile.rows) * blocks_of(desc->N, tile.cols))) return BOLT_ERR_UNSUPPORTED;
   const hipStream_t st = (hipStream_t)stream;
   const half_t* none = no_bias();

@@ -97,3 +97,14 @@ def test_workspace_of_the_routing_does_not_fall_as_tokens_grow(bolt, experts):
 def test_workspace_of_the_experts_does_not_fall_as_tokens_grow(bolt):
     held = [bolt.bolt_moe_workspace_bytes(bolt.moe_desc(n, 16, 4, 264, 136)) for n in range(0, 3000, 7)]
     assert held == sorted(held)
+
+
+@pytest.mark.parametrize("N,K,group", [(1024, 8192, 128), (4096, 4096, 64), (256, 8192, 32), (72, 4104, 32), (12288, 520, 128)])
+@pytest.mark.parametrize("act", ["relu", "silu"])
+def test_workspace_of_the_4_bit_layer_does_not_fall_as_rows_grow(bolt, N, K, group, act):
+    held = [bolt.bolt_gemm_w4_workspace_bytes(bolt.gemm_w4_desc(M, N, K, group, act=act)) for M in (*range(1, 9000, 13), 1 << 17, 1 << 20)]
+    assert held == sorted(held) and held[0] == 0 and held[-1] == N * K * 2
+
+
+def test_weights_of_2_gib_are_not_unpacked(bolt):
+    assert bolt.bolt_gemm_w4_workspace_bytes(bolt.gemm_w4_desc(4096, 1 << 15, 1 << 15, 128)) == 0
