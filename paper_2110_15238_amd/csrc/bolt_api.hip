@@ -409,8 +409,8 @@ static bool tune_log_enabled() {
   return on;
 }
 
-// need_split_k: only instances that can write partial sums qualify (the caller asked for split-K).
-static int fprop_heuristic(const std::vector<FpropInstance>& tab, const FpropProblem& pr, bool need_split_k = false) {
+// need_split_k: only instances that can write partial sums qualify (the caller asked for split-K).  us: the pick's estimate.
+static int fprop_heuristic(const std::vector<FpropInstance>& tab, const FpropProblem& pr, bool need_split_k = false, double* us = nullptr) {
   int best = -1;
   double best_cost = 0;
   for (int i = 0; i < (int)tab.size(); ++i) {
@@ -451,6 +451,7 @@ static int fprop_heuristic(const std::vector<FpropInstance>& tab, const FpropPro
     if (best < 0 || cost < best_cost) { best = i; best_cost = cost; }
   }
   if (tune_log_enabled() && best >= 0) std::fprintf(stderr, "[bolt_pick] -> %d %s\n", best, tab[best].name);
+  if (us) *us = best_cost;
   return best;
 }
 
@@ -458,8 +459,8 @@ static int fprop_heuristic(const std::vector<FpropInstance>& tab, const FpropPro
 // 0.8 us of host time per call, as much as a quarter of the smallest launch.  The key is every number that the rule and
 // the instances' legality tests read (sizes, leading dimensions, geometry, modes, the activation, whether alpha is 1), no
 // address; a collision replaces.
-static int fprop_pick(const std::vector<FpropInstance>& tab, const FpropProblem& pr, bool need_split_k) {
-  if (tune_log_enabled()) return fprop_heuristic(tab, pr, need_split_k);
+static int fprop_pick(const std::vector<FpropInstance>& tab, const FpropProblem& pr, bool need_split_k, double* us = nullptr) {
+  if (tune_log_enabled()) return fprop_heuristic(tab, pr, need_split_k, us);
   struct Key {
     const void* tab;
     int flags, M, N, K, ldx, ldw, ldy;
@@ -473,15 +474,17 @@ static int fprop_pick(const std::vector<FpropInstance>& tab, const FpropProblem&
   struct Entry {
     Key key;
     int id;
+    double us;
   };
   static thread_local Entry memo[64];  // (zero: no table at a null address)
   unsigned h = (unsigned)key.flags;
   for (int v : {key.M, key.N, key.K, key.ldx, key.cg.H, key.cg.R, key.cg.stride_h}) h = (h ^ (unsigned)v) * 0x9E3779B1u;
   Entry& e = memo[h >> 26];
   if (std::memcmp(&e.key, &key, sizeof(key)) != 0) {
-    e.id = fprop_heuristic(tab, pr, need_split_k);
+    e.id = fprop_heuristic(tab, pr, need_split_k, &e.us);
     e.key = key;
   }
+  if (us) *us = e.us;
   return e.id;
 }
 
@@ -534,6 +537,11 @@ static bolt_status make_gemm_problem(const bolt_gemm_desc* d, FpropProblem* pr) 
   p.ldx = d->lda; p.ldw = d->ldb; p.ldy = d->ldd;
   p.alpha = d->alpha; p.beta = d->beta; p.act = d->act;
   return BOLT_OK;
+}
+
+bool estimate_gemm(const bolt_gemm_desc& d, double* us) {
+  FpropProblem pr;
+  return make_gemm_problem(&d, &pr) == BOLT_OK && fprop_pick(tables().gemm, pr, false, us) >= 0;
 }
 
 static bolt_status make_conv_problem(const bolt_conv_desc* d, FpropProblem* pr) {

@@ -1,6 +1,7 @@
 // What launches the products of rows with packed or FP16 weights: one function per family (csrc/inst_few_rows_*.hip,
 // csrc/inst_shared_rows_*.hip, csrc/inst_moe_tile.hip).  mode: ROWS_*.
 #pragma once
+#include "../../include/bolt.h"
 #include "routed_rows.hpp"
 
 namespace bolt {
@@ -27,4 +28,7 @@ hipError_t launch_few_rows_w4(const RowsParams& p, int mode, bool gated, int gro
 hipError_t launch_shared_rows_f16(const RowsParams& p, int mode, bool gated, hipStream_t stream);
 hipError_t launch_shared_rows_w4(const RowsParams& p, int mode, bool gated, int group, SharedTile tile, hipStream_t stream);
 hipError_t launch_many_rows_f16(const RowsParams& p, int mode, bool gated, ManyTile tile, hipStream_t stream);
+
+// What bolt_gemm_epilogue's own choice of a kernel is estimated to take, in us; false where it has none (csrc/bolt_api.hip).
+bool estimate_gemm(const bolt_gemm_desc& d, double* us);
 }  // namespace bolt

@@ -269,12 +269,25 @@ const DenseTile& dense_tile(int64_t M, int64_t N, int64_t steps, int group) {
 // Rows from which unpacking can pay: the caller's buffer for unpacked weights goes by this alone, so that it does not come and go as M grows.
 // (Unpacked weights are addressed with 31-bit offsets.)
 bool dense_may_unpack(int64_t M, int64_t N, int64_t K) { return M >= 512 && M * N >= 1 << 19 && N * K * 2 <= INT32_MAX; }
-// Unpacking (10 bytes written and read for 4 weights, 4 TB/s) and a GEMM on FP16 operands, against the best tile on packed ones.
-bool dense_unpacks(int64_t M, int64_t N, int64_t K, int group) {
-  if (!dense_may_unpack(M, N, K)) return false;
-  const int64_t steps = W4Format(N, K, group).steps;
-  const double unpacked = 9.0 + 2.5 * (double)N * K / 4.0e6 + 2.0 * (double)M * N * K / 1.25e9;
-  return unpacked < dense_us(dense_tile(M, N, steps, group), M, N, steps, group);
+// The FP16 layer over unpacked weights.
+bolt_gemm_desc unpacked_desc(const bolt_gemm_w4_desc& d) {
+  return {d.M, d.N, d.K, d.lda, d.K, d.ldd, d.alpha, d.beta, d.act, BOLT_LAYOUT_NK};
+}
+// Unpacking and a GEMM on FP16 operands, by the estimate of the GEMM's own kernel, against the best tile on packed ones.  SiLU has one
+// kernel there, 256 x 256 tiles, and an estimate of its own (a fit to the same sizes).  us on packed weights / unpacked / unpacked with
+// SiLU, groups of 128: 2048 rows of 256 x 8192 23 / 29 / 133; 512 of 1024 x 12288 31 / 46 / 197; 1536 of 4096 x 4096 68 / 63 / 87; 4096 of
+// 4096 x 4096 149 / 114 / 118.  Over 221 sizes (256 to 12288 outputs, K 512 to 12288, 512 to 8192 rows) with groups of 32 and 128 the
+// choice takes 1.02 times the faster side (1.32 at most; packed ones everywhere 1.13 and 1.85), with SiLU 1.01 (1.27; 1.03 and 1.32).
+bool dense_unpacks(const bolt_gemm_w4_desc& d) {
+  if (!dense_may_unpack(d.M, d.N, d.K)) return false;
+  const int64_t steps = W4Format(d.N, d.K, d.group).steps;
+  const double packed = dense_us(dense_tile(d.M, d.N, steps, d.group), d.M, d.N, steps, d.group), weights = (double)d.N * d.K * 1e-6;
+  if (d.act == BOLT_ACT_SILU) {
+    const double rounds = (double)blocks_of(blocks_of(d.M, 256) * blocks_of(d.N, 256), 256);
+    return 12.3 + 0.57 * weights + blocks_of(d.K, 64) * (rounds <= 1 ? 0.95 : 1.29 * rounds) + 0.79e-6 * d.M * d.N < packed;
+  }
+  double gemm;
+  return launches(blocks_of(d.M, 32) * blocks_of(d.N, 32)) && estimate_gemm(unpacked_desc(d), &gemm) && 3.0 + 0.6 * weights + gemm < packed;
 }
 
 // ---- which kernels run the experts ------------------------------------------------------------------------------------
@@ -393,7 +406,7 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   const W4Format f(desc->N, desc->K, desc->group);
   const DenseTile& tile = dense_tile(desc->M, desc->N, f.steps, desc->group);
   // (alpha 0: the kernels of many rows start their sums at beta / alpha times the bias)
-  const bool packed_tiles = desc->M > 16 && (desc->alpha == 0.f || !dense_unpacks(desc->M, desc->N, desc->K, desc->group));
+  const bool packed_tiles = desc->M > 16 && (desc->alpha == 0.f || !dense_unpacks(*desc));
   if (packed_tiles && !launches(blocks_of(desc->M, tile.rows) * blocks_of(desc->N, tile.cols))) return BOLT_ERR_UNSUPPORTED;
   const hipStream_t st = (hipStream_t)stream;
   const half_t* none = no_bias();
@@ -414,7 +427,7 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   if (packed_tiles) return status_of(launch_shared_rows_w4(p, ROWS_DENSE, false, desc->group, tile.tile, st));
   if (launch_w4_unpack(packed, (half_t*)workspace, f, st) != hipSuccess) return BOLT_ERR_LAUNCH;
   if (desc->act != BOLT_ACT_SILU) {
-    const bolt_gemm_desc g = {desc->M, desc->N, desc->K, desc->lda, desc->K, desc->ldd, desc->alpha, desc->beta, desc->act, BOLT_LAYOUT_NK};
+    const bolt_gemm_desc g = unpacked_desc(*desc);
     return bolt_gemm_epilogue(&g, A, workspace, bias, D, nullptr, nullptr, 0, stream);
   }
   p.w = (const unsigned char*)workspace;

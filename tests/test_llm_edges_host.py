@@ -54,6 +54,7 @@ def test_rows_that_32_bits_cannot_count_past_are_refused(bolt):
 def test_launches_of_two_to_the_32_threads_are_refused(bolt):
     """2^30 rows of 8 outputs (17 GB on either side) are 2^24 tiles of 64 x 128, 512 threads each; 2^30 slots of 8 x 8 experts (a GB of x)
     2^23 of 128 x 256."""
+    assert _gemm(bolt, bolt.gemm_w4_desc(1 << 30, 8, 8, 32)) == UNSUPPORTED
     assert _gemm(bolt, bolt.gemm_w4_desc(1 << 30, 8, 8, 32, alpha=0.0)) == UNSUPPORTED  # (alpha 0: weights as they are packed)
     assert _experts(bolt, bolt.moe_desc(1 << 26, 16, 16, 8, 8, weights="w4", group=32)) == UNSUPPORTED
 
