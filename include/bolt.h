@@ -342,7 +342,8 @@ typedef struct {
 
 /* A: M x K (lda), packed: bolt_w4_pack(N, K, group, 1), bias: N halves or NULL, D: M x N (ldd).  K, N, lda, ldd multiples of 8.
  * From M = 512 and M * N = 2^19 on the workspace has room for N x K halves (none, and no unpacking, where those are 2 GiB or more): such
- * layers may be unpacked and run on weights in FP16. */
+ * layers may be unpacked, by an estimate of the time, and then run on weights scale * (q - z) rounded once to FP16, where the others use them
+ * exactly (outputs that depend on a weight beyond FP16's range always do).  So a row's last bits can depend on how many rows there are. */
 bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const void* packed, const void* bias, void* D, void* workspace,
                          size_t workspace_bytes, void* stream);
 size_t bolt_gemm_w4_workspace_bytes(const bolt_gemm_w4_desc* desc);

@@ -27,6 +27,8 @@ hipError_t launch_few_rows_f16(const RowsParams& p, int mode, bool gated, hipStr
 hipError_t launch_few_rows_w4(const RowsParams& p, int mode, bool gated, int group, hipStream_t stream);
 hipError_t launch_shared_rows_f16(const RowsParams& p, int mode, bool gated, hipStream_t stream);
 hipError_t launch_shared_rows_w4(const RowsParams& p, int mode, bool gated, int group, SharedTile tile, hipStream_t stream);
+// A linear layer's outputs whose tiles of 16 weight rows are marked in p.unpacked, and no others.
+hipError_t launch_shared_rows_w4_marked(const RowsParams& p, int group, hipStream_t stream);
 hipError_t launch_many_rows_f16(const RowsParams& p, int mode, bool gated, ManyTile tile, hipStream_t stream);
 
 // What bolt_gemm_epilogue's own choice of a kernel is estimated to take, in us; false where it has none (csrc/bolt_api.hip).

@@ -24,6 +24,11 @@ static hipError_t launch_group(const RowsParams& p, int group, SharedTile tile, 
   if (group == 64) return launch<MODE, GATED, 2>(p, tile, stream);
   return launch<MODE, GATED, 4>(p, tile, stream);
 }
+hipError_t launch_shared_rows_w4_marked(const RowsParams& p, int group, hipStream_t stream) {
+  if (group == 128) return launch_shared_rows_marked<1, 8, 2, 8, 3>(p, stream);
+  if (group == 64) return launch_shared_rows_marked<2, 8, 2, 8, 3>(p, stream);
+  return launch_shared_rows_marked<4, 8, 2, 8, 3>(p, stream);
+}
 hipError_t launch_shared_rows_w4(const RowsParams& p, int mode, bool gated, int group, SharedTile tile, hipStream_t stream) {
   if (mode == ROWS_DENSE) return launch_group<ROWS_DENSE, false>(p, group, tile, stream);
   if (mode == ROWS_DOWN) return launch_group<ROWS_DOWN, false>(p, group, tile, stream);

@@ -56,6 +56,8 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const unsigned char* q, co
 // A packed 4-bit matrix as [N][K] halves, scale * (q - z) rounded once: for problems of so many rows that the matrix cores bound
 // them, where decoding once and running on operands in FP16 costs less than decoding in every tile.  The rounding is that of a weight
 // held in FP16.  One thread for 16 packed bytes.
+// A weight beyond a half's range (a scale above kW4MostScale) has no such form: the first element of a tile of 16 rows with one is left
+// a NaN, which no other tile has there, and launch_shared_rows_w4_marked computes those tiles' outputs from the packed weights.
 template <int NG>
 __global__ __launch_bounds__(256) void w4_unpack_kernel(const unsigned char* packed, half_t* out, const W4Format f) {
   const half_t* const scales = (const half_t*)(packed + f.scales_at(1));
@@ -65,6 +67,16 @@ __global__ __launch_bounds__(256) void w4_unpack_kernel(const unsigned char* pac
     const int lane = (int)(i & 63), g = lane >> 4, r = lane & 15;
     const int64_t block = i >> 6, tile = block / f.steps;
     const int step = (int)(block - tile * f.steps), row = (int)tile * 16 + r;
+    bool marked = false;
+    if (step == 0) {  // (the same for all lanes of a wave, which share the tile's scales)
+      const half8* const all = (const half8*)(scales + tile * f.steps * (16 * NG));
+      for (int j = lane; j < f.steps * (2 * NG); j += 64) {
+        const half8 v = all[j];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) marked |= !(__builtin_fabsf((float)v[e]) <= kW4MostScale);
+      }
+      marked = __any(marked) && lane == 0;
+    }
     if (row >= f.N) continue;
     const uintx4 w = *(const uintx4*)(packed + i * 16);
     half_t* const to = out + (int64_t)row * f.K;
@@ -74,7 +86,9 @@ __global__ __launch_bounds__(256) void w4_unpack_kernel(const unsigned char* pac
       if (k >= f.K) continue;
       const unsigned z = zeros[(block * 16 + r) * NG + j];
       const half_t scale = scales[((block * 4 + (r >> 2)) * NG + j) * 4 + (r & 3)];
-      *(half8*)(to + k) = w4_values(w[s], w4_minus1(z), w4_minus16(z)) * scale;
+      half8 v = w4_values(w[s], w4_minus1(z), w4_minus16(z)) * scale;
+      if (s == 0 && marked) v[0] = __builtin_bit_cast(half_t, (unsigned short)0x7e00);
+      *(half8*)(to + k) = v;
     }
   }
 }
@@ -273,21 +287,22 @@ bool dense_may_unpack(int64_t M, int64_t N, int64_t K) { return M >= 512 && M * 
 bolt_gemm_desc unpacked_desc(const bolt_gemm_w4_desc& d) {
   return {d.M, d.N, d.K, d.lda, d.K, d.ldd, d.alpha, d.beta, d.act, BOLT_LAYOUT_NK};
 }
-// Unpacking and a GEMM on FP16 operands, by the estimate of the GEMM's own kernel, against the best tile on packed ones.  SiLU has one
-// kernel there, 256 x 256 tiles, and an estimate of its own (a fit to the same sizes).  us on packed weights / unpacked / unpacked with
-// SiLU, groups of 128: 2048 rows of 256 x 8192 23 / 29 / 133; 512 of 1024 x 12288 31 / 46 / 197; 1536 of 4096 x 4096 68 / 63 / 87; 4096 of
-// 4096 x 4096 149 / 114 / 118.  Over 221 sizes (256 to 12288 outputs, K 512 to 12288, 512 to 8192 rows) with groups of 32 and 128 the
-// choice takes 1.02 times the faster side (1.32 at most; packed ones everywhere 1.13 and 1.85), with SiLU 1.01 (1.27; 1.03 and 1.32).
+// Unpacking, a GEMM on FP16 operands, by the estimate of the GEMM's own kernel, and the launch that looks for marked weights, against the
+// best tile on packed ones.  SiLU has one kernel there, 256 x 256 tiles, and an estimate of its own (a fit to the same sizes).  us on packed
+// weights / unpacked / unpacked with SiLU, groups of 128: 2048 rows of 256 x 8192 23 / 34 / 138; 512 of 1024 x 12288 31 / 51 / 202; 1536
+// of 4096 x 4096 68 / 68 / 92; 4096 of 4096 x 4096 149 / 119 / 123.  Over 221 sizes (256 to 12288 outputs, K 512 to 12288, 512 to 8192
+// rows) with groups of 32 and 128 the choice takes 1.01 times the faster side (1.36 at most; packed ones everywhere 1.09 and 1.77), with
+// SiLU 1.004 (1.23; 1.03 and 1.29).
 bool dense_unpacks(const bolt_gemm_w4_desc& d) {
   if (!dense_may_unpack(d.M, d.N, d.K)) return false;
   const int64_t steps = W4Format(d.N, d.K, d.group).steps;
   const double packed = dense_us(dense_tile(d.M, d.N, steps, d.group), d.M, d.N, steps, d.group), weights = (double)d.N * d.K * 1e-6;
   if (d.act == BOLT_ACT_SILU) {
     const double rounds = (double)blocks_of(blocks_of(d.M, 256) * blocks_of(d.N, 256), 256);
-    return 12.3 + 0.57 * weights + blocks_of(d.K, 64) * (rounds <= 1 ? 0.95 : 1.29 * rounds) + 0.79e-6 * d.M * d.N < packed;
+    return 17.3 + 0.57 * weights + blocks_of(d.K, 64) * (rounds <= 1 ? 0.95 : 1.29 * rounds) + 0.79e-6 * d.M * d.N < packed;
   }
   double gemm;
-  return launches(blocks_of(d.M, 32) * blocks_of(d.N, 32)) && estimate_gemm(unpacked_desc(d), &gemm) && 3.0 + 0.6 * weights + gemm < packed;
+  return launches(blocks_of(d.M, 32) * blocks_of(d.N, 32)) && estimate_gemm(unpacked_desc(d), &gemm) && 8.0 + 0.6 * weights + gemm < packed;
 }
 
 // ---- which kernels run the experts ------------------------------------------------------------------------------------
@@ -428,11 +443,15 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   if (launch_w4_unpack(packed, (half_t*)workspace, f, st) != hipSuccess) return BOLT_ERR_LAUNCH;
   if (desc->act != BOLT_ACT_SILU) {
     const bolt_gemm_desc g = unpacked_desc(*desc);
-    return bolt_gemm_epilogue(&g, A, workspace, bias, D, nullptr, nullptr, 0, stream);
+    if (bolt_status s = bolt_gemm_epilogue(&g, A, workspace, bias, D, nullptr, nullptr, 0, stream); s != BOLT_OK) return s;
+  } else {
+    RowsParams u = p;
+    u.w = (const unsigned char*)workspace;
+    u.w_stride = (int64_t)p.N * p.K * 2;
+    if (launch_many_rows_f16(u, ROWS_DENSE, false, ManyTile::ROWS256, st) != hipSuccess) return BOLT_ERR_LAUNCH;
   }
-  p.w = (const unsigned char*)workspace;
-  p.w_stride = (int64_t)p.N * p.K * 2;
-  return status_of(launch_many_rows_f16(p, ROWS_DENSE, false, ManyTile::ROWS256, st));
+  p.unpacked = (const half_t*)workspace;
+  return status_of(launch_shared_rows_w4_marked(p, desc->group, st));
 }
 
 size_t bolt_moe_route_workspace_bytes(const bolt_moe_route_desc* desc) {

@@ -51,6 +51,7 @@ struct RowsParams {
   const int* order;
   int experts, top_k;
   int row_blocks, col_blocks;
+  const half_t* unpacked;      // [N][K], for the marks of w4_unpack_kernel
   int walk;                    // tiles of columns that a workgroup walks over
 };
 

@@ -40,37 +40,11 @@ struct SharedRowsTraits {
 };
 
 template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S>
-__global__ __launch_bounds__(64 * WN * KG) void shared_rows_kernel(const RowsParams p) {
+__device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<WT, MODE, GATED, NG, MB, R>& w, int wave_all, int cb, half_t* lds) {
   using T = SharedRowsTraits<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
   using Wave = RowsWave<WT, MODE, GATED, NG, MB, R>;
   constexpr int BM = T::BM, KS = T::KS;
-  extern __shared__ __attribute__((aligned(16))) half_t lds[];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave_all = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kg = wave_all / WN, wave = wave_all - kg * WN;
-  Wave w(p, lane);
-
-  // ---- the tile ---------------------------------------------------------------------------------------------------
-  int cb;
-  if constexpr (MODE == ROWS_DENSE) {
-    const int id = xcd_run((int)blockIdx.x, (int)gridDim.x);
-    cb = id / p.row_blocks;
-    w.row0 = (id - cb * p.row_blocks) * BM;
-    w.rows = p.M - w.row0 < BM ? p.M - w.row0 : BM;
-  } else {
-    const BlockCounts counts = count_row_blocks<BM>(p.offsets, p.experts, lane);
-    const int total = counts.total() * p.col_blocks;
-    if ((int)blockIdx.x >= total) return;
-    const int tile = xcd_run((int)blockIdx.x, total);
-    RowBlock at;
-    if (!find_row_block<BM>(p.offsets, counts, tile / p.col_blocks, &at)) return;
-    const int local = tile - at.first * p.col_blocks;
-    cb = local / at.count;
-    const int done = (local - cb * at.count) * BM;
-    w.expert = at.expert;
-    w.row0 = at.lo + done;
-    w.rows = at.n - done < BM ? at.n - done : BM;
-  }
+  const int lane = w.lane, kg = wave_all / WN, wave = wave_all - kg * WN;
   const int col0 = cb * T::COLS + wave * (16 * R / (GATED ? 2 : 1));  // this wave's first output column
   w.take_columns(col0);
   // Scales and zero points: lane l of piece m loads dword 64 m + l of a wave's step: R * NG * 8 of scales ([tile][quad of rows][group][4
@@ -238,6 +212,53 @@ v = apply_act4(v, p.act);
 }
 
 template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S>
+__global__ __launch_bounds__(64 * WN * KG) void shared_rows_kernel(const RowsParams p) {
+  using T = SharedRowsTraits<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
+  constexpr int BM = T::BM;
+  extern __shared__ __attribute__((aligned(16))) half_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  RowsWave<WT, MODE, GATED, NG, MB, R> w(p, lane);
+  int cb;
+  if constexpr (MODE == ROWS_DENSE) {
+    const int id = xcd_run((int)blockIdx.x, (int)gridDim.x);
+    cb = id / p.row_blocks;
+    w.row0 = (id - cb * p.row_blocks) * BM;
+    w.rows = p.M - w.row0 < BM ? p.M - w.row0 : BM;
+  } else {
+    const BlockCounts counts = count_row_blocks<BM>(p.offsets, p.experts, lane);
+    const int total = counts.total() * p.col_blocks;
+    if ((int)blockIdx.x >= total) return;
+    const int tile = xcd_run((int)blockIdx.x, total);
+    RowBlock at;
+    if (!find_row_block<BM>(p.offsets, counts, tile / p.col_blocks, &at)) return;
+    const int local = tile - at.first * p.col_blocks;
+    cb = local / at.count;
+    const int done = (local - cb * at.count) * BM;
+    w.expert = at.expert;
+    w.row0 = at.lo + done;
+    w.rows = at.n - done < BM ? at.n - done : BM;
+  }
+  shared_rows_tile<WT, MODE, GATED, NG, MB, R, WN, KG, S>(p, w, __builtin_amdgcn_readfirstlane(tid >> 6), cb, lds);
+}
+
+// The tiles of columns that hold marked weights (w4_unpack_kernel), all rows; a workgroup whose columns hold none reads 16 numbers and ends.
+template <int NG, int MB, int R, int WN, int S>
+__global__ __launch_bounds__(64 * WN) void shared_rows_marked_kernel(const RowsParams p) {
+  using T = SharedRowsTraits<WEIGHTS_W4, ROWS_DENSE, false, NG, MB, R, WN, 1, S>;
+  extern __shared__ __attribute__((aligned(16))) half_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63, cb = blockIdx.x;
+  const int row = cb * T::COLS + (lane < T::COLS / 16 ? lane : 0) * 16;
+  const half_t first = row < p.N ? p.unpacked[(int64_t)row * p.K] : (half_t)0.f;
+  if (!__any(first != first)) return;  // (the same for every wave)
+  for (int rb = blockIdx.y; rb < p.row_blocks; rb += gridDim.y) {
+    RowsWave<WEIGHTS_W4, ROWS_DENSE, false, NG, MB, R> w(p, lane);
+    w.row0 = rb * T::BM;
+    w.rows = p.M - w.row0 < T::BM ? p.M - w.row0 : T::BM;
+    shared_rows_tile<WEIGHTS_W4, ROWS_DENSE, false, NG, MB, R, WN, 1, S>(p, w, __builtin_amdgcn_readfirstlane(tid >> 6), cb, lds);
+  }
+}
+
+template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S>
 hipError_t launch_shared_rows(RowsParams p, hipStream_t stream) {
   auto kern = shared_rows_kernel<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
   using T = SharedRowsTraits<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
@@ -246,6 +267,18 @@ hipError_t launch_shared_rows(RowsParams p, hipStream_t stream) {
   p.col_blocks = ((GATED ? p.hidden : p.N) + T::COLS - 1) / T::COLS;
   p.row_blocks = row_blocks<T::BM>(p, MODE);
   hipLaunchKernelGGL(kern, dim3(p.row_blocks * p.col_blocks), dim3(T::NT), T::LDS_BYTES, stream, p);
+  return hipGetLastError();
+}
+template <int NG, int MB, int R, int WN, int S>
+hipError_t launch_shared_rows_marked(RowsParams p, hipStream_t stream) {
+  auto kern = shared_rows_marked_kernel<NG, MB, R, WN, S>;
+  using T = SharedRowsTraits<WEIGHTS_W4, ROWS_DENSE, false, NG, MB, R, WN, 1, S>;
+  static LdsOptIn opt_in;
+  if (hipError_t e = opt_in.ensure((const void*)kern, T::LDS_BYTES); e != hipSuccess) return e;
+  p.col_blocks = (p.N + T::COLS - 1) / T::COLS;
+  p.row_blocks = row_blocks<T::BM>(p, ROWS_DENSE);
+  const int per_column = p.col_blocks < 256 ? 256 / p.col_blocks : 1;  // workgroups: one round of the compute units
+  hipLaunchKernelGGL(kern, dim3(p.col_blocks, p.row_blocks < per_column ? p.row_blocks : per_column), dim3(T::NT), T::LDS_BYTES, stream, p);
   return hipGetLastError();
 }
 

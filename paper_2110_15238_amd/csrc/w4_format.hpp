@@ -30,6 +30,10 @@ struct W4Format {
   int64_t bytes(int count) const { return zeros_at(count) + count * scale_count; }
 };
 
+// Largest scale (in absolute value) of which every multiple up to 15 is finite as a half: 15 * 4364 = 65460, and 15 * 4368 = 65520 rounds to
+// infinity.
+static constexpr float kW4MostScale = 4364.f;
+
 // Eight values q - z as halves, exact: 0x6400 | q is 1024 + q and 0x6400 | q << 4 is 1024 + 16 q as a half; minus1 holds two
 // halves -1024 - z, minus16 two halves -64 - z.  The empty asm keeps the constants in registers: as literals they would make two
 // instructions of every (w & mask) | exponent.

@@ -32,3 +32,46 @@ def test_gemm_w4_narrow_layers_run_on_the_weights_as_they_are(bolt, M, N, K, gro
     y = ref.act(A.double() @ _matrix(raw, group).t().contiguous(), act)
     size = A.double() @ _matrix(raw, group).abs().t().contiguous()
     _within(_gemm(bolt, d, A, packed), y, size * 3 * ref.U32 * ref.STEEP + y.abs() * ((ref.CLOSE if act == "silu" else 0) + ref.U16) + ref.TINY)
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("K,group", [(1032, 32), (2056, 64), (4104, 128)])
+def test_gemm_w4_unpacked_takes_weights_beyond_a_half(bolt, act, K, group):
+    """scale * (q - z) past 65504: finite at every number of rows, in the columns that hold such weights and in the others."""
+    M, N = 4096, 8200
+    g = _gen(group)
+    groups = -(-K // group)
+    q = torch.randint(0, 256, (1, N, K // 2), dtype=torch.uint8, device="cuda", generator=g)
+    s = ((torch.rand((1, N, groups), device="cuda", generator=g) + 0.1) * (0.4 / math.sqrt(K))).half()
+    z = torch.randint(0, 16, (1, N, groups), dtype=torch.uint8, device="cuda", generator=g)
+    for n, k, v in ((5, 3, 6e4), (5, 4, -5e3), (300, 0, 4368.0), (8199, groups - 1, 65504.0), (4000, 1, 4364.0)):
+        s[0, n, k] = v
+    packed = torch.empty(bolt.bolt_w4_packed_bytes(N, K, group), dtype=torch.uint8, device="cuda")
+    bolt.bolt_w4_pack(N, K, group, q, s, z, packed)
+    A, bias = _half(g, M, K, std=1e-3), _half(g, N)
+    W = _matrix((q, s, z), group)
+    assert W.abs().max() > 65520  # (infinite as a half)
+    want, bound = ref.linear(A.double(), W, bias.double(), act, 0.5, shift=ref.U16)
+    inside = want.abs() < 6e4
+    d = bolt.gemm_w4_desc(M, N, K, group, act=act, alpha=0.5)
+    got = _gemm(bolt, d, A, packed, bias)
+    _within(got[inside], want[inside], bound[inside])
+    assert inside.double().mean() > 0.99
+    few = _gemm(bolt, bolt.gemm_w4_desc(8, N, K, group, act=act, alpha=0.5), A[:8].contiguous(), packed, bias)
+    assert (torch.isfinite(few) == torch.isfinite(got[:8])).all()
+
+
+def test_gemm_w4_unpacked_keeps_scales_that_are_not_finite_to_their_columns(bolt):
+    M, N, K, group = 4096, 8192, 520, 32
+    g = _gen(9)
+    raw, _ = _w4(bolt, g, 1, N, K, group)
+    raw[1][0, 77, 2], raw[1][0, 4100, 0] = float("inf"), float("nan")
+    packed = torch.empty(bolt.bolt_w4_packed_bytes(N, K, group), dtype=torch.uint8, device="cuda")
+    bolt.bolt_w4_pack(N, K, group, *raw, packed)
+    A = _half(g, M, K)
+    got = _gemm(bolt, bolt.gemm_w4_desc(M, N, K, group), A, packed)
+    others = torch.ones(N, dtype=torch.bool, device="cuda")
+    others[[77, 4100]] = False
+    assert not torch.isfinite(got[:, ~others]).any()
+    W = _matrix(raw, group)[others]
+    _within(got[:, others], *ref.linear(A.double(), W, None, "none", shift=ref.U16))
