@@ -420,8 +420,9 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   if (!aligned16(workspace)) return BOLT_ERR_ALIGNMENT;
   const W4Format f(desc->N, desc->K, desc->group);
   const DenseTile& tile = dense_tile(desc->M, desc->N, f.steps, desc->group);
-  // (alpha 0: the kernels of many rows start their sums at beta / alpha times the bias)
-  const bool packed_tiles = desc->M > 16 && (desc->alpha == 0.f || !dense_unpacks(*desc));
+  // The kernels of many rows start their sums at beta / alpha times the bias, which has to be finite.
+  const bool bias_in_sum = desc->alpha != 0.f && std::fabs(desc->beta) <= 1e30f * std::fabs(desc->alpha);
+  const bool packed_tiles = desc->M > 16 && (!bias_in_sum || !dense_unpacks(*desc));
   if (packed_tiles && !launches(blocks_of(desc->M, tile.rows) * blocks_of(desc->N, tile.cols))) return BOLT_ERR_UNSUPPORTED;
   const hipStream_t st = (hipStream_t)stream;
   const half_t* none = no_bias();

@@ -226,7 +226,7 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
     if (grp == 0) wait_loads_0();
     else wait_loads_x();
     wait_reads();
-    const float bias_scale = MODE == ROWS_DENSE ? p.beta / p.alpha : 1.f;  // (the host keeps alpha from being zero)
+    const float bias_scale = MODE == ROWS_DENSE ? p.beta / p.alpha : 1.f;  // (the host keeps it finite)
 #pragma unroll
     for (int a = 0; a < FN; ++a)
 #pragma unroll

@@ -75,3 +75,16 @@ def test_gemm_w4_unpacked_keeps_scales_that_are_not_finite_to_their_columns(bolt
     assert not torch.isfinite(got[:, ~others]).any()
     W = _matrix(raw, group)[others]
     _within(got[:, others], *ref.linear(A.double(), W, None, "none", shift=ref.U16))
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("alpha", [1e-36, 1e-39])
+@pytest.mark.parametrize("with_bias", [True, False])
+def test_gemm_w4_unpacked_takes_an_alpha_next_to_zero(bolt, act, alpha, with_bias):
+    """beta / alpha times the bias, where the sums of many rows start, is past 32 bits."""
+    M, N, K = 4096, 8192, 520
+    g = _gen(11)
+    raw, packed = _w4(bolt, g, 1, N, K, 32)
+    A, bias = _half(g, M, K), _half(g, N, std=1000.0) if with_bias else None
+    d = bolt.gemm_w4_desc(M, N, K, 32, act=act, alpha=alpha, beta=0.5)
+    _within(_gemm(bolt, d, A, packed, bias), *ref.linear(A.double(), _matrix(raw, 32), None if bias is None else bias.double(), act, d.alpha, d.beta))
