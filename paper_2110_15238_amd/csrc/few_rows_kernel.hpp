@@ -87,7 +87,7 @@ struct RowsWave {
     }
   }
   // Step `step` of the weights.  4-bit weights are padded to whole steps.  FP16, RAGGED: beyond column K a lane reads its row's first
-  // columns instead, which meet zeros.
+  // columns instead.
   template <bool RAGGED>
   __device__ __forceinline__ void load_weights(int step, Weights& out) const {
 #pragma unroll
@@ -122,7 +122,10 @@ struct RowsWave {
         out.part[s][b] = in ? v : half8{0, 0, 0, 0, 0, 0, 0, 0};
       }
   }
-  __device__ __forceinline__ void multiply(const Weights& w, const Rows& x, floatx4 (&acc)[R][MB]) const {
+  // RAGGED: step `step` may end beyond column K or not exist.  What was read in place of its weights meets zero activations, and is zero here, as an
+  // infinite one would make a NaN of that: FP16 weights, the scales of 4-bit ones.
+  template <bool RAGGED>
+  __device__ __forceinline__ void multiply(int step, const Weights& w, const Rows& x, floatx4 (&acc)[R][MB]) const {
 #pragma unroll
     for (int t = 0; t < R; ++t) {
       if constexpr (WT == WEIGHTS_W4) {
@@ -139,16 +142,19 @@ struct RowsWave {
 #pragma unroll
             for (int b = 0; b < MB; ++b) sum[b] = mfma_16x16x32(a, x.part[s][b], sum[b]);
           }
+          const half4 scale = !RAGGED || step < p.steps ? w.scale[t][i] : half4{0, 0, 0, 0};
 #pragma unroll
           for (int b = 0; b < MB; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[t][b][e] += (float)w.scale[t][i][e] * sum[b][e];
+            for (int e = 0; e < 4; ++e) acc[t][b][e] += (float)scale[e] * sum[b][e];
         }
       } else {
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+        for (int s = 0; s < KS; ++s) {
+          const uintx4 a = !RAGGED || step * STEP + s * 32 + g * 8 < p.K ? w.piece[t][s] : uintx4{0, 0, 0, 0};
 #pragma unroll
-          for (int b = 0; b < MB; ++b) acc[t][b] = mfma_16x16x32(__builtin_bit_cast(half8, w.piece[t][s]), x.part[s][b], acc[t][b]);
+          for (int b = 0; b < MB; ++b) acc[t][b] = mfma_16x16x32(__builtin_bit_cast(half8, a), x.part[s][b], acc[t][b]);
+        }
       }
     }
   }
@@ -226,7 +232,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
     w.template load_weights<false>(wave + i * NW, wf[decltype(b)::value]);
     w.template load_rows<false>(wave + i * NW, xf[decltype(b)::value]);
   };
-  auto multiply = [&](auto b) { w.multiply(wf[decltype(b)::value], xf[decltype(b)::value], acc); };
+  auto multiply = [&](auto b) { w.template multiply<false>(0, wf[decltype(b)::value], xf[decltype(b)::value], acc); };
   if (n >= NB) {
     for_constants<NB>([&](auto b) { load(decltype(b)::value, b); });
     int c = 0;
@@ -254,7 +260,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
   if (whole < p.steps && whole % NW == wave) {
     w.template load_weights<true>(whole, wf[0]);
     w.template load_rows<true>(whole, xf[0]);
-    w.multiply(wf[0], xf[0], acc);
+    w.template multiply<true>(whole, wf[0], xf[0], acc);
   }
   w.put_sums(part, wave, acc);
   __syncthreads();
@@ -264,8 +270,9 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
 // Reductions of at most NX steps per wave: the wave's share of the activations stays in registers while the workgroup walks over
 // p.walk tiles of columns.  The weights of the next tile are on their way while a tile is multiplied, summed and stored, so the
 // cost of finding the rows and of the first round trip to memory is paid once per walk, and the waves' sums have two places, so one
-// barrier per tile is enough.  Steps that a wave does not have meet zero activations (and read its last step's weights again).
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
+// barrier per tile is enough.  FULL: every wave has NX whole steps; else steps that a wave does not have read the last one again and meet
+// zeros (one token, 8 experts of 2048 x 1024 in FP16, both products and the sum: 28.7 us, and 29.7 so).
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX, bool FULL>
 __global__ __launch_bounds__(64 * NW) void few_rows_walk_kernel(const RowsParams p) {
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int PART = NW * R * 64 * 4;
@@ -292,17 +299,19 @@ __global__ __launch_bounds__(64 * NW) void few_rows_walk_kernel(const RowsParams
     w.take_columns((cb + tile) * Wave::COLS);
     for_constants<NX>([&](auto i) {
       const int step = wave + decltype(i)::value * NW;
-      w.template load_weights<true>(step < last_step ? step : last_step, wf[decltype(set)::value][decltype(i)::value]);
+      w.template load_weights<!FULL>(FULL || step < last_step ? step : last_step, wf[decltype(set)::value][decltype(i)::value]);
     });
   };
   using S0 = std::integral_constant<int, 0>;
   using S1 = std::integral_constant<int, 1>;
   load(0, S0{});
   w.take_rows();
-  for_constants<NX>([&](auto i) { w.template load_rows<true>(wave + decltype(i)::value * NW, xf[decltype(i)::value]); });
+  for_constants<NX>([&](auto i) { w.template load_rows<!FULL>(wave + decltype(i)::value * NW, xf[decltype(i)::value]); });
   auto tile = [&](int it, auto set) {
     floatx4 acc[R][1] = {};
-    for_constants<NX>([&](auto i) { w.multiply(wf[decltype(set)::value][decltype(i)::value], xf[decltype(i)::value], acc); });
+    for_constants<NX>([&](auto i) {
+      w.template multiply<!FULL>(wave + decltype(i)::value * NW, wf[decltype(set)::value][decltype(i)::value], xf[decltype(i)::value], acc);
+    });
     float* const mine = part + decltype(set)::value * PART;
     w.put_sums(mine, wave, acc);
     barrier_after_lds_writes();
@@ -336,9 +345,9 @@ hipError_t launch_few_rows(RowsParams p, hipStream_t stream) {
   hipLaunchKernelGGL(kern, dim3(p.row_blocks * p.col_blocks), dim3(64 * NW), LDS_BYTES, stream, p);
   return hipGetLastError();
 }
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX, bool FULL = false>
 hipError_t launch_few_rows_walk(RowsParams p, hipStream_t stream) {
-  auto kern = few_rows_walk_kernel<WT, MODE, GATED, NG, R, NW, NX>;
+  auto kern = few_rows_walk_kernel<WT, MODE, GATED, NG, R, NW, NX, FULL>;
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int LDS_BYTES = 2 * NW * R * 64 * 16;
   static LdsOptIn opt_in;

@@ -419,7 +419,7 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   if (need > 0 && (!workspace || workspace_bytes < need)) return BOLT_ERR_WORKSPACE;
   if (!aligned16(workspace)) return BOLT_ERR_ALIGNMENT;
   const W4Format f(desc->N, desc->K, desc->group);
-  const DenseTile& tile = dense_tile(desc->M, desc->N, f.steps, desc->group);
+  const DenseTile& tile = desc->M > 16 ? dense_tile(desc->M, desc->N, f.steps, desc->group) : kDenseTiles[0];
   // The kernels of many rows start their sums at beta / alpha times the bias, which has to be finite.
   const bool bias_in_sum = desc->alpha != 0.f && std::fabs(desc->beta) <= 1e30f * std::fabs(desc->alpha);
   const bool packed_tiles = desc->M > 16 && (!bias_in_sum || !dense_unpacks(*desc));
@@ -433,6 +433,7 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   p.w = (const unsigned char*)packed;
   p.scales = (const half_t*)((const char*)packed + f.scales_at(1));
   p.zeros = (const unsigned char*)packed + f.zeros_at(1);
+  p.none = none;
   p.bias = bias ? (const half_t*)bias : none;
   p.bias_on = bias ? 1 : 0;
   p.y = D;
@@ -520,6 +521,7 @@ bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const voi
   p.M = slots;
   p.offsets = (const int*)offsets; p.order = (const int*)order;
   p.experts = E; p.top_k = desc->top_k;
+  p.none = none;
   p.alpha = p.beta = 1.f;
   auto product = [&](int N, int K, const void* w, const void* b, int mode) {
     const bool gate = mode == ROWS_UP && gated;

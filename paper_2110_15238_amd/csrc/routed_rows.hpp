@@ -39,7 +39,8 @@ struct RowsParams {
   const half_t* scales;        // 4 bits only
   const unsigned char* zeros;
   int64_t scale_stride;        // scales from one expert's to the next's
-  const half_t* bias;          // [count][N]; eight zeros if there is none
+  const half_t* none;          // eight zeros
+  const half_t* bias;          // [count][N]; `none` if there is none
   int bias_on;
   void* y;                     // halves; DOWN: floats
   int64_t ldy;

@@ -85,7 +85,7 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
   }
   half_t* const ring = lds + kg * S * T::STAGE;
 
-  // ---- steps kg, kg + KG, ...: every set of waves runs `turns` of them; those past the end meet zero activations -------------
+  // ---- steps kg, kg + KG, ...: every set of waves runs `turns` of them; one past the end is not multiplied -------------------
   const int last_step = p.steps - 1, turns = (p.steps + KG - 1) / KG;
   auto load = [&](int turn, half_t* stage) {
     const int step = kg + turn * KG, at = step < last_step ? step : last_step;
@@ -96,8 +96,8 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
         lds_load16(w.wrow[t] + (int64_t)at * W4Format::BLOCK_BYTES, mine + t * 512);
       } else {
         for_constants<KS>([&](auto sc) {
-          const int k = at * 64 + decltype(sc)::value * 32;  // (beyond K: the row's first columns, which meet zeros)
-          lds_load16(w.wrow[t] + (int64_t)(k + w.g * 8 < p.K ? k : -w.g * 8) * 2, mine + (t * KS + decltype(sc)::value) * 512);
+          const int k = at * 64 + decltype(sc)::value * 32;  // (beyond K: zeros; an infinite weight would make a NaN of the zero it meets)
+          lds_load16(k + w.g * 8 < p.K ? w.wrow[t] + (int64_t)k * 2 : (const unsigned char*)p.none, mine + (t * KS + decltype(sc)::value) * 512);
         });
       }
     });
@@ -160,7 +160,7 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
     // this turn's loads have landed for every wave of the set, and every wave is done with the stage that is filled next
     barrier_after_reads_and_loads<AHEAD>();
     load(t + S - 1, ring + fill * T::STAGE);
-    multiply(ring + stage * T::STAGE);
+    if (KG == 1 || kg + t * KG <= last_step) multiply(ring + stage * T::STAGE);
     fill = stage;
     stage = stage + 1 == S ? 0 : stage + 1;
   }

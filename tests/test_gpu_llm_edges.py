@@ -88,3 +88,49 @@ def test_gemm_w4_unpacked_takes_an_alpha_next_to_zero(bolt, act, alpha, with_bia
     A, bias = _half(g, M, K), _half(g, N, std=1000.0) if with_bias else None
     d = bolt.gemm_w4_desc(M, N, K, 32, act=act, alpha=alpha, beta=0.5)
     _within(_gemm(bolt, d, A, packed, bias), *ref.linear(A.double(), _matrix(raw, 32), None if bias is None else bias.double(), act, d.alpha, d.beta))
+
+
+# few rows: walks with waves that have no step, a short last step; some ten, with sets of waves that end apart; tiles
+@pytest.mark.parametrize("M", [1, 13, 20, 64, 200, 700])
+@pytest.mark.parametrize("K,group", [(8, 32), (136, 32), (264, 64), (392, 128), (4232, 128)])
+def test_gemm_w4_infinite_scales(bolt, M, K, group):
+    """All values above zero, so an infinite scale anywhere in a row gives infinity: zeros that stand for missing steps must not meet it."""
+    N = 72
+    g = _gen(M + K)
+    groups = -(-K // group)
+    q = torch.randint(1, 16, (1, N, K // 2, 2), dtype=torch.uint8, device="cuda", generator=g)
+    q = q[..., 0] | q[..., 1] << 4
+    s = torch.full((1, N, groups), 2.0 ** -8, dtype=torch.float16, device="cuda")
+    z = torch.zeros((1, N, groups), dtype=torch.uint8, device="cuda")
+    s[0, 3, 0], s[0, 40, groups - 1], s[0, 71, groups // 2] = float("inf"), float("inf"), float("inf")
+    packed = torch.empty(bolt.bolt_w4_packed_bytes(N, K, group), dtype=torch.uint8, device="cuda")
+    bolt.bolt_w4_pack(N, K, group, q, s, z, packed)
+    A = torch.rand((M, K), device="cuda", generator=g).half() * 0.1 + 0.01
+    got = _gemm(bolt, bolt.gemm_w4_desc(M, N, K, group), A, packed)
+    spoiled = torch.zeros(N, dtype=torch.bool, device="cuda")
+    spoiled[[3, 40, 71]] = True
+    assert (got[:, spoiled] == float("inf")).all() and torch.isfinite(got[:, ~spoiled]).all()
+
+
+# ---- experts ------------------------------------------------------------------------------------------------------------------
+# few rows (walks; deep reductions, D = 2120), some ten rows with two sets of waves (5 and 3 steps), tiles of 64 rows
+@pytest.mark.parametrize("T", [2, 40, 500])
+@pytest.mark.parametrize("D,F", [(8, 8), (72, 136), (264, 136), (2120, 2120)])
+@pytest.mark.parametrize("where", ["up", "down"])
+def test_experts_infinite_weights(bolt, T, D, F, where):
+    """All values above zero, so an infinite weight of the first columns, or of the last, gives infinity in its outputs."""
+    E, k = 4, 2
+    g = _gen(T + D)
+    above = lambda *s, top: (torch.rand(s, device="cuda", generator=g) * top).half() + 2.0 ** -12
+    x, up, down = above(T, D, top=0.1), above(E, F, D, top=0.05), above(E, D, F, top=0.05)
+    ids = torch.stack((torch.randint(0, 3, (T,), device="cuda", generator=g), torch.full((T,), 3, device="cuda")), 1).int()
+    weights = torch.full((T, k), 0.5, device="cuda")
+    offsets, order = (t.cuda() for t in ref.lists(ids, E))
+    held = up if where == "up" else down
+    held[0, 5, 0], held[1, 2, held.shape[2] - 1], held[2, 0, min(33, held.shape[2] - 2)] = float("inf"), float("inf"), float("inf")
+    d = bolt.moe_desc(T, E, k, D, F, act="relu", gated=False)
+    y = bolt.bolt_moe_experts(d, x, up, None, down, None, ids, weights, offsets, order, torch.empty((T, D), dtype=torch.float16, device="cuda"),
+                              torch.empty(bolt.bolt_moe_workspace_bytes(d), dtype=torch.uint8, device="cuda"))
+    want, _ = ref.experts(x, lambda e: up[e].double(), None, lambda e: down[e].double(), None, ids, weights, "relu", False)
+    assert not torch.isnan(want).any() and torch.isinf(want).any()
+    assert torch.equal(torch.isposinf(y), torch.isposinf(want)) and not torch.isnan(y).any()
