@@ -46,8 +46,8 @@ __device__ __forceinline__ float route_exp(float x) {
   return p + p * (lo * 0.69314718055994530942f);
 }
 __device__ __forceinline__ float route_sigmoid(float x) {
-  // exp(-x) overflows below -88: the score is zero there; the quotient is the hardware's correctly rounded division
-  return x < -88.f ? 0.f : 1.f / (1.f + route_exp(-x));
+  // exp(-x) overflows below -88.7228: the score is zero there; the quotient is the hardware's correctly rounded division
+  return x < -88.72f ? 0.f : 1.f / (1.f + route_exp(-x));
 }
 
 struct MaxU { __device__ __forceinline__ unsigned operator()(unsigned a, unsigned b) const { return a > b ? a : b; } };

@@ -134,3 +134,18 @@ def test_experts_infinite_weights(bolt, T, D, F, where):
     want, _ = ref.experts(x, lambda e: up[e].double(), None, lambda e: down[e].double(), None, ids, weights, "relu", False)
     assert not torch.isnan(want).any() and torch.isinf(want).any()
     assert torch.equal(torch.isposinf(y), torch.isposinf(want)) and not torch.isnan(y).any()
+
+
+# ---- routing ------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("T", [3, 40, 300])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_route_sigmoid_scores_next_to_the_smallest(bolt, T, dtype):
+    """1 / (1 + exp(-x)) is a number in 32 bits down to x = -88.72 (denormal from -87.3 on): equal ones share the weight, and none is
+    left below."""
+    from test_gpu_llm import _route
+    logits = torch.full((T, 24), -88.5, dtype=dtype)  # (exact in a half)
+    logits[1] = -89.0
+    ids, w, _, _, _, _, _ = _route(bolt, logits, 4, score="sigmoid")
+    assert (ids == torch.arange(4)).all()
+    keep = [i for i in range(T) if i != 1]
+    assert (w[keep] - 0.25).abs().max() <= 1e-6 and (w[1] == 0).all()
