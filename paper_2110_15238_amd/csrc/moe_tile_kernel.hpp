@@ -19,8 +19,8 @@ namespace bolt {
 template <int ROWS, int BK, int NW>
 struct ListedRowsLoader {
   static constexpr int CH = BK / 8, RPI = 64 / CH, ALL = ROWS / RPI;  // ALL: instructions of a tile
-  static constexpr int NI = ALL > NW ? ALL / NW : 1;                  // of a wave (few rows: waves past the last load nothing)
-  static_assert(BK == 64 && (ALL % NW == 0 || ALL < NW) && NW % 2 == 0, "as DmaTileLoader");
+  static constexpr int NI = ALL / NW;                                 // of a wave
+  static_assert(BK == 64 && ALL % NW == 0 && NW % 2 == 0, "every wave loads as many pieces, which the main loop's waits count");
   __amdgpu_buffer_rsrc_t rsrc;
   unsigned at[NI];  // kInvalidOffset for rows that do not exist
   int lc, wave, K;
@@ -33,14 +33,13 @@ struct ListedRowsLoader {
     const int lrow = lane / CH;
     lc = (lane % CH) ^ dma_swizzle<BK>(wave * RPI + lrow);
 #pragma unroll
-    for (int j = 0; j < NI; ++j) at[j] = ALL < NW && wave >= ALL ? kInvalidOffset : offset_of((j * NW + wave) * RPI + lrow);
+    for (int j = 0; j < NI; ++j) at[j] = offset_of((j * NW + wave) * RPI + lrow);
   }
   template <int J0, int J1>
   __device__ __forceinline__ void issue_part(int kt, half_t* dst, const ConvGeom&) {
     const int k = kt * BK + lc * 8;
 #pragma unroll
     for (int j = J0; j < J1; ++j) {
-      if (ALL < NW && wave >= ALL) return;
       const unsigned off = k < K ? at[j] + (unsigned)k * 2u : kInvalidOffset;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, BOLT_LDS_PTR(dst + (j * NW + wave) * RPI * BK), 16, off, 0, 0, 0);
     }
