@@ -5,7 +5,7 @@ import math
 import pytest
 
 import llm_ref as ref
-from test_gpu_llm import _gen, _half, _matrix, _w4, _within, bolt  # noqa: F401  (the fixture among them)
+from test_gpu_llm import _check_route, _gen, _half, _matrix, _route, _run_experts, _w4, _within, bolt  # noqa: F401  (the fixture among them)
 
 pytestmark = pytest.mark.gpu
 
@@ -112,6 +112,35 @@ def test_gemm_w4_infinite_scales(bolt, M, K, group):
     assert (got[:, spoiled] == float("inf")).all() and torch.isfinite(got[:, ~spoiled]).all()
 
 
+# tiles of 64 x 128 and of 128 x 256, which fewer than 512 rows take from some thousand outputs on; ragged rows, columns and last steps
+LARGE_TILES = [(100, 12296, 72), (333, 8200, 520), (400, 8200, 1032), (333, 12296, 520), (500, 8200, 1096), (411, 12296, 72)]
+
+
+@pytest.mark.parametrize("M,N,K", LARGE_TILES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros,act", [(True, "none"), (False, "silu")])
+def test_gemm_w4_large_tiles(bolt, M, N, K, group, zeros, act):
+    g = _gen(M + K)
+    raw, packed = _w4(bolt, g, 1, N, K, group, zeros)
+    A, bias = _half(g, M, K), _half(g, N) if zeros else None
+    d = bolt.gemm_w4_desc(M, N, K, group, act=act, alpha=0.5, beta=-2.0)
+    assert bolt.bolt_gemm_w4_workspace_bytes(d) == 0  # (not unpacked)
+    _within(_gemm(bolt, d, A, packed, bias), *ref.linear(A.double(), _matrix(raw, group), None if bias is None else bias.double(), act, 0.5, -2.0))
+
+
+@pytest.mark.parametrize("M,N,K", [*LARGE_TILES, (13, 72, 4104), (100, 72, 4104), (700, 72, 4104), (40, 4104, 4232)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_gemm_w4_is_exact_on_integers_in_large_tiles_and_deep_layers(bolt, M, N, K, group):
+    """Every product and sum is exact on the weights as they are, so a value in a wrong place or a lost column shows."""
+    g = _gen(M + K)
+    raw, packed = _w4(bolt, g, 1, N, K, group, True, ones=True)
+    A = torch.randint(-1, 2, (M, K), device="cuda", generator=g).half() * (torch.randint(0, 4, (M, K), device="cuda", generator=g) == 0)
+    d = bolt.gemm_w4_desc(M, N, K, group)
+    assert bolt.bolt_gemm_w4_workspace_bytes(d) == 0
+    want = A.double() @ _matrix(raw, group).t().contiguous()
+    assert want.abs().max() <= 2048 and torch.equal(_gemm(bolt, d, A, packed).double(), want)
+
+
 # ---- experts ------------------------------------------------------------------------------------------------------------------
 # few rows (walks; deep reductions, D = 2120), some ten rows with two sets of waves (5 and 3 steps), tiles of 64 rows
 @pytest.mark.parametrize("T", [2, 40, 500])
@@ -136,16 +165,123 @@ def test_experts_infinite_weights(bolt, T, D, F, where):
     assert torch.equal(torch.isposinf(y), torch.isposinf(want)) and not torch.isnan(y).any()
 
 
+@pytest.mark.parametrize("T,E,k,D,F", [(900, 4, 2, 2056, 1032), (1300, 6, 3, 1032, 2056), (2100, 4, 1, 4104, 520)])
+@pytest.mark.parametrize("gated,act,bias", [(True, "silu", False), (False, "relu", True)])
+@pytest.mark.parametrize("group", [32, 64])
+def test_experts_many_rows_of_4_bits(bolt, T, E, k, D, F, gated, act, bias, group):
+    """Tiles of 64 x 128 and 128 x 256 with several groups in a step."""
+    _run_experts(bolt, T, E, k, D, F, act, gated, "w4", group, bias, 0.1, skew=0.5)
+
+
+@pytest.mark.parametrize("T,k", [(600, 2), (512, 1)])
+@pytest.mark.parametrize("kind", ["f16", "w4"])
+@pytest.mark.parametrize("gated", [True, False])
+def test_experts_rows_past_2_gib(bolt, T, k, kind, gated):
+    """x from 2 GiB on (a wide stride) runs on the kernel of few rows, many blocks of them per expert."""
+    assert T * (1 << 21) * 2 >= 1 << 31
+    _run_experts(bolt, T, 4, k, 72, 136, "silu", gated, kind, 64, True, 0.1, skew=1.0, ldx=1 << 21)
+
+
+@pytest.mark.parametrize("T", [3, 50])
+@pytest.mark.parametrize("kind", ["f16", "w4"])
+def test_experts_matrices_past_2_gib(bolt, T, kind):
+    """One expert's gate and value rows take 2 GiB as halves.  Small integers in the first and last hidden units and zeros between: exact."""
+    E, D, F, edge, group = 2, 1024, 1 << 19, 100, 128
+    g = _gen(T)
+    units = torch.cat((torch.arange(edge), torch.arange(F - edge, F))).cuda()
+    x = (torch.randint(0, 24, (T, D), device="cuda", generator=g) == 0).half()
+    small = (torch.randint(0, 12, (E, 4 * edge, D), device="cuda", generator=g) == 0).half()  # gate rows, then value rows
+    back = torch.randint(-1, 2, (E, D, 2 * edge), device="cuda", generator=g).half()
+    up, down = torch.zeros((E, 2 * F, D), dtype=torch.float16, device="cuda"), torch.zeros((E, D, F), dtype=torch.float16, device="cuda")
+    up[:, torch.cat((units, F + units))], down[:, :, units] = small, back
+
+    def pack(w):
+        q = torch.empty((*w.shape[:2], w.shape[2] // 2), dtype=torch.uint8, device="cuda")
+        for e in range(E):
+            v = (w[e] + 8).to(torch.uint8)
+            q[e] = v[:, 0::2] | v[:, 1::2] << 4
+        packed = torch.empty(bolt.bolt_w4_packed_bytes(w.shape[1], w.shape[2], group, E), dtype=torch.uint8, device="cuda")
+        ones = torch.ones((E, w.shape[1], w.shape[2] // group), dtype=torch.float16, device="cuda")
+        return bolt.bolt_w4_pack(w.shape[1], w.shape[2], group, q, ones, None, packed)
+
+    if kind == "w4":
+        up, down = pack(up), pack(down)
+    ids = torch.randint(0, E, (T, 1), device="cuda", generator=g).int()
+    ids[-1] = E - 1
+    offsets, order = (t.cuda() for t in ref.lists(ids, E))
+    d = bolt.moe_desc(T, E, 1, D, F, act="relu", gated=True, weights=kind, group=group)
+    y = bolt.bolt_moe_experts(d, x, up, None, down, None, ids, torch.ones((T, 1), device="cuda"), offsets, order,
+                              torch.empty((T, D), dtype=torch.float16, device="cuda"),
+                              torch.empty(bolt.bolt_moe_workspace_bytes(d), dtype=torch.uint8, device="cuda"))
+    want, _ = ref.experts(x, lambda e: small[e].double(), None, lambda e: back[e].double(), None, ids, torch.ones((T, 1), device="cuda"), "relu", True)
+    assert 0 < want.abs().max() <= 2048 and torch.equal(y.double(), want)
+
+
 # ---- routing ------------------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("T", [3, 40, 300])
 @pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
 def test_route_sigmoid_scores_next_to_the_smallest(bolt, T, dtype):
     """1 / (1 + exp(-x)) is a number in 32 bits down to x = -88.72 (denormal from -87.3 on): equal ones share the weight, and none is
     left below."""
-    from test_gpu_llm import _route
     logits = torch.full((T, 24), -88.5, dtype=dtype)  # (exact in a half)
     logits[1] = -89.0
     ids, w, _, _, _, _, _ = _route(bolt, logits, 4, score="sigmoid")
     assert (ids == torch.arange(4)).all()
     keep = [i for i in range(T) if i != 1]
     assert (w[keep] - 0.25).abs().max() <= 1e-6 and (w[1] == 0).all()
+
+
+ROUTES = [(64, 6, 1, 1), (200, 8, 8, 3), (256, 10, 1, 1), (48, 2, 4, 1), (500, 4, 10, 5), (16, 3, 16, 5)]
+
+
+@pytest.mark.parametrize("T", [1, 17, 64, 300, 8200])
+@pytest.mark.parametrize("E,k,groups,top_groups", ROUTES)
+@pytest.mark.parametrize("score,biased", [("sigmoid", False), ("sigmoid", True), ("softmax", True)])
+def test_route_half_logits(bolt, T, E, k, groups, top_groups, score, biased):
+    """FP16 logits where the tests beside it have FP32 ones: packed keys under sigmoid, and keys of score and bias."""
+    g = torch.Generator().manual_seed(T * E)
+    logits = (torch.randn(T, E, generator=g) * 1.5).half()
+    bias = torch.randn(E, generator=g) * (0.1 if score == "sigmoid" else 0.02) if biased else None
+    mask = (torch.rand(T, generator=g) > 0.2).to(torch.uint8) if T % 2 else None
+    got = _route(bolt, logits, k, bias=bias, mask=mask, score=score, groups=groups, top_groups=top_groups, renormalize=T != 300, scale=1.5)
+    _check_route(got, E, not biased and groups == 1)
+
+
+@pytest.mark.parametrize("T", [16385, 40000])
+@pytest.mark.parametrize("E,k,groups,top_groups,score,half,biased", [
+    (64, 8, 1, 1, "softmax", True, False), (128, 4, 1, 1, "softmax", True, False), (256, 8, 8, 4, "sigmoid", False, True),
+    (200, 6, 1, 1, "softmax", False, False), (100, 3, 1, 1, "sigmoid", True, False), (256, 8, 1, 1, "softmax", False, False)])
+def test_route_several_rounds(bolt, T, E, k, groups, top_groups, score, half, biased):
+    """More tokens than workgroups route at once: the next token's logits are requested ahead, whole pieces or one by one."""
+    g = torch.Generator().manual_seed(T + E)
+    logits = torch.randn(T, E, generator=g) * 1.5
+    bias = torch.randn(E, generator=g) * 0.1 if biased else None
+    mask = (torch.rand(T, generator=g) > 0.1).to(torch.uint8) if T % 2 else None
+    got = _route(bolt, logits.half() if half else logits, k, bias=bias, mask=mask, score=score, groups=groups, top_groups=top_groups)
+    _check_route(got, E, not biased and groups == 1)
+
+
+@pytest.mark.parametrize("T", [6, 40, 300])
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("biased", [True, False])
+@pytest.mark.parametrize("groups,top_groups", [(1, 1), (5, 2)])
+def test_route_rows_of_nothing_in_either_type(bolt, T, half, score, biased, groups, top_groups):
+    """Minus infinity, the type's lowest value, NaN, one live expert, plus infinity: a choice and finite weights, with a bias and groups too."""
+    E, inf, dtype = 40, float("inf"), torch.float16 if half else torch.float32
+    g = torch.Generator().manual_seed(2)
+    logits = torch.randn(T, E, generator=g).to(dtype)
+    logits[0], logits[1], logits[2] = -inf, torch.finfo(dtype).min, float("nan")
+    logits[3] = -inf
+    logits[3, 17] = 0.25
+    logits[4, 9], logits[4, 10] = inf, inf
+    logits[5, ::2] = float("nan")
+    bias = torch.linspace(0.3, 0.0, E) if biased else None
+    ids, w, offsets, order, want_ids, want_w, gap = _route(bolt, logits, 3, bias=bias, score=score, groups=groups, top_groups=top_groups)
+    held = torch.tensor([0, 1, 2, 3])  # (places that hang on rounding are none of these rows')
+    assert torch.equal(ids[held], want_ids[held]) and torch.isfinite(w).all()
+    sure = gap > 1e-5
+    assert torch.equal(ids[sure], want_ids[sure]) and (w[sure].double() - want_w[sure]).abs().max() <= 1e-5
+    assert ids[0].tolist() == [0, 1, 2] and ids[2].tolist() == [0, 1, 2] and ids[4, 0] == 9
+    o, r = ref.lists(ids, E)
+    assert torch.equal(offsets, o) and torch.equal(order, r)
