@@ -122,10 +122,11 @@ struct RowsWave {
         out.part[s][b] = in ? v : half8{0, 0, 0, 0, 0, 0, 0, 0};
       }
   }
-  // RAGGED: step `step` may end beyond column K or not exist.  What was read in place of its weights meets zero activations, and is zero here, as an
-  // infinite one would make a NaN of that: FP16 weights, the scales of 4-bit ones.
+  // RAGGED: step `step` may end beyond column K or not exist.  What was read in place of its weights meets zero activations, of which an infinite
+  // weight or scale would make a NaN: FP16 weights are zero there, a step of 4-bit ones that does not exist is left out.
   template <bool RAGGED>
   __device__ __forceinline__ void multiply(int step, const Weights& w, const Rows& x, floatx4 (&acc)[R][MB]) const {
+    if (RAGGED && WT == WEIGHTS_W4 && step >= p.steps) return;
 #pragma unroll
     for (int t = 0; t < R; ++t) {
       if constexpr (WT == WEIGHTS_W4) {
@@ -142,7 +143,7 @@ struct RowsWave {
 #pragma unroll
             for (int b = 0; b < MB; ++b) sum[b] = mfma_16x16x32(a, x.part[s][b], sum[b]);
           }
-          const half4 scale = !RAGGED || step < p.steps ? w.scale[t][i] : half4{0, 0, 0, 0};
+          const half4 scale = w.scale[t][i];
 #pragma unroll
           for (int b = 0; b < MB; ++b)
 #pragma unroll
