@@ -10,7 +10,10 @@ static hipError_t launch(const RowsParams& p, hipStream_t stream) {
   const int n = (p.steps + 7) / 8;     // steps of a wave
   if (n == 1) return launch_few_rows_walk<WEIGHTS_W4, MODE, GATED, NG, 2, 8, 1>(p, stream);
   if (n == 2) return launch_few_rows_walk<WEIGHTS_W4, MODE, GATED, NG, 2, 8, 2>(p, stream);
-  if (n <= 4) return launch_few_rows_walk<WEIGHTS_W4, MODE, GATED, NG, R4, 8, 4>(p, stream);
+  // (four steps of two tiles with groups of 32 do not fit the registers: one token, 8 of 64 experts of 2560 x 1024, gated, 33 us walking
+  // with 228 bytes a lane spilled, 21 with the sets of the deep kernel; 2 of 8 experts of 4096 x 4096 40 and 24)
+  if constexpr (!(GATED && NG == 4))
+    if (n <= 4) return launch_few_rows_walk<WEIGHTS_W4, MODE, GATED, NG, R4, 8, 4>(p, stream);
   if constexpr (MODE == ROWS_DENSE) {
     // us for 1 and 16 rows, tiles of 16 weight rows on 8 waves / of 32 on 16: 2048 x 8192 6.1 and 10.9 / 7.9 and 12.4, 4096 x 6000 6.4 and 8.7 /
     // 7.9 and 9.6, 6152 x 5000 (385 tiles of 16) 7.8 and 10.8 / 6.7 and 8.1, 12288 x 5000 10.9 and 14.9 / 11.8 and 14.4

@@ -109,3 +109,20 @@ def test_workspace_of_the_4_bit_layer_does_not_fall_as_rows_grow(bolt, N, K, gro
 
 def test_weights_of_2_gib_are_not_unpacked(bolt):
     assert bolt.bolt_gemm_w4_workspace_bytes(bolt.gemm_w4_desc(4096, 1 << 15, 1 << 15, 128)) == 0
+
+
+def test_kernels_keep_their_working_set_in_registers():
+    """The compiler's report of the build: no kernel of these operators spills, but for the persistent one of many rows, which may outside its k
+    loop (44 to 84 bytes a lane).  Skipped where only the built library was shipped."""
+    build = os.path.join(ROOT, "paper_2110_15238_amd", "csrc", "_build")
+    if not os.path.exists(build):
+        pytest.skip("no build directory (library shipped pre-built)")
+    seen = set()
+    for name in ("inst_few_rows_f16", "inst_few_rows_w4", "inst_shared_rows_f16", "inst_shared_rows_w4", "inst_moe_tile", "moe_api"):
+        found = re.findall(r"Function Name: (\S+)\s+VGPRs: \d+\s+ScratchSize \[bytes/lane\]: (\d+)", open(os.path.join(build, name + ".usage")).read())
+        assert found
+        for kernel, scratch in found:
+            seen.add(kernel)
+            assert int(scratch) <= (128 if "moe_pp_kernel" in kernel else 0), (kernel, scratch)
+    for family in ("few_rows_kernel", "few_rows_walk_kernel", "shared_rows_kernel", "moe_tile_kernel", "moe_pp_kernel", "moe_route_kernel"):
+        assert any(family in k for k in seen), family
