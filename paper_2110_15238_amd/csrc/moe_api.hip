@@ -289,20 +289,20 @@ bolt_gemm_desc unpacked_desc(const bolt_gemm_w4_desc& d) {
 }
 // Unpacking, a GEMM on FP16 operands, by the estimate of the GEMM's own kernel, and the launch that looks for marked weights, against the
 // best tile on packed ones.  SiLU has one kernel there, 256 x 256 tiles, and an estimate of its own (a fit to the same sizes).  us on packed
-// weights / unpacked / unpacked with SiLU, groups of 128: 2048 rows of 256 x 8192 23 / 34 / 138; 512 of 1024 x 12288 31 / 51 / 202; 1536
-// of 4096 x 4096 68 / 68 / 92; 4096 of 4096 x 4096 149 / 119 / 123.  Over 221 sizes (256 to 12288 outputs, K 512 to 12288, 512 to 8192
-// rows) with groups of 32 and 128 the choice takes 1.01 times the faster side (1.36 at most; packed ones everywhere 1.09 and 1.77), with
-// SiLU 1.004 (1.23; 1.03 and 1.29).
+// weights / unpacked / unpacked with SiLU, groups of 128: 2048 rows of 256 x 8192 23 / 30 / 133; 512 of 1024 x 12288 32 / 47 / 196; 1536
+// of 4096 x 4096 67 / 64 / 84; 4096 of 4096 x 4096 142 / 114 / 119.  Over 221 sizes (256 to 12288 outputs, K 512 to 12288, 512 to 8192
+// rows) with groups of 32 and 128 the choice takes 1.014 times the faster side (1.31 at most; packed ones everywhere 1.11 and 1.85), with
+// SiLU 1.005 (1.23; 1.03 and 1.31).
 bool dense_unpacks(const bolt_gemm_w4_desc& d) {
   if (!dense_may_unpack(d.M, d.N, d.K)) return false;
   const int64_t steps = W4Format(d.N, d.K, d.group).steps;
   const double packed = dense_us(dense_tile(d.M, d.N, steps, d.group), d.M, d.N, steps, d.group), weights = (double)d.N * d.K * 1e-6;
   if (d.act == BOLT_ACT_SILU) {
     const double rounds = (double)blocks_of(blocks_of(d.M, 256) * blocks_of(d.N, 256), 256);
-    return 17.3 + 0.57 * weights + blocks_of(d.K, 64) * (rounds <= 1 ? 0.95 : 1.29 * rounds) + 0.79e-6 * d.M * d.N < packed;
+    return 13.0 + 0.57 * weights + blocks_of(d.K, 64) * (rounds <= 1 ? 0.95 : 1.29 * rounds) + 0.79e-6 * d.M * d.N < packed;
   }
   double gemm;
-  return launches(blocks_of(d.M, 32) * blocks_of(d.N, 32)) && estimate_gemm(unpacked_desc(d), &gemm) && 8.0 + 0.6 * weights + gemm < packed;
+  return launches(blocks_of(d.M, 32) * blocks_of(d.N, 32)) && estimate_gemm(unpacked_desc(d), &gemm) && 4.0 + 0.6 * weights + gemm < packed;
 }
 
 // ---- which kernels run the experts ------------------------------------------------------------------------------------
@@ -327,7 +327,9 @@ struct Choice {
 // 1 token 15 / 19 / 26; 4 tokens 27 / 23 / 26; 32 tokens 42 / 38 / 34 / 37; 128 tokens 67 / 53 / 45 / 49 / 53 / 68; 512 tokens 157 / 120 / 93 /
 // 77 / 90 / 131; 1024 tokens - / - / 162 / 127 / 127 / 143; 2048 tokens - / - / - / - / 246 / 225.  A tile that leaves compute units without a
 // workgroup gives way to the next smaller one: groups of 32, no gate, 968 wide, 3592 hidden, 350 tokens, 6 of 6 experts 144 by the rows alone, 114 so;
-// groups of 128, gated, 1264 wide, 4072 hidden, 1104 tokens, 3 of 4 experts 186 and 167.
+// groups of 128, gated, 1264 wide, 4072 hidden, 1104 tokens, 3 of 4 experts 186 and 167.  Over 108 sizes (9 shapes, 1 to 8192 tokens) the choice
+// takes 1.01 times the best tile for both products, 1.32 at most (4096 tokens, 4 of 16 experts, 512 x 512 without a gate: 103 / 69 / 59 / 65 / 78 by
+// 16 x 64 .. 128 x 256, which it takes).
 Choice choose_w4(const Spread& s, int weight_rows) {
   if (s.experts * blocks_of(weight_rows, 32) <= 512 && s.rows <= 16) return {Family::FEW, {}, {}};
   const auto fills = [&](int rows, int cols) { return s.blocks(rows) * blocks_of(weight_rows, cols) >= 256; };
@@ -343,6 +345,10 @@ Choice choose_w4(const Spread& s, int weight_rows) {
 // 109; 512 tokens 183 / 183 / 117 / 140 / 122; 1024 tokens - / - / 142 / 151 / 182; 2048 tokens - / - / 238 / 214 / 189; 4096 tokens - / - / 398 / 348 /
 // 285; and 1000 wide, 2504 hidden, no gate, 8 experts, 2 per token: 64 tokens 31 / 31 / 47, 256 tokens - / 51 / 51 / 70 / 100, 1024 tokens - / - /
 // 90 / 84 / 114, 4096 tokens - / - / 221 / 200 / 160.
+// It does not look at the reduction's length.  Short ones, gated, 4 of 55 experts, 2000 wide, 464 hidden, 64 / 128 / 256 rows: 1024 tokens 130 / 136 /
+// 119, 2048 tokens 178 / 169 / 128, 4096 tokens 295 / 256 / 220, 8192 tokens 514 / 427 / 369; 5 of 9 experts, 448 x 424: 2048 tokens 44 / 43 / 48, 8192
+// tokens 145 / 123 / 117.  Over 108 sizes (9 shapes, 1 to 8192 tokens) the choice takes 1.03 times the best family for both products, 1.39 at
+// most (the 2048 tokens above).
 Choice choose_f16(const Spread& s, int weight_rows, bool offsets_fit) {
   if (s.rows <= 10 || !offsets_fit) return {Family::FEW, {}, {}};
   if (s.rows >= 192 && s.blocks(256) * blocks_of(weight_rows, 256) >= 144) return {Family::MANY, {}, ManyTile::ROWS256};
