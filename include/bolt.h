@@ -385,7 +385,8 @@ typedef enum { BOLT_WEIGHTS_F16 = 0, BOLT_WEIGHTS_W4 = 1 } bolt_weights;
  *   u = x[t] . w_up[e]^T + b_up[e];  h = act(u), or with `gated` act(u[0 : hidden]) * u[hidden : 2 hidden];
  *   expert(x) = h . w_down[e]^T + b_down[e].
  * x of 2 GiB and more, or an expert's matrix of that size, runs on the kernel for few rows, and is BOLT_ERR_UNSUPPORTED where that would
- * take 2^32 threads.  h is rounded to FP16 (the next product's operand); a slot's row and the weighted sum over slots are FP32. */
+ * take 2^32 threads.  h is rounded to FP16 (the next product's operand; infinite beyond 65504); a slot's row and the weighted sum over slots
+ * are FP32. */
 typedef struct {
   int32_t tokens, experts, top_k;
   int32_t width, hidden; /* multiples of 8 */

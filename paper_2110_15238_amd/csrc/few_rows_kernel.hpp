@@ -10,8 +10,8 @@
 //   and is scaled there, so neither scale nor zero point costs accuracy.  (Nine vector instructions make eight operands.)
 //   Activation rows beyond the last repeat the last: their columns of the result are not stored.  Columns beyond K are zero on
 //   both sides.
-// Measured: 4096 x 4096 in 4 bits, one row, 4.2 us (8.7 MB); 6152 x 5000, 13 rows, 7.7 us (17 MB); one token's 8 experts in FP16, 2048 x 1024:
-// 16.8 us for 67 MB of gate and value rows (4.0 TB/s; a large copy moves 5.15), 8 us for 34 MB behind them.
+// Measured: 4096 x 4096 in 4 bits, one row, 4.2 us (8.7 MB); 6152 x 5000, 13 rows, 7.3 us (17 MB); one token's 8 experts in FP16, 2048 x 1024:
+// 16.3 us for 67 MB of gate and value rows (4.1 TB/s; a large copy moves 5.15), 8.5 us for 34 MB behind them.
 #pragma once
 #include "routed_rows.hpp"
 #include "w4_format.hpp"
@@ -188,7 +188,7 @@ struct RowsWave {
       const int j = b * 16 + (at & 15), col = col0 + t * 16 + (at >> 4) * 4;
       if (j >= rows || col >= outputs) continue;
       floatx4 v = with_bias(sum_of(GATED ? 2 * t : t, b, at), col);
-v = apply_act4(v, p.act);
+      v = apply_act4(v, p.act);
       if constexpr (GATED) v *= with_bias(sum_of(2 * t + 1, b, at), p.hidden + col);
       if constexpr (MODE == ROWS_DOWN) {
         *(floatx4*)((float*)p.y + (int64_t)p.order[row0 + j] * p.ldy + col) = v;

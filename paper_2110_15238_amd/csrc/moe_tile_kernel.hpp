@@ -7,9 +7,11 @@
 //   UP: the activation rows are gathered by the loader (one byte offset per row and lane, as for a convolution's pixels); with a gate the
 //       weight tile alternates 32 gate rows and the 32 value rows of the same columns, so that a lane holds both factors of an output.
 //   DOWN: the rows lie in the list's order; results leave in FP32, to the slot's row.
-// What bounds it: a round trip to memory per step of the reduction that the stages do not cover (700 tokens to 2 of 8 experts, 1000 wide, 2504
-// hidden, 64 x 128 tiles: 25 us up, 31 us down, 0.75 us a step; two stages 26 and 40, four or six no better, two sets of waves that split the
-// reduction 31 and 30).
+// What bounds it: a workgroup's own chain of steps, where there is one workgroup for each compute unit.  1000 wide, 2504 hidden, 158 rows for each
+// expert, 64 x 128 tiles, the down product's 40 steps: 17.5 us with 24 tiles on the chip, 19 with 96, 22 with 240 (0.37 to 0.46 us a step, of which the
+// matrix instructions are 0.11; operands from the caches, 9 TB/s with 240 tiles), so neither bandwidth nor the L2s; 37 with 384 tiles, which are two
+// rounds.  Weights that no cache holds add to a step (700 tokens to 2 of 8 experts: 22 and 23 us up and down on the same weights again and again, 25 and
+// 31 on changing ones).  Two stages are slower (26 and 40 there), four or six no better, two sets of waves that split the reduction 31 and 30.
 #pragma once
 #include "routed_rows.hpp"
 
@@ -149,7 +151,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void moe_tile_kernel(const 
 #pragma unroll
         for (int b = 0; b < FM; ++b) {
           floatx4 v = value(GATED ? 2 * a : a, b, q);
-v = apply_act4(v, p.act);
+          v = apply_act4(v, p.act);
           if constexpr (GATED) v *= value(2 * a + 1, b, q);
           half4 o;
 #pragma unroll

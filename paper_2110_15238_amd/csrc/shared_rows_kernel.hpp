@@ -9,9 +9,9 @@
 // fixed order.  One barrier per step.
 // What bounds it: of few rows the instructions of a step (decoding, LDS reads, matrix instructions one behind the other), which several
 // workgroups per compute unit cover for each other, so tiles are small; of many rows LDS reads, decoding and matrix instructions are
-// about equally long and overlap in part.  Measured in 4 bits: 29 tokens to 8 of 128 experts 2048 x 768, 32 us for 165 MB of gate and value rows
-// (5 TB/s) and 22 us for the 83 MB behind; 3001 tokens to 4 of 32 experts 1536 x 1280, 154 and 93 us (600 and 500 TFLOP/s); 100 x 8192 x 2048
-// 11.1 us.  More stages than three cost resident workgroups and are slower (the first 64 us: 75 with four); so are 4 tiles of weight rows
+// about equally long and overlap in part.  Measured in 4 bits: 29 tokens to 8 of 128 experts 2048 x 768, 29 to 32 us for 165 MB of gate and value rows
+// (5 TB/s and more) and 19 to 22 us for the 83 MB behind; 3001 tokens to 4 of 32 experts 1536 x 1280, 154 and 93 us (600 and 500 TFLOP/s); 100 x 8192 x 2048
+// 9.9 to 10.3 us.  More stages than three cost resident workgroups and are slower (the first 64 us: 75 with four); so are 4 tiles of weight rows
 // per wave, which leave one wave per SIMD (64 x 256 tiles, 265 -> 346 us for the second).
 #pragma once
 #include "few_rows_kernel.hpp"
@@ -197,7 +197,7 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
         return v;
       };
       floatx4 v = with_bias(acc[a][b], col);
-v = apply_act4(v, p.act);
+      v = apply_act4(v, p.act);
       if constexpr (GATED) v *= with_bias(acc[a + 1][b], p.hidden + col);
       if constexpr (MODE == ROWS_DOWN) {
         *(floatx4*)((float*)p.y + to * p.ldy + col) = v;
