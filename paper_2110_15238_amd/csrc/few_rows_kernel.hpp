@@ -41,6 +41,8 @@ struct RowsWave {
   int lane, g, l16, expert, row0, rows;
   const half_t* xrow[MB];
   const unsigned char* wrow[R];
+  __amdgpu_buffer_rsrc_t wtile[R];  // FP16: the rows of a tile, and this lane's place in them
+  unsigned wlane[R];
   const half_t* scale_at[R];
   const unsigned char* zero_at[R];
 
@@ -83,11 +85,14 @@ struct RowsWave {
         zero_at[t] = p.zeros + scales + ((int64_t)(row >> 4) * p.steps * 16 + (row & 15)) * NG;
       } else {
         wrow[t] = w + ((int64_t)row * p.K + g * 8) * 2;
+        const int base = first < last ? first : last;
+        wtile[t] = make_rsrc(w + (int64_t)base * p.K * 2, (unsigned)(16 * p.K * 2));  // (K <= 2^21)
+        wlane[t] = (unsigned)(((row - base) * p.K + g * 8) * 2);
       }
     }
   }
-  // Step `step` of the weights.  4-bit weights are padded to whole steps.  FP16, RAGGED: beyond column K a lane reads its row's first
-  // columns instead.
+  // Step `step` of the weights.  4-bit weights are padded to whole steps.  FP16, RAGGED: columns beyond K are zero (the buffer's range; through
+  // one for whole steps too the deep kernel takes 145 registers for 100, and two of 16 experts of 4096 x 2560 99.6 us for 90.7).
   template <bool RAGGED>
   __device__ __forceinline__ void load_weights(int step, Weights& out) const {
 #pragma unroll
@@ -105,7 +110,12 @@ struct RowsWave {
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
           const int k = step * STEP + s * 32;
-          out.piece[t][s] = *(const uintx4*)(wrow[t] + (int64_t)(RAGGED && k + g * 8 >= p.K ? -g * 8 : k) * 2);
+          if constexpr (RAGGED) {
+            const unsigned at = k + g * 8 < p.K ? wlane[t] : kInvalidOffset;
+            out.piece[t][s] = __builtin_bit_cast(uintx4, __builtin_amdgcn_raw_buffer_load_b128(wtile[t], at, k * 2, 0));
+          } else {
+            out.piece[t][s] = *(const uintx4*)(wrow[t] + (int64_t)k * 2);
+          }
         }
       }
     }
@@ -122,8 +132,8 @@ struct RowsWave {
         out.part[s][b] = in ? v : half8{0, 0, 0, 0, 0, 0, 0, 0};
       }
   }
-  // RAGGED: step `step` may end beyond column K or not exist.  What was read in place of its weights meets zero activations, of which an infinite
-  // weight or scale would make a NaN: FP16 weights are zero there, a step of 4-bit ones that does not exist is left out.
+  // RAGGED: step `step` may not exist; of 4-bit weights another's were read for it then, and it is left out (a scale may be infinite, and would
+  // make a NaN of the zero activations).
   template <bool RAGGED>
   __device__ __forceinline__ void multiply(int step, const Weights& w, const Rows& x, floatx4 (&acc)[R][MB]) const {
     if (RAGGED && WT == WEIGHTS_W4 && step >= p.steps) return;
@@ -151,11 +161,9 @@ struct RowsWave {
         }
       } else {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          const uintx4 a = !RAGGED || step * STEP + s * 32 + g * 8 < p.K ? w.piece[t][s] : uintx4{0, 0, 0, 0};
+        for (int s = 0; s < KS; ++s)
 #pragma unroll
-          for (int b = 0; b < MB; ++b) acc[t][b] = mfma_16x16x32(__builtin_bit_cast(half8, a), x.part[s][b], acc[t][b]);
-        }
+          for (int b = 0; b < MB; ++b) acc[t][b] = mfma_16x16x32(__builtin_bit_cast(half8, w.piece[t][s]), x.part[s][b], acc[t][b]);
       }
     }
   }
@@ -271,9 +279,8 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
 // Reductions of at most NX steps per wave: the wave's share of the activations stays in registers while the workgroup walks over
 // p.walk tiles of columns.  The weights of the next tile are on their way while a tile is multiplied, summed and stored, so the
 // cost of finding the rows and of the first round trip to memory is paid once per walk, and the waves' sums have two places, so one
-// barrier per tile is enough.  FULL: every wave has NX whole steps; else steps that a wave does not have read the last one again and meet
-// zeros (one token, 8 experts of 2048 x 1024 in FP16, both products and the sum: 28.7 us, and 29.7 so).
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX, bool FULL>
+// barrier per tile is enough.  Steps that a wave does not have meet zero activations; their FP16 weights are zero, 4-bit ones are left out.
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
 __global__ __launch_bounds__(64 * NW) void few_rows_walk_kernel(const RowsParams p) {
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int PART = NW * R * 64 * 4;
@@ -300,18 +307,18 @@ __global__ __launch_bounds__(64 * NW) void few_rows_walk_kernel(const RowsParams
     w.take_columns((cb + tile) * Wave::COLS);
     for_constants<NX>([&](auto i) {
       const int step = wave + decltype(i)::value * NW;
-      w.template load_weights<!FULL>(FULL || step < last_step ? step : last_step, wf[decltype(set)::value][decltype(i)::value]);
+      w.template load_weights<true>(WT == WEIGHTS_F16 || step < last_step ? step : last_step, wf[decltype(set)::value][decltype(i)::value]);
     });
   };
   using S0 = std::integral_constant<int, 0>;
   using S1 = std::integral_constant<int, 1>;
   load(0, S0{});
   w.take_rows();
-  for_constants<NX>([&](auto i) { w.template load_rows<!FULL>(wave + decltype(i)::value * NW, xf[decltype(i)::value]); });
+  for_constants<NX>([&](auto i) { w.template load_rows<true>(wave + decltype(i)::value * NW, xf[decltype(i)::value]); });
   auto tile = [&](int it, auto set) {
     floatx4 acc[R][1] = {};
     for_constants<NX>([&](auto i) {
-      w.template multiply<!FULL>(wave + decltype(i)::value * NW, wf[decltype(set)::value][decltype(i)::value], xf[decltype(i)::value], acc);
+      w.template multiply<true>(wave + decltype(i)::value * NW, wf[decltype(set)::value][decltype(i)::value], xf[decltype(i)::value], acc);
     });
     float* const mine = part + decltype(set)::value * PART;
     w.put_sums(mine, wave, acc);
@@ -346,9 +353,9 @@ hipError_t launch_few_rows(RowsParams p, hipStream_t stream) {
   hipLaunchKernelGGL(kern, dim3(p.row_blocks * p.col_blocks), dim3(64 * NW), LDS_BYTES, stream, p);
   return hipGetLastError();
 }
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX, bool FULL = false>
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
 hipError_t launch_few_rows_walk(RowsParams p, hipStream_t stream) {
-  auto kern = few_rows_walk_kernel<WT, MODE, GATED, NG, R, NW, NX, FULL>;
+  auto kern = few_rows_walk_kernel<WT, MODE, GATED, NG, R, NW, NX>;
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int LDS_BYTES = 2 * NW * R * 64 * 16;
   static LdsOptIn opt_in;

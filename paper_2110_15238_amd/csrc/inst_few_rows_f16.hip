@@ -3,16 +3,12 @@
 #include "few_rows_kernel.hpp"
 
 namespace bolt {
-template <int MODE, bool GATED, bool FULL>
-static hipError_t launch_walk(const RowsParams& p, int n, hipStream_t stream) {
-  if (n == 1) return launch_few_rows_walk<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 1, FULL>(p, stream);
-  if (n == 2) return launch_few_rows_walk<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 2, FULL>(p, stream);
-  return launch_few_rows_walk<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 4, FULL>(p, stream);
-}
 template <int MODE, bool GATED>
 static hipError_t launch(const RowsParams& p, hipStream_t stream) {
   const int n = (p.steps + 7) / 8;  // steps of a wave
-  if (n <= 4) return p.K % 512 == 0 && n != 3 ? launch_walk<MODE, GATED, true>(p, n, stream) : launch_walk<MODE, GATED, false>(p, n, stream);
+  if (n == 1) return launch_few_rows_walk<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 1>(p, stream);
+  if (n == 2) return launch_few_rows_walk<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 2>(p, stream);
+  if (n <= 4) return launch_few_rows_walk<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 4>(p, stream);
   return launch_few_rows<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 3>(p, stream);
 }
 hipError_t launch_few_rows_f16(const RowsParams& p, int mode, bool gated, hipStream_t stream) {
