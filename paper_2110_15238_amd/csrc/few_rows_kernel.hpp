@@ -280,8 +280,11 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
 // p.walk tiles of columns.  The weights of the next tile are on their way while a tile is multiplied, summed and stored, so the
 // cost of finding the rows and of the first round trip to memory is paid once per walk, and the waves' sums have two places, so one
 // barrier per tile is enough.  Steps that a wave does not have meet zero activations; their FP16 weights are zero, 4-bit ones are left out.
+// (Two workgroups of eight waves share a compute unit with up to 128 registers, which the routed kernels of one group a step and two steps just miss if
+// left alone: one token, 8 of 64 experts, 2048 x 2048, no gate, 20.9 us so and 17.7 held to 128; 3 tokens, 3 of 44 experts, 1560 x 664, gated, 14.6
+// and 13.7.  Linear layers would spill.)
 template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
-__global__ __launch_bounds__(64 * NW) void few_rows_walk_kernel(const RowsParams p) {
+__global__ __launch_bounds__(64 * NW, WT == WEIGHTS_W4 && MODE != ROWS_DENSE && NG == 1 && NX == 2 ? 4 : 1) void few_rows_walk_kernel(const RowsParams p) {
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int PART = NW * R * 64 * 4;
   extern __shared__ __attribute__((aligned(16))) float part[];  // [2][PART]
