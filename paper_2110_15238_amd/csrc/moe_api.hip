@@ -291,12 +291,13 @@ bolt_gemm_desc unpacked_desc(const bolt_gemm_w4_desc& d) {
 // best tile on packed ones.  SiLU has one kernel there, 256 x 256 tiles, and an estimate of its own (a fit to the same sizes).  us on packed
 // weights / unpacked / unpacked with SiLU, groups of 128: 2048 rows of 256 x 8192 23 / 30 / 133; 512 of 1024 x 12288 32 / 47 / 196; 1536
 // of 4096 x 4096 67 / 64 / 84; 4096 of 4096 x 4096 142 / 114 / 119.  Over 221 sizes (256 to 12288 outputs, K 512 to 12288, 512 to 8192
-// rows) with groups of 32 and 128 the choice takes 1.014 times the faster side (1.31 at most; packed ones everywhere 1.11 and 1.85), with
+// rows) with groups of 32 and 128 the choice takes 1.012 times the faster side (1.31 at most; packed ones everywhere 1.11 and 1.85), with
 // SiLU 1.005 (1.23; 1.03 and 1.31).
 bool dense_unpacks(const bolt_gemm_w4_desc& d) {
   if (!dense_may_unpack(d.M, d.N, d.K)) return false;
   const int64_t steps = W4Format(d.N, d.K, d.group).steps;
-  const double packed = dense_us(dense_tile(d.M, d.N, steps, d.group), d.M, d.N, steps, d.group), weights = (double)d.N * d.K * 1e-6;
+  // (the packed side's estimate is some 10 % low from a few hundred rows on)
+  const double packed = 1.1 * dense_us(dense_tile(d.M, d.N, steps, d.group), d.M, d.N, steps, d.group), weights = (double)d.N * d.K * 1e-6;
   if (d.act == BOLT_ACT_SILU) {
     const double rounds = (double)blocks_of(blocks_of(d.M, 256) * blocks_of(d.N, 256), 256);
     return 13.0 + 0.57 * weights + blocks_of(d.K, 64) * (rounds <= 1 ? 0.95 : 1.29 * rounds) + 0.79e-6 * d.M * d.N < packed;
