@@ -358,13 +358,14 @@ Choice choose_f16(const Spread& s, int weight_rows, bool offsets_fit) {
 }
 
 // Whether the launch of a product with N weight rows of K columns can be made; the number of row blocks is the host's bound of it.
-bool product_launches(const bolt_moe_desc& d, const Spread& s, int N, int K, bool offsets_fit) {
+bool product_launches(const bolt_moe_desc& d, const Spread& s, int N, int K, bool gate, bool offsets_fit) {
   const bool w4 = d.weights == BOLT_WEIGHTS_W4;
   const Choice c = w4 ? choose_w4(s, N) : choose_f16(s, N, offsets_fit);
   const int64_t slots = (int64_t)d.tokens * d.top_k, short_blocks = std::min<int64_t>(slots, d.experts);
   if (c.family == Family::FEW || !offsets_fit) {
     const int64_t blocks = slots / 16 + short_blocks;
-    const bool walks = blocks_of(K, w4 ? W4Format::STEP : 64) <= 32;  // (each row block once at least, some thousand workgroups otherwise)
+    // walks: each row block once at least, some thousand workgroups otherwise (csrc/inst_few_rows_*.hip)
+    const bool walks = blocks_of(K, w4 ? W4Format::STEP : 64) <= (w4 && gate && d.group == 32 ? 16 : 32);
     return launches(walks ? 2 * blocks + 2048 : blocks * blocks_of(N, 32));
   }
   if (c.family == Family::MANY && c.many == ManyTile::ROWS256) return true;  // (one workgroup per compute unit)
@@ -518,7 +519,8 @@ bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const voi
                            (int64_t)desc->width * desc->hidden * 2 <= most && (int64_t)256 * desc->hidden * 2 <= most;
   // (beyond them the kernel of few rows runs)
   const Spread spread(*desc);
-  if (!product_launches(*desc, spread, up_rows, desc->width, offsets_fit) || !product_launches(*desc, spread, desc->width, desc->hidden, offsets_fit))
+  if (!product_launches(*desc, spread, up_rows, desc->width, gated, offsets_fit) ||
+      !product_launches(*desc, spread, desc->width, desc->hidden, false, offsets_fit))
     return BOLT_ERR_UNSUPPORTED;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;

@@ -59,6 +59,12 @@ def test_launches_of_two_to_the_32_threads_are_refused(bolt):
     assert _experts(bolt, bolt.moe_desc(1 << 26, 16, 16, 8, 8, weights="w4", group=32)) == UNSUPPORTED
 
 
+@pytest.mark.parametrize("weights,group,width", [("f16", 0, 4096), ("w4", 128, 8192), ("w4", 32, 4096)])
+def test_many_rows_past_2_gib_are_refused_where_the_deep_kernel_would_take_2_to_the_32_threads(bolt, weights, group, width):
+    """The deep kernel of few rows has a workgroup for every 16 rows and 32 weight rows.  (Gated groups of 32 take it from 17 steps of 128 on.)"""
+    assert _experts(bolt, bolt.moe_desc(300000, 8, 8, width, 4096, weights=weights, group=group)) == UNSUPPORTED
+
+
 def test_addresses_of_device_variables_are_looked_up_for_each_device(tmp_path):
     """The zeros that stand for a missing bias lie elsewhere on every GPU of a process.  The lookup on the host alone, with made-up devices; and
     nothing in the library asks for such an address but through it."""
