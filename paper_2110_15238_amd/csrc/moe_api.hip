@@ -156,7 +156,7 @@ bolt_status status_of(hipError_t e) { return e == hipSuccess ? BOLT_OK : BOLT_ER
 constexpr int kMaxLength = 1 << 21;  // of a row, as in the other operators
 // Rows and slots: the kernels count them in 32 bits, as far as the end of the last workgroup's share and one stride past it.
 constexpr int64_t kMaxRows = (1ll << 31) - (1 << 16);
-// Threads of a launch: the runtime counts them in 32 bits, and no workgroup here has more than 512.
+// Threads of a launch: the runtime counts them in 32 bits.  No workgroup whose number grows with the rows has more than 512.
 bool launches(int64_t blocks) { return blocks <= UINT32_MAX / 512; }
 
 bolt_status check_w4_shape(int32_t N, int32_t K, int32_t group) {

@@ -10,8 +10,8 @@
 // Tiles run in bands of 8 row blocks of an expert, and an XCD's 32 workgroups walk neighbouring tiles: a band's rows stay in its L2 while
 // the expert's weights stream through.
 // Measured: 8192 tokens to 6 of 64 experts, 2048 x 1024, gated: up 400 to 470 us (880 to 1030 TFLOP/s of what was asked for, 1.18 times that with the
-// blocks' padding), down 280 to 310 us (670 to 740: 400 MB of FP32 rows leave it).  The matrix cores work 69 and 51 % of the cycles at 1.7 to 1.8 GHz,
-// the L2s miss 31 and 38 % of the requests.  No effect: tiles from a counter instead of dealt out (7.1 rounds take 8), wave groups
+// blocks' padding), down 280 to 310 us (670 to 740: 400 MB of FP32 rows leave it).  The matrix cores work 69 and 50 % of the cycles at 1.7 to 1.8 GHz,
+// the L2s miss 31 and 37 % of the requests.  No effect: tiles from a counter instead of dealt out (7.1 rounds take 8), wave groups
 // without rows that leave their MFMAs out, XCDs that start apart, rows stored from registers or through LDS.
 #pragma once
 #include <type_traits>
