@@ -405,6 +405,65 @@ bolt_status bolt_moe_experts(const bolt_moe_desc* desc, const void* x, const voi
                              size_t workspace_bytes, void* stream);
 size_t bolt_moe_workspace_bytes(const bolt_moe_desc* desc);
 
+/* ---- A projection shared by requests that each bring a low-rank adapter --------------------------------------------
+ *   D[m] = act(alpha * (A[m] . W^T + scales[a] * (A[m] . down[a]^T) . up[a]^T) + beta * bias),  a = ids[m];
+ * a row whose id is below zero, or no less than `adapters`, has no adapter and is A[m] . W^T alone.  scales[a] * (A[m] . down[a]^T) is rounded to
+ * FP16 (the next product's operand; infinite beyond 65504); beyond 16 rows the adapters' share of a row is rounded to FP16 once more before it
+ * is added.  An adapter's infinities and NaN reach its own rows only. */
+typedef struct {
+  int32_t M, N, K;
+  int32_t lda, ldd;       /* in elements; A and D are row-major */
+  int32_t weights;        /* bolt_weights of W */
+  int32_t group;          /* of 4-bit weights */
+  int32_t adapters, rank; /* rank: a multiple of 8, up to 128; adapters of lower rank are filled up with zeros */
+  float alpha, beta;
+  int32_t act;            /* bolt_act, not SiLU */
+} bolt_gemm_lora_desc;
+
+/* A: M x K (lda); W: N x K FP16, dense, or bolt_w4_pack(N, K, group, 1); bias: N halves or NULL; ids: M int32; down: [adapters][rank][K], up:
+ * [adapters][N][rank], FP16; scales: `adapters` floats or NULL (1); D: M x N (ldd), not A.  K, N, lda, ldd multiples of 8.  M may be 0. */
+bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const void* W, const void* bias, const void* ids, const void* down,
+                           const void* up, const void* scales, void* D, void* workspace, size_t workspace_bytes, void* stream);
+size_t bolt_gemm_lora_workspace_bytes(const bolt_gemm_lora_desc* desc);
+
+/* ---- Rows in 8 bits: the norm that writes them, the linear layer that reads them ----------------------------------
+ * 8 bits are E4M3 as the Open Compute Project defines it (no infinities, largest value 448), value = scale * q with an FP32 scale
+ * for every row. */
+
+/* v = x + residual, in FP32;  sum = v;  n = v / sqrt(mean(v^2) + eps) * (weight_offset + weight);  y = n;  scales[row] = max |n| / 448,
+ * q = n / scale, all from the unrounded v.  A row whose largest |n| is below 2^-118 has zeros for q.  A row that holds an infinity or a NaN has a NaN
+ * for its scale, and for all of its q.  Up to 2^31 - 65536 rows of up to 65536 values. */
+typedef struct {
+  int32_t rows, width;             /* width a multiple of 8 */
+  int32_t ldx, ldr, lds, ldy, ldq; /* row strides of x, residual, sum, y and q in elements, multiples of 8; of those that are not NULL */
+  float eps;                       /* >= 0 */
+  float weight_offset;             /* 0, or 1 for weights that are held as their distance from 1 */
+} bolt_rms_norm_desc;
+
+/* x: rows x width; residual: the same, or NULL (none); weight: `width` halves; outputs, each may be NULL, y or q not both: sum and y: rows x
+ * width FP16; q: rows x width bytes, scales: `rows` floats (with q).  One of sum and y may be x or the residual itself, with the same stride; buffers
+ * must not overlap otherwise.  rows may be 0. */
+bolt_status bolt_rms_norm(const bolt_rms_norm_desc* desc, const void* x, const void* residual, const void* weight, void* sum, void* y, void* q,
+                          void* scales, void* stream);
+
+/* Rows of FP16 values in 8 bits, without a norm: scales[row] = max |x| / 448, q = x / scale, with the limits and special rows of bolt_rms_norm
+ * (an infinity: infinite scale).  For activations that no norm precedes, and for weights [N][K], whose scales are then the columns' of the product. */
+bolt_status bolt_quantize_rows(int32_t rows, int32_t width, int32_t ldx, int32_t ldq, const void* x, void* q, void* scales, void* stream);
+
+/* D[m][n] = act(alpha * a_scales[m] * w_scales[n] * sum over k of A[m][k] * W[n][k] + beta * bias[n]), A and W in E4M3. */
+typedef struct {
+  int32_t M, N, K;
+  int32_t lda, ldd; /* in elements; A, W (N x K, dense) and D are row-major.  N, ldd multiples of 8, K, lda of 16 */
+  float alpha, beta;
+  int32_t act;      /* bolt_act, SiLU included */
+} bolt_gemm_q8_desc;
+
+/* A: M x K (lda) bytes, W: N x K bytes; a_scales: M floats, w_scales: N floats, 16-byte aligned, either may be NULL (1 everywhere); bias: N halves or
+ * NULL; D: M x N (ldd) FP16.  M may be 0.  The workspace is for sums that several workgroups share. */
+bolt_status bolt_gemm_q8(const bolt_gemm_q8_desc* desc, const void* A, const void* a_scales, const void* W, const void* w_scales, const void* bias, void* D,
+                         void* workspace, size_t workspace_bytes, void* stream);
+size_t bolt_gemm_q8_workspace_bytes(const bolt_gemm_q8_desc* desc);
+
 /* Measured roofline denominators: runs an MFMA-only loop of v_mfma_f32_16x16x32_f16 on pseudo-random FP16
  * operands, `iterations` x 16 instructions per wave, 8 waves per compute unit (returns the sustained FP16 TFLOP/s
  * under the chip's power limit), or a streaming copy of `bytes` bytes between two halves of `buffer` (returns

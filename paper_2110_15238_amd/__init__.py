@@ -5,8 +5,8 @@ The Python layer only marshals arguments; importing it fails if the HIP library 
 """
 from . import binding
 from .binding import (ACT, LAYOUT_KN, LAYOUT_NK, OP_B2B_CONV, OP_B2B_CONV_RES, OP_B2B_GEMM, OP_B2B_GEMM_RES, OP_CONV2D, OP_CONV_CHAIN3, OP_GEMM, OP_GEMM_CHAIN3, BoltConfig, BoltError,
-                      ConvDesc, GemmDesc, GemmW4Desc, MoeDesc, MoeRouteDesc, TENSOR_NCHW, TENSOR_NHWC, TuneResult, conv_desc,
-                      conv_out_hw, gemm_desc, gemm_w4_desc, moe_desc, moe_route_desc)
+                      ConvDesc, GemmDesc, GemmLoraDesc, GemmQ8Desc, GemmW4Desc, MoeDesc, MoeRouteDesc, RmsNormDesc, TENSOR_NCHW, TENSOR_NHWC, TuneResult,
+                      conv_desc, conv_out_hw, gemm_desc, gemm_lora_desc, gemm_q8_desc, gemm_w4_desc, moe_desc, moe_route_desc, rms_norm_desc)
 
 # the C ABI's entry points under their own names
 bolt_gemm_epilogue = binding.gemm_epilogue
@@ -38,6 +38,12 @@ bolt_moe_route = binding.moe_route
 bolt_moe_route_workspace_bytes = binding.moe_route_workspace_bytes
 bolt_moe_experts = binding.moe_experts
 bolt_moe_workspace_bytes = binding.moe_workspace_bytes
+bolt_rms_norm = binding.rms_norm
+bolt_quantize_rows = binding.quantize_rows
+bolt_gemm_q8 = binding.gemm_q8
+bolt_gemm_q8_workspace_bytes = binding.gemm_q8_workspace_bytes
+bolt_gemm_lora = binding.gemm_lora
+bolt_gemm_lora_workspace_bytes = binding.gemm_lora_workspace_bytes
 bolt_workspace_bytes = binding.workspace_bytes
 bolt_check = binding.check
 bolt_status_string = binding.status_string

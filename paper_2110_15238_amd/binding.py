@@ -71,6 +71,21 @@ class MoeDesc(C.Structure):
                                          "weights", "group")]
 
 
+class RmsNormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "width", "ldx", "ldr", "lds", "ldy", "ldq")] + \
+        [("eps", C.c_float), ("weight_offset", C.c_float)]
+
+
+class GemmQ8Desc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("lda", C.c_int32), ("ldd", C.c_int32),
+                ("alpha", C.c_float), ("beta", C.c_float), ("act", C.c_int32)]
+
+
+class GemmLoraDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("M", "N", "K", "lda", "ldd", "weights", "group", "adapters", "rank")] + \
+        [("alpha", C.c_float), ("beta", C.c_float), ("act", C.c_int32)]
+
+
 LOGITS = {"f16": 0, "f32": 1}
 SCORE = {"softmax": 0, "sigmoid": 1}
 WEIGHTS = {"f16": 0, "w4": 1}
@@ -167,6 +182,18 @@ _lib.bolt_moe_experts.restype = C.c_int
 _lib.bolt_moe_experts.argtypes = [C.POINTER(MoeDesc)] + [_vp] * 11 + [_sz, _vp]
 _lib.bolt_moe_workspace_bytes.restype = _sz
 _lib.bolt_moe_workspace_bytes.argtypes = [C.POINTER(MoeDesc)]
+_lib.bolt_rms_norm.restype = C.c_int
+_lib.bolt_rms_norm.argtypes = [C.POINTER(RmsNormDesc)] + [_vp] * 8
+_lib.bolt_quantize_rows.restype = C.c_int
+_lib.bolt_quantize_rows.argtypes = [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]
+_lib.bolt_gemm_q8.restype = C.c_int
+_lib.bolt_gemm_q8.argtypes = [C.POINTER(GemmQ8Desc)] + [_vp] * 7 + [_sz, _vp]
+_lib.bolt_gemm_q8_workspace_bytes.restype = _sz
+_lib.bolt_gemm_q8_workspace_bytes.argtypes = [C.POINTER(GemmQ8Desc)]
+_lib.bolt_gemm_lora.restype = C.c_int
+_lib.bolt_gemm_lora.argtypes = [C.POINTER(GemmLoraDesc)] + [_vp] * 9 + [_sz, _vp]
+_lib.bolt_gemm_lora_workspace_bytes.restype = _sz
+_lib.bolt_gemm_lora_workspace_bytes.argtypes = [C.POINTER(GemmLoraDesc)]
 _lib.bolt_probe_mfma_peak.restype = C.c_int
 _lib.bolt_probe_mfma_peak.argtypes = [_i32, _vp, C.POINTER(C.c_float)]
 _lib.bolt_probe_copy_bandwidth.restype = C.c_int
@@ -179,7 +206,8 @@ EXPORTED = ["bolt_gemm_epilogue", "bolt_gemm_epilogue_noalloc", "bolt_conv2d_fpr
             "bolt_chain_instance_supports",
             "bolt_pad_channels_nhwc", "bolt_nchw_to_nhwc", "bolt_nhwc_to_nchw", "bolt_bias_act", "bolt_w4_packed_bytes", "bolt_w4_pack",
             "bolt_gemm_w4", "bolt_gemm_w4_workspace_bytes", "bolt_moe_route", "bolt_moe_route_workspace_bytes", "bolt_moe_experts",
-            "bolt_moe_workspace_bytes", "bolt_workspace_bytes", "bolt_check", "bolt_status_string",
+            "bolt_moe_workspace_bytes", "bolt_rms_norm", "bolt_quantize_rows", "bolt_gemm_q8", "bolt_gemm_q8_workspace_bytes", "bolt_gemm_lora",
+            "bolt_gemm_lora_workspace_bytes", "bolt_workspace_bytes", "bolt_check", "bolt_status_string",
             "bolt_num_instances", "bolt_instance_config", "bolt_instance_supports", "bolt_probe_mfma_peak",
             "bolt_probe_copy_bandwidth"]
 
@@ -222,7 +250,7 @@ def _load_fast():
     _load_torch()
     try:
         from . import _fastcall
-        _fastcall.types(GemmDesc, ConvDesc, BoltConfig, GemmW4Desc, MoeRouteDesc, MoeDesc)
+        _fastcall.types(GemmDesc, ConvDesc, BoltConfig, GemmW4Desc, MoeRouteDesc, MoeDesc, RmsNormDesc, GemmQ8Desc, GemmLoraDesc)
         _fast = _fastcall
     except ImportError as e:
         warnings.warn("calls are marshalled through ctypes, a microsecond slower: %s (make -C paper_2110_15238_amd/csrc "
@@ -664,6 +692,97 @@ def moe_experts(desc: MoeDesc, x, w_up, b_up, w_down, b_down, ids, weights, offs
                                  _buffer(offsets, "int32", d.experts + 1, "offsets"), _buffer(order, "int32", slots, "order"),
                                  _buffer(y, "float16", _span(d.tokens, d.ldy, d.width), "y"), wp, wb, _stream()), "bolt_moe_experts")
     return y
+
+
+# ---- rows in 8 bits: the norm that writes them, the linear layer that reads them; projections with low-rank adapters ------------
+
+
+def rms_norm_desc(rows, width, ldx=None, ldr=None, lds=None, ldy=None, ldq=None, eps=1e-5, weight_offset=0.0) -> RmsNormDesc:
+    return RmsNormDesc(rows, width, *(width if ld is None else ld for ld in (ldx, ldr, lds, ldy, ldq)), eps, weight_offset)
+
+
+def rms_norm(desc: RmsNormDesc, x, residual, weight, sum=None, y=None, q=None, scales=None):
+    """sum = x + residual, y and q its norm times the weight: x, residual (or None), weight, sum (or None) and y (or None) float16, q (or
+    None) float8_e4m3fn with scales float32.  Returns (sum, y, q, scales)."""
+    status = (_fast or _load_fast()).rms_norm(desc, x, residual, weight, sum, y, q, scales)
+    if status == 0:
+        return sum, y, q, scales
+    if status is not None:
+        raise BoltError(status, "bolt_rms_norm")
+    d = desc
+    _check(_lib.bolt_rms_norm(C.byref(d), _buffer(x, "float16", _span(d.rows, d.ldx, d.width), "x"),
+                              _buffer_or_none(residual, "float16", _span(d.rows, d.ldr, d.width), "residual"),
+                              _buffer(weight, "float16", d.width, "weight"),
+                              _buffer_or_none(sum, "float16", _span(d.rows, d.lds, d.width), "sum"),
+                              _buffer_or_none(y, "float16", _span(d.rows, d.ldy, d.width), "y"),
+                              _buffer_or_none(q, "float8_e4m3fn", _span(d.rows, d.ldq, d.width), "q"),
+                              _buffer_or_none(scales, "float32", d.rows, "scales"), _stream()), "bolt_rms_norm")
+    return sum, y, q, scales
+
+
+def quantize_rows(x, q, scales):
+    """x: float16 [rows][width], rows of any stride -> q: float8_e4m3fn [rows][width], scales: float32 [rows]."""
+    rows, width = x.shape
+    assert q.shape == x.shape and all(t.stride(1) == 1 or width == 1 for t in (x, q)), "x and q: rows x width, values of a row next to each other"
+    ldx, ldq = (t.stride(0) if rows > 1 else width for t in (x, q))
+    torch = _torch or _load_torch()
+    assert x.is_cuda and x.dtype is torch.float16 and q.is_cuda and q.dtype is torch.float8_e4m3fn, "expects CUDA float16 rows and float8_e4m3fn ones"
+    _check(_lib.bolt_quantize_rows(rows, width, ldx, ldq, x.data_ptr(), q.data_ptr(), _buffer(scales, "float32", rows, "scales"), _stream()),
+           "bolt_quantize_rows")
+    return q, scales
+
+
+def gemm_q8_desc(M, N, K, lda=None, ldd=None, alpha=1.0, beta=1.0, act="none") -> GemmQ8Desc:
+    return GemmQ8Desc(M, N, K, K if lda is None else lda, N if ldd is None else ldd, alpha, beta, ACT[act])
+
+
+def gemm_q8_workspace_bytes(desc: GemmQ8Desc) -> int:
+    return int(_lib.bolt_gemm_q8_workspace_bytes(C.byref(desc)))
+
+
+def gemm_q8(desc: GemmQ8Desc, A, a_scales, W, w_scales, bias, D, workspace=None):
+    """D = act(alpha (a_scales A).(w_scales W)^T + beta bias): A, W float8_e4m3fn, the scales float32 or None."""
+    status = (_fast or _load_fast()).gemm_q8(desc, A, a_scales, W, w_scales, bias, D, workspace)
+    if status == 0:
+        return D
+    if status is not None:
+        raise BoltError(status, "bolt_gemm_q8")
+    d = desc
+    wp, wb = _ws(workspace)
+    _check(_lib.bolt_gemm_q8(C.byref(d), _buffer(A, "float8_e4m3fn", _span(d.M, d.lda, d.K), "A"), _buffer_or_none(a_scales, "float32", d.M, "a_scales"),
+                             _buffer(W, "float8_e4m3fn", d.N * d.K, "W"), _buffer_or_none(w_scales, "float32", d.N, "w_scales"),
+                             _buffer_or_none(bias, "float16", d.N, "bias"), _buffer(D, "float16", _span(d.M, d.ldd, d.N), "D"),
+                             wp, wb, _stream()), "bolt_gemm_q8")
+    return D
+
+
+def gemm_lora_desc(M, N, K, adapters, rank, weights="f16", group=0, lda=None, ldd=None, alpha=1.0, beta=1.0, act="none") -> GemmLoraDesc:
+    return GemmLoraDesc(M, N, K, K if lda is None else lda, N if ldd is None else ldd, WEIGHTS[weights], group, adapters, rank, alpha, beta,
+                        ACT[act])
+
+
+def gemm_lora_workspace_bytes(desc: GemmLoraDesc) -> int:
+    return int(_lib.bolt_gemm_lora_workspace_bytes(C.byref(desc)))
+
+
+def gemm_lora(desc: GemmLoraDesc, A, W, bias, ids, down, up, scales, D, workspace):
+    """D = act(alpha (A.W^T + scales[id] (A.down[id]^T).up[id]^T) + beta bias), id = ids[row] (int32; none below zero): W float16, or packed by
+    w4_pack (uint8); down, up float16; scales float32 or None."""
+    status = (_fast or _load_fast()).gemm_lora(desc, A, W, bias, ids, down, up, scales, D, workspace)
+    if status == 0:
+        return D
+    if status is not None:
+        raise BoltError(status, "bolt_gemm_lora")
+    d = desc
+    w4 = d.weights == WEIGHTS["w4"]
+    wp, wb = _ws(workspace)
+    _check(_lib.bolt_gemm_lora(C.byref(d), _buffer(A, "float16", _span(d.M, d.lda, d.K), "A"),
+                               _buffer(W, "uint8", w4_packed_bytes(d.N, d.K, d.group), "W") if w4 else _buffer(W, "float16", d.N * d.K, "W"),
+                               _buffer_or_none(bias, "float16", d.N, "bias"), _buffer(ids, "int32", d.M, "ids"),
+                               _buffer(down, "float16", d.adapters * d.rank * d.K, "down"), _buffer(up, "float16", d.adapters * d.N * d.rank, "up"),
+                               _buffer_or_none(scales, "float32", d.adapters, "scales"), _buffer(D, "float16", _span(d.M, d.ldd, d.N), "D"),
+                               wp, wb, _stream()), "bolt_gemm_lora")
+    return D
 
 
 def probe_mfma_peak(iterations: int = 20000) -> float:

@@ -11,7 +11,7 @@
 
 namespace {
 
-PyObject *g_gemm_desc, *g_conv_desc, *g_config, *g_gemm_w4_desc, *g_route_desc, *g_moe_desc;  // the ctypes structure types of binding.py
+PyObject *g_gemm_desc, *g_conv_desc, *g_config, *g_gemm_w4_desc, *g_route_desc, *g_moe_desc, *g_norm_desc, *g_gemm_q8_desc, *g_gemm_lora_desc;  // the ctypes structure types of binding.py
 
 // A structure's bytes, copied: the call below runs without the interpreter lock.
 template <typename T>
@@ -32,6 +32,9 @@ bool read(PyObject* o, bolt_conv_desc* d) { return read_struct(o, g_conv_desc, d
 bool read(PyObject* o, bolt_gemm_w4_desc* d) { return read_struct(o, g_gemm_w4_desc, d); }
 bool read(PyObject* o, bolt_moe_route_desc* d) { return read_struct(o, g_route_desc, d); }
 bool read(PyObject* o, bolt_moe_desc* d) { return read_struct(o, g_moe_desc, d); }
+bool read(PyObject* o, bolt_rms_norm_desc* d) { return read_struct(o, g_norm_desc, d); }
+bool read(PyObject* o, bolt_gemm_q8_desc* d) { return read_struct(o, g_gemm_q8_desc, d); }
+bool read(PyObject* o, bolt_gemm_lora_desc* d) { return read_struct(o, g_gemm_lora_desc, d); }
 
 struct Config {
   bolt_config value;
@@ -229,6 +232,46 @@ PyObject* experts(PyObject* const* a) {
   });
 }
 
+// (desc, x, residual, weight, sum, y, q, scales)
+PyObject* norm(PyObject* const* a) {
+  bolt_rms_norm_desc d;
+  void *x, *r, *w, *sum, *y, *q, *scales;
+  if (!read(a[0], &d) || !buffer(a[1], at::kHalf, span(d.rows, d.ldx, d.width), &x) || !buffer_or_none(a[2], at::kHalf, span(d.rows, d.ldr, d.width), &r) ||
+      !buffer(a[3], at::kHalf, d.width, &w) || !buffer_or_none(a[4], at::kHalf, span(d.rows, d.lds, d.width), &sum) ||
+      !buffer_or_none(a[5], at::kHalf, span(d.rows, d.ldy, d.width), &y) ||
+      !buffer_or_none(a[6], at::kFloat8_e4m3fn, span(d.rows, d.ldq, d.width), &q) || !buffer_or_none(a[7], at::kFloat, d.rows, &scales))
+    return nullptr;
+  return call([&](void* s) { return bolt_rms_norm(&d, x, r, w, sum, y, q, scales, s); });
+}
+
+// (desc, A, a_scales, W, w_scales, bias, D, workspace)
+PyObject* product_q8(PyObject* const* a) {
+  bolt_gemm_q8_desc d;
+  void *x, *xs, *w, *wsc, *b, *y;
+  Workspace ws;
+  if (!read(a[0], &d) || !buffer(a[1], at::kFloat8_e4m3fn, span(d.M, d.lda, d.K), &x) || !buffer_or_none(a[2], at::kFloat, d.M, &xs) ||
+      !buffer(a[3], at::kFloat8_e4m3fn, (int64_t)d.N * d.K, &w) || !buffer_or_none(a[4], at::kFloat, d.N, &wsc) ||
+      !buffer_or_none(a[5], at::kHalf, d.N, &b) || !buffer(a[6], at::kHalf, span(d.M, d.ldd, d.N), &y) || !ws.read(a[7]))
+    return nullptr;
+  return call([&](void* s) { return bolt_gemm_q8(&d, x, xs, w, wsc, b, y, ws.ptr, ws.bytes, s); });
+}
+
+// (desc, A, W, bias, ids, down, up, scales, D, workspace)
+PyObject* product_lora(PyObject* const* a) {
+  bolt_gemm_lora_desc d;
+  void *x, *w, *b, *ids, *down, *up, *scales, *y;
+  Workspace ws;
+  if (!read(a[0], &d)) return nullptr;
+  const bool w4 = d.weights == BOLT_WEIGHTS_W4;
+  const int64_t weights = w4 ? (int64_t)bolt_w4_packed_bytes(d.N, d.K, d.group, 1) : (int64_t)d.N * d.K, ranks = (int64_t)d.adapters * d.rank;
+  if (!buffer(a[1], at::kHalf, span(d.M, d.lda, d.K), &x) || !buffer(a[2], w4 ? at::kByte : at::kHalf, weights, &w) ||
+      !buffer_or_none(a[3], at::kHalf, d.N, &b) || !buffer(a[4], at::kInt, d.M, &ids) || !buffer(a[5], at::kHalf, ranks * d.K, &down) ||
+      !buffer(a[6], at::kHalf, ranks * d.N, &up) || !buffer_or_none(a[7], at::kFloat, d.adapters, &scales) ||
+      !buffer(a[8], at::kHalf, span(d.M, d.ldd, d.N), &y) || !ws.read(a[9]))
+    return nullptr;
+  return call([&](void* s) { return bolt_gemm_lora(&d, x, w, b, ids, down, up, scales, y, ws.ptr, ws.bytes, s); });
+}
+
 #define FASTCALL(NAME, WANT, ...) \
   PyObject* NAME(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded<&__VA_ARGS__>(a, n, WANT); }
 FASTCALL(gemm, 7, single<bolt_gemm_desc, &bolt_gemm_epilogue>)
@@ -242,15 +285,18 @@ FASTCALL(conv_chain, 6, chain<bolt_conv_desc, &bolt_b2b_conv_chain>)
 FASTCALL(gemm_w4, 6, product_w4)
 FASTCALL(moe_route, 9, route)
 FASTCALL(moe_experts, 12, experts)
+FASTCALL(rms_norm, 8, norm)
+FASTCALL(gemm_q8, 8, product_q8)
+FASTCALL(gemm_lora, 10, product_lora)
 
-// The structure types, once: GemmDesc, ConvDesc, BoltConfig, GemmW4Desc, MoeRouteDesc, MoeDesc.
+// The structure types, once: GemmDesc, ConvDesc, BoltConfig, GemmW4Desc, MoeRouteDesc, MoeDesc, RmsNormDesc, GemmQ8Desc, GemmLoraDesc.
 PyObject* types(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 6) {
-    PyErr_SetString(PyExc_TypeError, "types(GemmDesc, ConvDesc, BoltConfig, GemmW4Desc, MoeRouteDesc, MoeDesc)");
+  if (n != 9) {
+    PyErr_SetString(PyExc_TypeError, "types(GemmDesc, ConvDesc, BoltConfig, GemmW4Desc, MoeRouteDesc, MoeDesc, RmsNormDesc, GemmQ8Desc, GemmLoraDesc)");
     return nullptr;
   }
-  PyObject** const at[6] = {&g_gemm_desc, &g_conv_desc, &g_config, &g_gemm_w4_desc, &g_route_desc, &g_moe_desc};
-  for (int i = 0; i < 6; ++i) {
+  PyObject** const at[9] = {&g_gemm_desc, &g_conv_desc, &g_config, &g_gemm_w4_desc, &g_route_desc, &g_moe_desc, &g_norm_desc, &g_gemm_q8_desc, &g_gemm_lora_desc};
+  for (int i = 0; i < 9; ++i) {
     Py_INCREF(a[i]);
     *at[i] = a[i];
   }
@@ -259,7 +305,7 @@ PyObject* types(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {METHOD(gemm), METHOD(conv), METHOD(gemm_residual), METHOD(conv_residual), METHOD(gemm_pair), METHOD(conv_pair),
-                           METHOD(gemm_chain), METHOD(conv_chain), METHOD(gemm_w4), METHOD(moe_route), METHOD(moe_experts), METHOD(types), {nullptr, nullptr, 0, nullptr}};
+                           METHOD(gemm_chain), METHOD(conv_chain), METHOD(gemm_w4), METHOD(moe_route), METHOD(moe_experts), METHOD(rms_norm), METHOD(gemm_q8), METHOD(gemm_lora), METHOD(types), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -31,6 +31,21 @@ hipError_t launch_shared_rows_w4(const RowsParams& p, int mode, bool gated, int 
 hipError_t launch_shared_rows_w4_marked(const RowsParams& p, int group, hipStream_t stream);
 hipError_t launch_many_rows_f16(const RowsParams& p, int mode, bool gated, ManyTile tile, hipStream_t stream);
 
+// Linear layers of E4M3 operands: x, ldx, K and steps in pairs (halves); x_scales, w_scales.
+enum class TileF8 { ROWS32_COLS32, ROWS32_COLS64, ROWS64_COLS128, ROWS128_COLS256, ROWS256_COLS256 };
+hipError_t launch_few_rows_f8(const RowsParams& p, hipStream_t stream);
+hipError_t launch_rows_f8(const RowsParams& p, TileF8 tile, hipStream_t stream);
+
+// Linear layers of up to 16 rows whose sums take the rows' adapters (adapter, low, up, adapters, rank).
+hipError_t launch_few_rows_f16_lora(const RowsParams& p, hipStream_t stream);
+hipError_t launch_few_rows_w4_lora(const RowsParams& p, int group, hipStream_t stream);
+
+// bolt_gemm_w4 behind its checks; `add` (M x N, ldadd, or null): added to A . W^T before alpha, from 17 rows on (csrc/moe_api.hip).
+bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d);
+bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, const half_t* add, int ldadd, void* D,
+                        void* workspace, void* stream);
+RowsParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, void* D, const half_t* none);
+
 // What bolt_gemm_epilogue's own choice of a kernel is estimated to take, in us; false where it has none (csrc/bolt_api.hip).
 bool estimate_gemm(const bolt_gemm_desc& d, double* us);
 }  // namespace bolt

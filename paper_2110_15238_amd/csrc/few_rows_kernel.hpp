@@ -159,12 +159,47 @@ struct RowsWave {
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[t][b][e] += (float)scale[e] * sum[b][e];
         }
+      } else if constexpr (WT == WEIGHTS_F8) {
+#pragma unroll
+        for (int b = 0; b < MB; ++b)
+          acc[t][b] = mfma_16x16x128_f8(__builtin_bit_cast(half8, w.piece[t][0]), __builtin_bit_cast(half8, w.piece[t][1]), x.part[0][b], x.part[1][b], acc[t][b]);
       } else {
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
           for (int b = 0; b < MB; ++b) acc[t][b] = mfma_16x16x32(__builtin_bit_cast(half8, w.piece[t][s]), x.part[s][b], acc[t][b]);
       }
+    }
+  }
+  // The rows' adapters: acc += up[a] . low^T for every adapter a that one of the rows has, the waves by turns.  Each sum is taken only where the
+  // row's adapter is a: one adapter's infinity does not reach the others' rows.
+  template <int NW>
+  __device__ __forceinline__ void add_adapters(int col0, int wave, floatx4 (&acc)[R][MB]) const {
+    static_assert(MB == 1, "one block of 16 rows");
+    const int mine = row_adapter(p.adapter, p.adapters, row0 + l16, l16 < rows);
+    unsigned left = (unsigned)__ballot(mine >= 0) & 0xffffu;
+    const half_t* const low = p.low + (int64_t)(row0 + (l16 < rows ? l16 : rows - 1)) * p.rank + g * 8;
+    for (int turn = 0; left != 0; ++turn) {
+      const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
+      left &= ~(unsigned)__ballot(mine == a);
+      if (turn % NW != wave) continue;
+      const half_t* const up = p.up + (int64_t)a * p.N * p.rank + g * 8;
+      floatx4 sum[R] = {};
+      for (int k = 0; k < p.rank; k += 32) {
+        const bool in = k + g * 8 < p.rank;
+        const int at = in ? k : -g * 8;
+        const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0}, b = *(const half8*)(low + at);
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+          const int n = col0 + t * 16 + l16;
+          const half8 u = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + at);
+          sum[t] = mfma_16x16x32(in ? u : zero, in ? b : zero, sum[t]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < R; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][0][e] += mine == a ? sum[t][e] : 0.f;
     }
   }
   // part: [waves][R * MB][64 lanes][4] floats
@@ -195,7 +230,9 @@ struct RowsWave {
       const int at = i & 63, b = (i >> 6) % MB, t = (i >> 6) / MB;
       const int j = b * 16 + (at & 15), col = col0 + t * 16 + (at >> 4) * 4;
       if (j >= rows || col >= outputs) continue;
-      floatx4 v = with_bias(sum_of(GATED ? 2 * t : t, b, at), col);
+      floatx4 sum = sum_of(GATED ? 2 * t : t, b, at);
+      if constexpr (WT == WEIGHTS_F8) sum *= column_scales(p, col) * (p.x_scales ? p.x_scales[row0 + j] : 1.f);
+      floatx4 v = with_bias(sum, col);
       v = apply_act4(v, p.act);
       if constexpr (GATED) v *= with_bias(sum_of(2 * t + 1, b, at), p.hidden + col);
       if constexpr (MODE == ROWS_DOWN) {
@@ -211,7 +248,7 @@ struct RowsWave {
 };
 
 // Deep reductions: a wave's steps pass through NB register sets, one tile of columns per workgroup.
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NB>
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NB, bool LORA = false>
 __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   extern __shared__ __attribute__((aligned(16))) float part[];
@@ -242,8 +279,12 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
     w.template load_rows<false>(wave + i * NW, xf[decltype(b)::value]);
   };
   auto multiply = [&](auto b) { w.template multiply<false>(0, wf[decltype(b)::value], xf[decltype(b)::value], acc); };
+  auto adapters = [&] {
+    if constexpr (LORA) w.template add_adapters<NW>(col0, wave, acc);
+  };
   if (n >= NB) {
     for_constants<NB>([&](auto b) { load(decltype(b)::value, b); });
+    adapters();
     int c = 0;
     for (; c + 2 * NB <= n; c += NB)
       for_constants<NB>([&](auto b) {
@@ -262,6 +303,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
     for_constants<NB>([&](auto b) {
       if (decltype(b)::value < n) load(decltype(b)::value, b);
     });
+    adapters();
     for_constants<NB>([&](auto b) {
       if (decltype(b)::value < n) multiply(b);
     });
@@ -283,7 +325,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
 // (Two workgroups of eight waves share a compute unit with up to 128 registers, which the routed kernels of one group a step and two steps just miss if
 // left alone: one token, 8 of 64 experts, 2048 x 2048, no gate, 20.9 us so and 17.7 held to 128; 3 tokens, 3 of 44 experts, 1560 x 664, gated, 14.6
 // and 13.7.  Linear layers would spill.)
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX, bool LORA = false>
 __global__ __launch_bounds__(64 * NW, WT == WEIGHTS_W4 && MODE != ROWS_DENSE && NG == 1 && NX == 2 ? 4 : 1) void few_rows_walk_kernel(const RowsParams p) {
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int PART = NW * R * 64 * 4;
@@ -320,6 +362,7 @@ __global__ __launch_bounds__(64 * NW, WT == WEIGHTS_W4 && MODE != ROWS_DENSE && 
   for_constants<NX>([&](auto i) { w.template load_rows<true>(wave + decltype(i)::value * NW, xf[decltype(i)::value]); });
   auto tile = [&](int it, auto set) {
     floatx4 acc[R][1] = {};
+    if constexpr (LORA) w.template add_adapters<NW>((cb + it) * Wave::COLS, wave, acc);
     for_constants<NX>([&](auto i) {
       w.template multiply<true>(wave + decltype(i)::value * NW, wf[decltype(set)::value][decltype(i)::value], xf[decltype(i)::value], acc);
     });
@@ -344,9 +387,9 @@ __global__ __launch_bounds__(64 * NW, WT == WEIGHTS_W4 && MODE != ROWS_DENSE && 
   }
 }
 
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NB>
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NB, bool LORA = false>
 hipError_t launch_few_rows(RowsParams p, hipStream_t stream) {
-  auto kern = few_rows_kernel<WT, MODE, GATED, NG, R, NW, NB>;
+  auto kern = few_rows_kernel<WT, MODE, GATED, NG, R, NW, NB, LORA>;
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int LDS_BYTES = NW * R * 64 * 16;
   static LdsOptIn opt_in;
@@ -356,9 +399,9 @@ hipError_t launch_few_rows(RowsParams p, hipStream_t stream) {
   hipLaunchKernelGGL(kern, dim3(p.row_blocks * p.col_blocks), dim3(64 * NW), LDS_BYTES, stream, p);
   return hipGetLastError();
 }
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX, bool LORA = false>
 hipError_t launch_few_rows_walk(RowsParams p, hipStream_t stream) {
-  auto kern = few_rows_walk_kernel<WT, MODE, GATED, NG, R, NW, NX>;
+  auto kern = few_rows_walk_kernel<WT, MODE, GATED, NG, R, NW, NX, LORA>;
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int LDS_BYTES = 2 * NW * R * 64 * 16;
   static LdsOptIn opt_in;

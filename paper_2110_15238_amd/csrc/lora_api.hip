@@ -1,0 +1,134 @@
+// C ABI of projections that are shared by requests with low-rank adapters of their own.
+#include <algorithm>
+
+#include "few_rows_instances.hpp"
+#include "llm_checks.hpp"
+#include "lora_kernel.hpp"
+
+namespace bolt {
+namespace {
+
+constexpr int kMaxRank = 128, kFewRows = 16;
+
+bolt_gemm_w4_desc base_w4(const bolt_gemm_lora_desc& d) { return {d.M, d.N, d.K, d.lda, d.ldd, d.group, d.alpha, d.beta, d.act}; }
+
+bolt_status check_gemm_lora(const bolt_gemm_lora_desc* d) {
+  if (!d || d->M < 0 || d->N <= 0 || d->K <= 0 || d->adapters <= 0 || d->rank <= 0 || d->lda < d->K || d->ldd < d->N) return BOLT_ERR_INVALID_ARG;
+  if (!known_act(d->act) || d->act == BOLT_ACT_SILU) return BOLT_ERR_INVALID_ARG;
+  if (d->weights != BOLT_WEIGHTS_F16 && d->weights != BOLT_WEIGHTS_W4) return BOLT_ERR_INVALID_ARG;
+  if (d->weights == BOLT_WEIGHTS_W4) {
+    const bolt_gemm_w4_desc base = base_w4(*d);
+    if (bolt_status s = check_gemm_w4(&base); s == BOLT_ERR_INVALID_ARG) return s;
+  }
+  if ((d->N | d->K | d->lda | d->ldd | d->rank) & 7) return BOLT_ERR_ALIGNMENT;
+  if (d->lda > kMaxLength || d->ldd > kMaxLength || d->rank > kMaxRank || d->M > kMaxRows) return BOLT_ERR_UNSUPPORTED;
+  // the launches of 64 x 256 outputs and of 16 rows here, and those of the projection
+  if (!launches(blocks_of(d->M, 16)) || !launches(blocks_of(d->M, 64) * blocks_of(d->N, 256))) return BOLT_ERR_UNSUPPORTED;
+  if (d->weights == BOLT_WEIGHTS_F16 && !launches(blocks_of(d->M, 32) * blocks_of(d->N, 32))) return BOLT_ERR_UNSUPPORTED;
+  return BOLT_OK;
+}
+
+// The workspace: low [M][rank]; of 4-bit weights that may be unpacked the unpacked ones and the adapters' share [M][N] (which otherwise goes through D:
+// there the rows with weights beyond FP16's range are computed a second time).
+struct LoraWorkspace {
+  int64_t weights_at, share_at, bytes;
+};
+LoraWorkspace lora_workspace(const bolt_gemm_lora_desc& d) {
+  LoraWorkspace w;
+  w.weights_at = w.share_at = w.bytes = round_up((int64_t)d.M * d.rank * 2, 256);
+  if (d.weights == BOLT_WEIGHTS_W4) {
+    const bolt_gemm_w4_desc base = base_w4(d);
+    if (const size_t unpacked = bolt_gemm_w4_workspace_bytes(&base); unpacked > 0) {
+      w.share_at = w.weights_at + round_up((int64_t)unpacked, 256);
+      w.bytes = w.share_at + round_up((int64_t)d.M * d.N * 2, 256);
+    }
+  }
+  return w;
+}
+
+template <int RT, int NW, int U, bool SPREAD>
+hipError_t launch_down(LoraParams p, hipStream_t stream) {
+  auto kern = lora_down_kernel<RT, NW, U, SPREAD>;
+  constexpr int LDS_BYTES = NW * RT * 1024;
+  static LdsOptIn opt_in;
+  if (hipError_t e = opt_in.ensure((const void*)kern, LDS_BYTES); e != hipSuccess) return e;
+  p.blocks = (p.M + 15) / 16;
+  p.tiles = (p.rank + 16 * RT - 1) / (16 * RT);
+  hipLaunchKernelGGL(kern, dim3(SPREAD ? p.blocks * p.tiles * 16 : p.blocks), dim3(64 * NW), LDS_BYTES, stream, p);
+  return hipGetLastError();
+}
+hipError_t launch_lora_down(const LoraParams& p, hipStream_t stream) {
+  if (p.M <= 64) return launch_down<1, 16, 4, true>(p, stream);
+  if (p.rank <= 16) return launch_down<1, 8, 4, false>(p, stream);
+  if (p.rank <= 32) return launch_down<2, 8, 2, false>(p, stream);
+  if (p.rank <= 64) return launch_down<4, 8, 2, false>(p, stream);
+  return launch_down<8, 8, 1, false>(p, stream);
+}
+hipError_t launch_lora_up(LoraParams p, hipStream_t stream) {
+  p.blocks = (p.M + 63) / 64;
+  p.tiles = (p.N + 255) / 256;
+  hipLaunchKernelGGL(lora_up_kernel, dim3(p.blocks * p.tiles), dim3(256), 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace bolt
+
+using namespace bolt;
+
+extern "C" {
+
+size_t bolt_gemm_lora_workspace_bytes(const bolt_gemm_lora_desc* desc) {
+  if (check_gemm_lora(desc) != BOLT_OK) return 0;
+  return (size_t)lora_workspace(*desc).bytes;
+}
+
+bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const void* W, const void* bias, const void* ids, const void* down,
+                           const void* up, const void* scales, void* D, void* workspace, size_t workspace_bytes, void* stream) {
+  if (bolt_status s = check_gemm_lora(desc); s != BOLT_OK) return s;
+  if (desc->M == 0) return BOLT_OK;
+  if (!A || !W || !ids || !down || !up || !D) return BOLT_ERR_INVALID_ARG;
+  for (const void* at : {A, W, bias, ids, down, up, scales, (const void*)D, (const void*)workspace})
+    if (!aligned16(at)) return BOLT_ERR_ALIGNMENT;
+  const bolt_gemm_lora_desc& d = *desc;
+  const LoraWorkspace ws = lora_workspace(d);
+  if (!workspace || workspace_bytes < (size_t)ws.bytes) return BOLT_ERR_WORKSPACE;
+  const half_t* none = no_bias();
+  if (!none) return BOLT_ERR_LAUNCH;
+  const bool w4 = d.weights == BOLT_WEIGHTS_W4;
+  const bolt_gemm_w4_desc base = base_w4(d);
+  const hipStream_t st = (hipStream_t)stream;
+  LoraParams l{};
+  l.x = (const half_t*)A; l.ldx = d.lda;
+  l.adapter = (const int*)ids;
+  l.down = (const half_t*)down; l.up = (const half_t*)up; l.scales = (const float*)scales;
+  l.low = (half_t*)workspace;
+  l.M = d.M; l.N = d.N; l.K = d.K; l.adapters = d.adapters; l.rank = d.rank;
+  if (launch_lora_down(l, st) != hipSuccess) return BOLT_ERR_LAUNCH;
+  if (d.M <= kFewRows) {
+    RowsParams p{};
+    if (w4) {
+      p = dense_w4_rows(base, A, W, bias, D, none);
+    } else {
+      p.x = (const half_t*)A; p.ldx = d.lda;
+      p.w = (const unsigned char*)W; p.w_stride = (int64_t)d.N * d.K * 2;
+      p.none = none;
+      p.bias = bias ? (const half_t*)bias : none;
+      p.bias_on = bias ? 1 : 0;
+      p.y = D; p.ldy = d.ldd;
+      p.M = d.M; p.N = d.N; p.K = d.K; p.steps = (d.K + 63) / 64;
+      p.alpha = d.alpha; p.beta = d.beta; p.act = d.act;
+    }
+    p.adapter = l.adapter; p.low = l.low; p.up = l.up; p.adapters = d.adapters; p.rank = d.rank;
+    return status_of(w4 ? launch_few_rows_w4_lora(p, d.group, st) : launch_few_rows_f16_lora(p, st));
+  }
+  const bool apart = ws.share_at != ws.weights_at;
+  l.y = apart ? (half_t*)((char*)workspace + ws.share_at) : (half_t*)D;
+  l.ldy = apart ? d.N : d.ldd;
+  if (launch_lora_up(l, st) != hipSuccess) return BOLT_ERR_LAUNCH;
+  if (w4) return run_gemm_w4(base, A, W, bias, l.y, (int)l.ldy, D, (char*)workspace + ws.weights_at, stream);
+  const bolt_gemm_desc g = {d.M, d.N, d.K, d.lda, d.K, d.ldd, d.alpha, d.beta, d.act, BOLT_LAYOUT_NK};
+  return bolt_gemm_epilogue_residual(&g, A, W, bias, D, d.ldd, d.alpha, D, nullptr, nullptr, 0, stream);
+}
+
+}  // extern "C"

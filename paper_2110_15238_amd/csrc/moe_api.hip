@@ -5,6 +5,7 @@
 
 #include "../../include/bolt.h"
 #include "few_rows_instances.hpp"
+#include "llm_checks.hpp"
 #include "w4_format.hpp"
 #include "moe_route_kernel.hpp"
 
@@ -143,35 +144,11 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const float* rows, con
 }
 
 __device__ __attribute__((aligned(16))) half_t g_no_bias[8];
-const half_t* no_bias() {
-  static PerDevice known;
-  return (const half_t*)address_on_device(known, g_no_bias);
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
-int64_t blocks_of(int64_t v, int64_t by) { return (v + by - 1) / by; }
-bool known_act(int a) { return a >= BOLT_ACT_NONE && a <= BOLT_ACT_SILU; }
-bolt_status status_of(hipError_t e) { return e == hipSuccess ? BOLT_OK : BOLT_ERR_LAUNCH; }
-constexpr int kMaxLength = 1 << 21;  // of a row, as in the other operators
-// Rows and slots: the kernels count them in 32 bits, as far as the end of the last workgroup's share and one stride past it.
-constexpr int64_t kMaxRows = (1ll << 31) - (1 << 16);
-// Threads of a launch: the runtime counts them in 32 bits.  No workgroup whose number grows with the rows has more than 512.
-bool launches(int64_t blocks) { return blocks <= UINT32_MAX / 512; }
 
 bolt_status check_w4_shape(int32_t N, int32_t K, int32_t group) {
   if (N <= 0 || K <= 0 || (group != 32 && group != 64 && group != 128)) return BOLT_ERR_INVALID_ARG;
   if ((N | K) & 7) return BOLT_ERR_ALIGNMENT;
   if (N > kMaxLength || K > kMaxLength) return BOLT_ERR_UNSUPPORTED;
-  return BOLT_OK;
-}
-
-bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d) {
-  if (!d) return BOLT_ERR_INVALID_ARG;
-  if (bolt_status s = check_w4_shape(d->N, d->K, d->group); s == BOLT_ERR_INVALID_ARG) return s;
-  if (d->M < 0 || !known_act(d->act) || d->lda < d->K || d->ldd < d->N) return BOLT_ERR_INVALID_ARG;
-  if ((d->N | d->K | d->lda | d->ldd) & 7) return BOLT_ERR_ALIGNMENT;
-  if (d->lda > kMaxLength || d->ldd > kMaxLength || d->N > kMaxLength || d->M > kMaxRows) return BOLT_ERR_UNSUPPORTED;
   return BOLT_OK;
 }
 
@@ -388,6 +365,69 @@ MoeWorkspace moe_workspace(const bolt_moe_desc& d) {
 }
 
 }  // namespace
+
+const half_t* no_bias() {
+  static PerDevice known;
+  return (const half_t*)address_on_device(known, g_no_bias);
+}
+
+bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d) {
+  if (!d) return BOLT_ERR_INVALID_ARG;
+  if (bolt_status s = check_w4_shape(d->N, d->K, d->group); s == BOLT_ERR_INVALID_ARG) return s;
+  if (d->M < 0 || !known_act(d->act) || d->lda < d->K || d->ldd < d->N) return BOLT_ERR_INVALID_ARG;
+  if ((d->N | d->K | d->lda | d->ldd) & 7) return BOLT_ERR_ALIGNMENT;
+  if (d->lda > kMaxLength || d->ldd > kMaxLength || d->N > kMaxLength || d->M > kMaxRows) return BOLT_ERR_UNSUPPORTED;
+  return BOLT_OK;
+}
+
+RowsParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, void* D, const half_t* none) {
+  const W4Format f(d.N, d.K, d.group);
+  RowsParams p{};
+  p.x = (const half_t*)A;
+  p.ldx = d.lda;
+  p.w = (const unsigned char*)packed;
+  p.scales = (const half_t*)((const char*)packed + f.scales_at(1));
+  p.zeros = (const unsigned char*)packed + f.zeros_at(1);
+  p.none = none;
+  p.bias = bias ? (const half_t*)bias : none;
+  p.bias_on = bias ? 1 : 0;
+  p.y = D;
+  p.ldy = d.ldd;
+  p.M = d.M; p.N = d.N; p.K = d.K; p.steps = f.steps;
+  p.alpha = d.alpha; p.beta = d.beta; p.act = d.act;
+  return p;
+}
+
+bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, const half_t* add, int ldadd, void* D,
+                        void* workspace, void* stream) {
+  const W4Format f(d.N, d.K, d.group);
+  const DenseTile& tile = d.M > 16 ? dense_tile(d.M, d.N, f.steps, d.group) : kDenseTiles[0];
+  // The kernels of many rows start their sums at beta / alpha times the bias, which has to be finite.
+  const bool bias_in_sum = d.alpha != 0.f && std::fabs(d.beta) <= 1e30f * std::fabs(d.alpha);
+  const bool packed_tiles = d.M > 16 && (!bias_in_sum || !dense_unpacks(d));
+  if (packed_tiles && !launches(blocks_of(d.M, tile.rows) * blocks_of(d.N, tile.cols))) return BOLT_ERR_UNSUPPORTED;
+  const hipStream_t st = (hipStream_t)stream;
+  const half_t* none = no_bias();
+  if (!none) return BOLT_ERR_LAUNCH;
+  RowsParams p = dense_w4_rows(d, A, packed, bias, D, none);
+  p.add = add; p.ldadd = ldadd;
+  if (d.M <= 16) return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, d.group, st));
+  if (packed_tiles) return status_of(launch_shared_rows_w4(p, ROWS_DENSE, false, d.group, tile.tile, st));
+  if (launch_w4_unpack(packed, (half_t*)workspace, f, st) != hipSuccess) return BOLT_ERR_LAUNCH;
+  if (d.act != BOLT_ACT_SILU) {
+    const bolt_gemm_desc g = unpacked_desc(d);
+    const bolt_status s = add ? bolt_gemm_epilogue_residual(&g, A, workspace, bias, add, ldadd, d.alpha, D, nullptr, nullptr, 0, stream)
+                              : bolt_gemm_epilogue(&g, A, workspace, bias, D, nullptr, nullptr, 0, stream);
+    if (s != BOLT_OK) return s;
+  } else {
+    RowsParams u = p;
+    u.w = (const unsigned char*)workspace;
+    u.w_stride = (int64_t)p.N * p.K * 2;
+    if (launch_many_rows_f16(u, ROWS_DENSE, false, ManyTile::ROWS256, st) != hipSuccess) return BOLT_ERR_LAUNCH;
+  }
+  p.unpacked = (const half_t*)workspace;
+  return status_of(launch_shared_rows_w4_marked(p, d.group, st));
+}
 }  // namespace bolt
 
 using namespace bolt;
@@ -426,42 +466,7 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   const size_t need = bolt_gemm_w4_workspace_bytes(desc);
   if (need > 0 && (!workspace || workspace_bytes < need)) return BOLT_ERR_WORKSPACE;
   if (!aligned16(workspace)) return BOLT_ERR_ALIGNMENT;
-  const W4Format f(desc->N, desc->K, desc->group);
-  const DenseTile& tile = desc->M > 16 ? dense_tile(desc->M, desc->N, f.steps, desc->group) : kDenseTiles[0];
-  // The kernels of many rows start their sums at beta / alpha times the bias, which has to be finite.
-  const bool bias_in_sum = desc->alpha != 0.f && std::fabs(desc->beta) <= 1e30f * std::fabs(desc->alpha);
-  const bool packed_tiles = desc->M > 16 && (!bias_in_sum || !dense_unpacks(*desc));
-  if (packed_tiles && !launches(blocks_of(desc->M, tile.rows) * blocks_of(desc->N, tile.cols))) return BOLT_ERR_UNSUPPORTED;
-  const hipStream_t st = (hipStream_t)stream;
-  const half_t* none = no_bias();
-  if (!none) return BOLT_ERR_LAUNCH;
-  RowsParams p{};
-  p.x = (const half_t*)A;
-  p.ldx = desc->lda;
-  p.w = (const unsigned char*)packed;
-  p.scales = (const half_t*)((const char*)packed + f.scales_at(1));
-  p.zeros = (const unsigned char*)packed + f.zeros_at(1);
-  p.none = none;
-  p.bias = bias ? (const half_t*)bias : none;
-  p.bias_on = bias ? 1 : 0;
-  p.y = D;
-  p.ldy = desc->ldd;
-  p.M = desc->M; p.N = desc->N; p.K = desc->K; p.steps = f.steps;
-  p.alpha = desc->alpha; p.beta = desc->beta; p.act = desc->act;
-  if (desc->M <= 16) return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, desc->group, st));
-  if (packed_tiles) return status_of(launch_shared_rows_w4(p, ROWS_DENSE, false, desc->group, tile.tile, st));
-  if (launch_w4_unpack(packed, (half_t*)workspace, f, st) != hipSuccess) return BOLT_ERR_LAUNCH;
-  if (desc->act != BOLT_ACT_SILU) {
-    const bolt_gemm_desc g = unpacked_desc(*desc);
-    if (bolt_status s = bolt_gemm_epilogue(&g, A, workspace, bias, D, nullptr, nullptr, 0, stream); s != BOLT_OK) return s;
-  } else {
-    RowsParams u = p;
-    u.w = (const unsigned char*)workspace;
-    u.w_stride = (int64_t)p.N * p.K * 2;
-    if (launch_many_rows_f16(u, ROWS_DENSE, false, ManyTile::ROWS256, st) != hipSuccess) return BOLT_ERR_LAUNCH;
-  }
-  p.unpacked = (const half_t*)workspace;
-  return status_of(launch_shared_rows_w4_marked(p, desc->group, st));
+  return run_gemm_w4(*desc, A, packed, bias, nullptr, 0, D, workspace, stream);
 }
 
 size_t bolt_moe_route_workspace_bytes(const bolt_moe_route_desc* desc) {

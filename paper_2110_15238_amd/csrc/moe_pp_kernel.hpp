@@ -22,8 +22,11 @@
 
 namespace bolt {
 
-template <int MODE, bool GATED>
+// WT: WEIGHTS_F8 for linear layers in E4M3 (ROWS_DENSE): bytes move as for FP16, a C phase has half the instructions, each of twice the depth and
+// twice the rate; sums start at zero and are scaled by row and column in the epilogue.
+template <int MODE, bool GATED, int WT = WEIGHTS_F16>
 __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
+  static_assert(WT == WEIGHTS_F16 || (WT == WEIGHTS_F8 && MODE == ROWS_DENSE && !GATED), "E4M3: linear layers");
   using T = FpropPpTraits;
   constexpr int BM = 256, BN = T::BN, BK = T::BK, WTM = BM / 2, WTN = T::WTN;
   constexpr int FM = WTM / 16, FN = WTN / 16, KS = BK / 32;
@@ -138,6 +141,13 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
     });
   };
   auto c_phase = [&]() {
+    if constexpr (WT == WEIGHTS_F8) {
+      for_constants<FM * FN>([&](auto ic) {
+        constexpr int i = decltype(ic)::value, a = i / FM, b = i % FM;
+        acc[a][b] = mfma_16x16x128_f8(wf[0][a], wf[1][a], xf[0][b], xf[1][b], acc[a][b]);
+      });
+      return;
+    }
     for_constants<KS * FM * FN>([&](auto ic) {
       constexpr int i = decltype(ic)::value, k = i / (FM * FN), a = (i / FM) % FN, b = i % FM;
       acc[a][b] = mfma_16x16x32(wf[k][a], xf[k][b], acc[a][b]);
@@ -161,7 +171,11 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
 
   // Halves: a wave group moves its rows through its own free stage (32 KB), R at a time, so that whole row segments are stored.
   // Floats (DOWN): a quad per lane straight to the slot's row, 64 bytes of a row by four lanes; slot[b] is that of row 16 b + lane % 16.
-  auto epilogue = [&](const Tile& t, const int (&slot)[FM]) {
+  struct Scales {  // E4M3: of the lane's rows and columns
+    float row[FM];
+    floatx4 col[FN];
+  };
+  auto epilogue = [&](const Tile& t, const int (&slot)[FM], const Scales& scales, const half4 (&bias)[FN]) {
     int elane = lane;
     asm volatile("" : "+v"(elane));  // (as in fprop_pp_kernel: the addresses below are not to live through the k loop)
     const int eg = elane >> 4, elr = elane & 15, gtid = wq * 64 + elane, r_half = grp * WTM;
@@ -190,7 +204,13 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
         for (int bb = 0; bb < R / 16; ++bb) {
           const int b = sp * (R / 16) + bb, srow = bb * 16 + elr, nl = column(a, eg);
           floatx4 v = acc[a][b];
-          if constexpr (MODE == ROWS_DENSE) v *= p.alpha;
+          if constexpr (WT == WEIGHTS_F8) {
+            v *= scales.col[a] * scales.row[b];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = p.alpha * v[e] + p.beta * (float)bias[a][e];
+          } else if constexpr (MODE == ROWS_DENSE) {
+            v *= p.alpha;
+          }
           v = apply_act4(v, p.act);
           if constexpr (GATED) v *= acc[a + 1][b];
           half4 o;
@@ -215,7 +235,7 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
   if (tile >= total) return;
   cur = find_tile(tile);
   setup_tile(cur, MODE == ROWS_UP ? find_row(cur) : 0);
-  load_bias(cur);
+  if constexpr (WT != WEIGHTS_F8) load_bias(cur);
   issue_first_tiles();
   while (true) {
     const bool more = tile + (int)gridDim.x < total;
@@ -226,13 +246,13 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
     if (grp == 0) wait_loads_0();
     else wait_loads_x();
     wait_reads();
-    const float bias_scale = MODE == ROWS_DENSE ? p.beta / p.alpha : 1.f;  // (the host keeps it finite)
+    const float bias_scale = WT == WEIGHTS_F8 ? 0.f : MODE == ROWS_DENSE ? p.beta / p.alpha : 1.f;  // (the host keeps it finite)
 #pragma unroll
     for (int a = 0; a < FN; ++a)
 #pragma unroll
       for (int b = 0; b < FM; ++b)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[a][b][e] = (float)bias_q[a][e] * bias_scale;
+        for (int e = 0; e < 4; ++e) acc[a][b][e] = WT == WEIGHTS_F8 ? 0.f : (float)bias_q[a][e] * bias_scale;
     raw_barrier();
     if (grp == 1) raw_barrier();
     int ws_cur = 0, xs_cur = 0;
@@ -272,21 +292,37 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
         slot[b] = p.order[cur.row0 + (r < cur.rows ? r : cur.rows - 1)];
       }
     }
+    Scales scales;
+    half4 bias[FN];
+    if constexpr (WT == WEIGHTS_F8) {
+      load_bias(cur);
+#pragma unroll
+      for (int a = 0; a < FN; ++a) {
+        const int c = cur.c0 + column(a, g);
+        bias[a] = bias_q[a];
+        scales.col[a] = column_scales(p, c < outputs ? c : 0);
+      }
+#pragma unroll
+      for (int b = 0; b < FM; ++b) {
+        const int r = grp * WTM + b * 16 + lr;
+        scales.row[b] = p.x_scales ? p.x_scales[cur.row0 + (r < cur.rows ? r : cur.rows - 1)] : 1.f;
+      }
+    }
     if (more) {
       setup_tile(next, next_row);
-      load_bias(next);
+      if constexpr (WT != WEIGHTS_F8) load_bias(next);
       issue_first_tiles();
     }
-    epilogue(cur, slot);
+    epilogue(cur, slot, scales, bias);
     tile += gridDim.x;
     cur = next;
     if (!more) break;
   }
 }
 
-template <int MODE, bool GATED>
+template <int MODE, bool GATED, int WT = WEIGHTS_F16>
 hipError_t launch_moe_pp(RowsParams p, hipStream_t stream) {
-  auto kern = moe_pp_kernel<MODE, GATED>;
+  auto kern = moe_pp_kernel<MODE, GATED, WT>;
   static LdsOptIn opt_in;
   if (hipError_t e = opt_in.ensure((const void*)kern, FpropPpTraits::LDS_BYTES); e != hipSuccess) return e;
   constexpr int COLS = GATED ? FpropPpTraits::BN / 2 : FpropPpTraits::BN, kComputeUnits = 256;

@@ -4,7 +4,9 @@
 
 namespace bolt {
 
-enum { WEIGHTS_F16 = 0, WEIGHTS_W4 = 1 };
+// WEIGHTS_F8: weights and activations in E4M3.  They move as the halves that two of them fill, so lengths of rows and reductions count those
+// pairs; two pieces of an FP16 operand make one of v_mfma_f32_16x16x128_f8f6f4.
+enum { WEIGHTS_F16 = 0, WEIGHTS_W4 = 1, WEIGHTS_F8 = 2 };
 // Where a product's rows come from and go to.
 //   DENSE: row m of x, to row m of y.
 //   UP:    rows of the routed list: token order[i] / top_k of x, to row i of y (the list's order).
@@ -54,6 +56,15 @@ struct RowsParams {
   int row_blocks, col_blocks;
   const half_t* unpacked;      // [N][K], for the marks of w4_unpack_kernel
   int walk;                    // tiles of columns that a workgroup walks over
+  const float* x_scales;       // E4M3: of the rows of x and of w, or null
+  const float* w_scales;
+  const half_t* add;           // [M][N] (ldadd), added to the sums before alpha, or null (linear layers of 4-bit weights, more than 16 rows)
+  int64_t ldadd;
+  // low-rank adapters (linear layers of up to 16 rows)
+  const int* adapter;          // of each row; none below zero and from `adapters` on
+  const half_t* low;           // [M][rank]: scale * x . down^T of each row's adapter
+  const half_t* up;            // [adapters][N][rank]
+  int adapters, rank;
 };
 
 // The experts' row blocks: each expert's list rows in blocks of B, counted expert by expert.
@@ -109,6 +120,27 @@ __device__ __forceinline__ bool find_row_block(const int* __restrict__ offsets, 
     first += blocks;
     ++e;
   }
+}
+
+// The adapter of a row, -1 for none; `exists`: the row does.
+__device__ __forceinline__ int row_adapter(const int* ids, int adapters, int row, bool exists) {
+  const int id = exists ? ids[row] : -1;
+  return id >= 0 && id < adapters ? id : -1;
+}
+
+// The 16 x 16 x 128 form for E4M3: lane l supplies 32 values of row (column) l % 16, the same 32 of the reduction on both sides; the
+// result lies as with the 16 x 16 x 32 form.  Twice the operations per cycle of FP16.
+__device__ __forceinline__ floatx4 mfma_16x16x128_f8(half8 a0, half8 a1, half8 b0, half8 b1, floatx4 c) {
+  typedef int intx8 __attribute__((ext_vector_type(8)));
+  typedef half_t half16 __attribute__((ext_vector_type(16)));
+  const half16 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
+  const half16 b = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
+  // (no scales, both formats 0: E4M3)
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(intx8, a), __builtin_bit_cast(intx8, b), c, 0, 0, 0, 0, 0, 0);
+}
+// The scales of four columns.
+__device__ __forceinline__ floatx4 column_scales(const RowsParams& p, int n) {
+  return p.w_scales ? *(const floatx4*)(p.w_scales + n) : floatx4{1.f, 1.f, 1.f, 1.f};
 }
 
 // Direct-to-LDS loads from any address: lane l's 16 (4) bytes go to `to` + 16 l (4 l).

@@ -125,6 +125,19 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
         for_constants<NG>([&](auto i) { scale[t][i] = *(const half4*)(scales + t * NG * 16 + (w.g * NG + decltype(i)::value) * 4); });
       });
     }
+    if constexpr (WT == WEIGHTS_F8) {
+      half8 x[MB][2];
+      for_constants<MB>([&](auto b) {
+        for_constants<2>([&](auto s) {
+          x[b][s] = *(const half8*)(xs + dma_chunk_offset<64>(decltype(b)::value * 16 + w.l16, decltype(s)::value * 4 + w.g));
+        });
+      });
+      for_constants<R>([&](auto t) {
+        const half8 a0 = *(const half8*)(mine + t * 1024 + lane * 8), a1 = *(const half8*)(mine + t * 1024 + 512 + lane * 8);
+        for_constants<MB>([&](auto b) { acc[t][b] = mfma_16x16x128_f8(a0, a1, x[b][0], x[b][1], acc[t][b]); });
+      });
+      return;
+    }
     floatx4 sum[R][MB];
     for_constants<KS>([&](auto sc) {
       constexpr int s = decltype(sc)::value;
@@ -201,6 +214,14 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
         for (int e = 0; e < 4; ++e) v[e] = p.alpha * v[e] + p.beta * (float)hb[e];
         return v;
       };
+      if constexpr (WT == WEIGHTS_F8) acc[a][b] *= column_scales(p, col) * (p.x_scales ? p.x_scales[w.row0 + j] : 1.f);
+      if constexpr (WT == WEIGHTS_W4 && MODE == ROWS_DENSE) {
+        if (p.add) {
+          const half4 more = *(const half4*)(p.add + to * p.ldadd + col);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[a][b][e] += (float)more[e];
+        }
+      }
       floatx4 v = with_bias(acc[a][b], col);
       v = apply_act4(v, p.act);
       if constexpr (GATED) v *= with_bias(acc[a + 1][b], p.hidden + col);
