@@ -178,7 +178,7 @@ struct RowsWave {
     static_assert(MB == 1, "one block of 16 rows");
     const int mine = row_adapter(p.adapter, p.adapters, row0 + l16, l16 < rows);
     unsigned left = (unsigned)__ballot(mine >= 0) & 0xffffu;
-    const half_t* const low = p.low + (int64_t)(row0 + (l16 < rows ? l16 : rows - 1)) * p.rank + g * 8;
+    const float* const low = p.low + (int64_t)(row0 + (l16 < rows ? l16 : rows - 1)) * p.rank + g * 8;
     for (int turn = 0; left != 0; ++turn) {
       const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
       left &= ~(unsigned)__ballot(mine == a);
@@ -188,7 +188,7 @@ struct RowsWave {
       for (int k = 0; k < p.rank; k += 32) {
         const bool in = k + g * 8 < p.rank;
         const int at = in ? k : -g * 8;
-        const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0}, b = *(const half8*)(low + at);
+        const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0}, b = low_operand(low + at, p.low_parts, (int64_t)p.M * p.rank);
 #pragma unroll
         for (int t = 0; t < R; ++t) {
           const int n = col0 + t * 16 + l16;
@@ -279,12 +279,15 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
     w.template load_rows<false>(wave + i * NW, xf[decltype(b)::value]);
   };
   auto multiply = [&](auto b) { w.template multiply<false>(0, wf[decltype(b)::value], xf[decltype(b)::value], acc); };
-  auto adapters = [&] {
-    if constexpr (LORA) w.template add_adapters<NW>(col0, wave, acc);
+  // The adapters' operands are asked for behind the first steps' and multiplied while those arrive.  (Sixteen waves have 128 registers each, too few
+  // for that: there they come last.)
+  auto adapters = [&](bool last) {
+    if constexpr (LORA)
+      if (last == (NW == 16)) w.template add_adapters<NW>(col0, wave, acc);
   };
   if (n >= NB) {
     for_constants<NB>([&](auto b) { load(decltype(b)::value, b); });
-    adapters();
+    adapters(false);
     int c = 0;
     for (; c + 2 * NB <= n; c += NB)
       for_constants<NB>([&](auto b) {
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
     for_constants<NB>([&](auto b) {
       if (decltype(b)::value < n) load(decltype(b)::value, b);
     });
-    adapters();
+    adapters(false);
     for_constants<NB>([&](auto b) {
       if (decltype(b)::value < n) multiply(b);
     });
@@ -313,6 +316,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
     w.template load_rows<true>(whole, xf[0]);
     w.template multiply<true>(whole, wf[0], xf[0], acc);
   }
+  adapters(true);
   w.put_sums(part, wave, acc);
   __syncthreads();
   w.template finish<NW>(part, col0, tid);
@@ -385,6 +389,14 @@ __global__ __launch_bounds__(64 * NW, WT == WEIGHTS_W4 && MODE != ROWS_DENSE && 
   } else {
     tile(it, S0{});
   }
+}
+
+// Tiles of 16 weight rows for a workgroup of a linear layer with FP16 or E4M3 weights, 1 or 2: whichever gives a compute unit fewer of them, 2 if
+// that is alike, since half as many workgroups then read the activations.  us, E4M3, 1 and 16 rows, 1 / 2 tiles: 4096 x 4096 5.7 and 6.2 / 6.7 and 7.9;
+// 6152 x 5008 9.7 and 13.3 / 9.5 and 11.2; 12288 x 4096 11.4 and 14.2 / 13.3 and 15.3; 1024 x 8192 6.8 and 9.5 / 10.3 and 12.9.
+inline int few_rows_tiles(int N) {
+  const int64_t one = (N + 16 * 256 - 1) / (16 * 256), two = (N + 32 * 256 - 1) / (32 * 256) * 2;
+  return one < two ? 1 : 2;
 }
 
 template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NB, bool LORA = false>

@@ -9,6 +9,8 @@ static hipError_t launch(const RowsParams& p, hipStream_t stream) {
   if (n == 1) return launch_few_rows_walk<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 1, LORA>(p, stream);
   if (n == 2) return launch_few_rows_walk<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 2, LORA>(p, stream);
   if (n <= 4) return launch_few_rows_walk<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 4, LORA>(p, stream);
+  if constexpr (MODE == ROWS_DENSE)
+    if (few_rows_tiles(p.N) == 1) return launch_few_rows<WEIGHTS_F16, MODE, GATED, 1, 1, 8, 3, LORA>(p, stream);
   return launch_few_rows<WEIGHTS_F16, MODE, GATED, 1, 2, 8, 3, LORA>(p, stream);
 }
 hipError_t launch_few_rows_f16(const RowsParams& p, int mode, bool gated, hipStream_t stream) {

@@ -9,6 +9,8 @@ namespace bolt {
 namespace {
 
 constexpr int kMaxRank = 128, kFewRows = 16;
+// Workgroups of 16 rows from which low's reduction is not split any more, and into how many parts at most.
+constexpr int kDownGroups = 128, kMostParts = kMostLowParts;
 
 bolt_gemm_w4_desc base_w4(const bolt_gemm_lora_desc& d) { return {d.M, d.N, d.K, d.lda, d.ldd, d.group, d.alpha, d.beta, d.act}; }
 
@@ -28,14 +30,15 @@ bolt_status check_gemm_lora(const bolt_gemm_lora_desc* d) {
   return BOLT_OK;
 }
 
-// The workspace: low [M][rank]; of 4-bit weights that may be unpacked the unpacked ones and the adapters' share [M][N] (which otherwise goes through D:
+// The workspace: low [parts][M][rank]; of 4-bit weights that may be unpacked the unpacked ones and the adapters' share [M][N] (which otherwise goes through D:
 // there the rows with weights beyond FP16's range are computed a second time).
 struct LoraWorkspace {
   int64_t weights_at, share_at, bytes;
 };
 LoraWorkspace lora_workspace(const bolt_gemm_lora_desc& d) {
   LoraWorkspace w;
-  w.weights_at = w.share_at = w.bytes = round_up((int64_t)d.M * d.rank * 2, 256);
+  // (a bound of parts * M that does not fall as M grows)
+  w.weights_at = w.share_at = w.bytes = round_up(std::max<int64_t>(d.M, std::min<int64_t>((int64_t)kMostParts * d.M, 16 * kDownGroups)) * d.rank * 4, 256);
   if (d.weights == BOLT_WEIGHTS_W4) {
     const bolt_gemm_w4_desc base = base_w4(d);
     if (const size_t unpacked = bolt_gemm_w4_workspace_bytes(&base); unpacked > 0) {
@@ -46,30 +49,41 @@ LoraWorkspace lora_workspace(const bolt_gemm_lora_desc& d) {
   return w;
 }
 
-template <int RT, int NW, int U, bool SPREAD>
+// Over how many workgroups a block's adapters are dealt: as many as the block can have where the launch has few workgroups.
+int turns_of(const LoraParams& p, int block_rows, int64_t workgroups) {
+  const int64_t most = std::min<int64_t>(std::min(block_rows, p.M), p.adapters);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, 2048 / workgroups));
+}
+
+template <int RT, int NW, int S>
 hipError_t launch_down(LoraParams p, hipStream_t stream) {
-  auto kern = lora_down_kernel<RT, NW, U, SPREAD>;
-  constexpr int LDS_BYTES = NW * RT * 1024;
+  auto kern = lora_down_kernel<RT, NW, S>;
+  constexpr int LDS_BYTES = NW * S * (2 + 2 * RT) * 1024;
+  static_assert(LDS_BYTES <= 160 * 1024 && NW * RT * 1024 <= LDS_BYTES, "stages; the sums take their place");
   static LdsOptIn opt_in;
   if (hipError_t e = opt_in.ensure((const void*)kern, LDS_BYTES); e != hipSuccess) return e;
-  p.blocks = (p.M + 15) / 16;
+  const int blocks = p.blocks = (p.M + 15) / 16;
   p.tiles = (p.rank + 16 * RT - 1) / (16 * RT);
-  hipLaunchKernelGGL(kern, dim3(SPREAD ? p.blocks * p.tiles * 16 : p.blocks), dim3(64 * NW), LDS_BYTES, stream, p);
+  p.turns = turns_of(p, 16, (int64_t)blocks * p.tiles * p.parts);
+  hipLaunchKernelGGL(kern, dim3(blocks * p.tiles * p.turns * p.parts), dim3(64 * NW), LDS_BYTES, stream, p);
   return hipGetLastError();
 }
+int low_parts(int M) { return std::max(1, std::min(kMostParts, kDownGroups / ((M + 15) / 16))); }
 hipError_t launch_lora_down(const LoraParams& p, hipStream_t stream) {
-  if (p.M <= 64) return launch_down<1, 16, 4, true>(p, stream);
-  if (p.rank <= 16) return launch_down<1, 8, 4, false>(p, stream);
-  if (p.rank <= 32) return launch_down<2, 8, 2, false>(p, stream);
-  if (p.rank <= 64) return launch_down<4, 8, 2, false>(p, stream);
-  return launch_down<8, 8, 1, false>(p, stream);
+  if (p.M <= 64 || p.rank <= 16) return launch_down<1, 4, 4>(p, stream);
+  if (p.rank <= 32) return launch_down<2, 4, 4>(p, stream);
+  if (p.rank <= 64) return launch_down<4, 4, 4>(p, stream);
+  return launch_down<8, 4, 2>(p, stream);
 }
-hipError_t launch_lora_up(LoraParams p, hipStream_t stream) {
-  p.blocks = (p.M + 63) / 64;
+template <int MB>
+hipError_t launch_up(LoraParams p, hipStream_t stream) {
+  const int blocks = p.blocks = (p.M + 16 * MB - 1) / (16 * MB);
   p.tiles = (p.N + 255) / 256;
-  hipLaunchKernelGGL(lora_up_kernel, dim3(p.blocks * p.tiles), dim3(256), 0, stream, p);
+  p.turns = turns_of(p, 16 * MB, (int64_t)blocks * p.tiles);
+  hipLaunchKernelGGL(lora_up_kernel<MB>, dim3(blocks * p.tiles * p.turns), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
+hipError_t launch_lora_up(const LoraParams& p, hipStream_t stream) { return p.M <= 64 ? launch_up<1>(p, stream) : launch_up<4>(p, stream); }
 
 }  // namespace
 }  // namespace bolt
@@ -102,7 +116,9 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
   l.x = (const half_t*)A; l.ldx = d.lda;
   l.adapter = (const int*)ids;
   l.down = (const half_t*)down; l.up = (const half_t*)up; l.scales = (const float*)scales;
-  l.low = (half_t*)workspace;
+  l.low = (float*)workspace;
+  l.none = none;
+  l.parts = low_parts(d.M);
   l.M = d.M; l.N = d.N; l.K = d.K; l.adapters = d.adapters; l.rank = d.rank;
   if (launch_lora_down(l, st) != hipSuccess) return BOLT_ERR_LAUNCH;
   if (d.M <= kFewRows) {
@@ -119,7 +135,7 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
       p.M = d.M; p.N = d.N; p.K = d.K; p.steps = (d.K + 63) / 64;
       p.alpha = d.alpha; p.beta = d.beta; p.act = d.act;
     }
-    p.adapter = l.adapter; p.low = l.low; p.up = l.up; p.adapters = d.adapters; p.rank = d.rank;
+    p.adapter = l.adapter; p.low = l.low; p.up = l.up; p.adapters = d.adapters; p.rank = d.rank; p.low_parts = l.parts;
     return status_of(w4 ? launch_few_rows_w4_lora(p, d.group, st) : launch_few_rows_f16_lora(p, st));
   }
   const bool apart = ws.share_at != ws.weights_at;

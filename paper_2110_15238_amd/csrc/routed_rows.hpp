@@ -60,11 +60,11 @@ struct RowsParams {
   const float* w_scales;
   const half_t* add;           // [M][N] (ldadd), added to the sums before alpha, or null (linear layers of 4-bit weights, more than 16 rows)
   int64_t ldadd;
-  // low-rank adapters (linear layers of up to 16 rows)
+  // low-rank adapters (linear layers)
   const int* adapter;          // of each row; none below zero and from `adapters` on
-  const half_t* low;           // [M][rank]: scale * x . down^T of each row's adapter
+  const float* low;            // [low_parts][M][rank]: their sum is scale * x . down^T of each row's adapter
   const half_t* up;            // [adapters][N][rank]
-  int adapters, rank;
+  int adapters, rank, low_parts;
 };
 
 // The experts' row blocks: each expert's list rows in blocks of B, counted expert by expert.
@@ -128,6 +128,33 @@ __device__ __forceinline__ int row_adapter(const int* ids, int adapters, int row
   return id >= 0 && id < adapters ? id : -1;
 }
 
+// Eight values of a row of low, which is `parts` FP32 sums `part` floats apart, as the FP16 operand of the product with up.  All parts are asked
+// for at once.
+constexpr int kMostLowParts = 4;
+__device__ __forceinline__ half8 low_operand(const float* low, int parts, int64_t part) {
+  floatx4 a = *(const floatx4*)low, b = *(const floatx4*)(low + 4);
+  if (parts > 1) {
+    floatx4 more[kMostLowParts - 1][2];
+#pragma unroll
+    for (int i = 1; i < kMostLowParts; ++i) {
+      const float* const from = low + (i < parts ? i : 0) * part;
+      more[i - 1][0] = *(const floatx4*)from;
+      more[i - 1][1] = *(const floatx4*)(from + 4);
+    }
+#pragma unroll
+    for (int i = 1; i < kMostLowParts; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        a[e] = i < parts ? a[e] + more[i - 1][0][e] : a[e];
+        b[e] = i < parts ? b[e] + more[i - 1][1][e] : b[e];
+      }
+  }
+  half8 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = (half_t)a[e], o[4 + e] = (half_t)b[e];
+  return o;
+}
+
 // The 16 x 16 x 128 form for E4M3: lane l supplies 32 values of row (column) l % 16, the same 32 of the reduction on both sides; the
 // result lies as with the 16 x 16 x 32 form.  Twice the operations per cycle of FP16.
 __device__ __forceinline__ floatx4 mfma_16x16x128_f8(half8 a0, half8 a1, half8 b0, half8 b1, floatx4 c) {
@@ -149,6 +176,18 @@ __device__ __forceinline__ void lds_load16(const void* from, half_t* to) {
 }
 __device__ __forceinline__ void lds_load4(const void* from, half_t* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, BOLT_LDS_PTR(to), 4, 0, 0);
+}
+
+// Waits of a wave that stages for itself: its direct-to-LDS loads but for the VM newest have landed; its LDS reads have returned.
+template <int VM>
+__device__ __forceinline__ void wave_waits_for_loads() {
+  static_assert(VM >= 0 && VM < 64, "vmcnt is a 6-bit counter");
+  __builtin_amdgcn_s_waitcnt((VM & 0xF) | ((VM >> 4) << 14) | 0x0F70);
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wave_waits_for_reads() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("" ::: "memory");
 }
 
 // Workgroup ids are dealt round-robin over 8 XCDs: every XCD gets a contiguous run of the `total` tiles.

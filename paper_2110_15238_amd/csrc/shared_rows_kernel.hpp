@@ -83,6 +83,22 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
       xat[j] = r < w.rows ? (unsigned)from * (unsigned)(p.ldx * 2) : kInvalidOffset;
     }
   }
+  // FP16, E4M3: a tile of 16 weight rows and 64 columns is two pieces of 8 whole lines, swizzled as the activations are.  (Pieces of 16 rows x 64
+  // bytes, in the order of the operand, come out of an L2 at a third of the rate.)
+  const unsigned char* wline[R][2];
+  int wchunk[2];
+  if constexpr (!T::W4) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = h * 8 + lrow;
+      wchunk[h] = (lane & 7) ^ dma_swizzle<64>(r);
+#pragma unroll
+      for (int t = 0; t < R; ++t) {
+        const int row = w.first_row(col0, t) + r;
+        wline[t][h] = p.w + w.expert * p.w_stride + (int64_t)(row < p.N ? row : p.N - 1) * p.K * 2;
+      }
+    }
+  }
   half_t* const ring = lds + kg * S * T::STAGE;
 
   // ---- steps kg, kg + KG, ...: every set of waves runs `turns` of them; one past the end is not multiplied -------------------
@@ -95,9 +111,10 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
       if constexpr (T::W4) {
         lds_load16(w.wrow[t] + (int64_t)at * W4Format::BLOCK_BYTES, mine + t * 512);
       } else {
-        for_constants<KS>([&](auto sc) {
-          const int k = at * 64 + decltype(sc)::value * 32;  // (beyond K: zeros; an infinite weight would make a NaN of the zero it meets)
-          lds_load16(k + w.g * 8 < p.K ? w.wrow[t] + (int64_t)k * 2 : (const unsigned char*)p.none, mine + (t * KS + decltype(sc)::value) * 512);
+        for_constants<2>([&](auto hc) {
+          constexpr int h = decltype(hc)::value;
+          const int k = at * 64 + wchunk[h] * 8;  // (beyond K: zeros; an infinite weight would make a NaN of the zero it meets)
+          lds_load16(k < p.K ? wline[t][h] + (int64_t)k * 2 : (const unsigned char*)p.none, mine + (t * 2 + h) * 512);
         });
       }
     });
@@ -133,7 +150,8 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
         });
       });
       for_constants<R>([&](auto t) {
-        const half8 a0 = *(const half8*)(mine + t * 1024 + lane * 8), a1 = *(const half8*)(mine + t * 1024 + 512 + lane * 8);
+        const half8 a0 = *(const half8*)(mine + t * 1024 + dma_chunk_offset<64>(w.l16, w.g));
+        const half8 a1 = *(const half8*)(mine + t * 1024 + dma_chunk_offset<64>(w.l16, 4 + w.g));
         for_constants<MB>([&](auto b) { acc[t][b] = mfma_16x16x128_f8(a0, a1, x[b][0], x[b][1], acc[t][b]); });
       });
       return;
@@ -158,7 +176,7 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
               for (int e = 0; e < 4; ++e) acc[t][b][e] += (float)scale[t][i][e] * sum[t][b][e];
             });
         } else {
-          const half8 a = *(const half8*)(mine + (t * KS + s) * 512 + lane * 8);
+          const half8 a = *(const half8*)(mine + t * 1024 + dma_chunk_offset<64>(w.l16, s * 4 + w.g));
           for_constants<MB>([&](auto b) { acc[t][b] = mfma_16x16x32(a, x[b], acc[t][b]); });
         }
       });
