@@ -39,6 +39,8 @@ hipError_t launch_rows_f8(const RowsParams& p, TileF8 tile, hipStream_t stream);
 // Linear layers of up to 16 rows whose sums take the rows' adapters (adapter, low, up, adapters, rank).
 hipError_t launch_few_rows_f16_lora(const RowsParams& p, hipStream_t stream);
 hipError_t launch_few_rows_w4_lora(const RowsParams& p, int group, hipStream_t stream);
+// The same for many rows, on 256 x 256 tiles.
+hipError_t launch_many_rows_f16_lora(const RowsParams& p, hipStream_t stream);
 
 // bolt_gemm_w4 behind its checks; `add` (M x N, ldadd, or null): added to A . W^T before alpha, from 17 rows on (csrc/moe_api.hip).
 bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d);

@@ -178,7 +178,7 @@ struct RowsWave {
     static_assert(MB == 1, "one block of 16 rows");
     const int mine = row_adapter(p.adapter, p.adapters, row0 + l16, l16 < rows);
     unsigned left = (unsigned)__ballot(mine >= 0) & 0xffffu;
-    const float* const low = p.low + (int64_t)(row0 + (l16 < rows ? l16 : rows - 1)) * p.rank + g * 8;
+    const int64_t low = (int64_t)(row0 + (l16 < rows ? l16 : rows - 1)) * p.rank + g * 8;
     for (int turn = 0; left != 0; ++turn) {
       const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
       left &= ~(unsigned)__ballot(mine == a);
@@ -188,7 +188,7 @@ struct RowsWave {
       for (int k = 0; k < p.rank; k += 32) {
         const bool in = k + g * 8 < p.rank;
         const int at = in ? k : -g * 8;
-        const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0}, b = low_operand(low + at, p.low_parts, (int64_t)p.M * p.rank);
+        const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0}, b = low_operand(p.low, low + at, p.low_parts, (int64_t)p.M * p.rank);
 #pragma unroll
         for (int t = 0; t < R; ++t) {
           const int n = col0 + t * 16 + l16;

@@ -1,5 +1,6 @@
 // C ABI of projections that are shared by requests with low-rank adapters of their own.
 #include <algorithm>
+#include <cmath>
 
 #include "few_rows_instances.hpp"
 #include "llm_checks.hpp"
@@ -10,7 +11,7 @@ namespace {
 
 constexpr int kMaxRank = 128, kFewRows = 16;
 // Workgroups of 16 rows from which low's reduction is not split any more, and into how many parts at most.
-constexpr int kDownGroups = 128, kMostParts = kMostLowParts;
+constexpr int kDownGroups = 256, kMostParts = kMostLowParts;
 
 bolt_gemm_w4_desc base_w4(const bolt_gemm_lora_desc& d) { return {d.M, d.N, d.K, d.lda, d.ldd, d.group, d.alpha, d.beta, d.act}; }
 
@@ -52,7 +53,7 @@ LoraWorkspace lora_workspace(const bolt_gemm_lora_desc& d) {
 // Over how many workgroups a block's adapters are dealt: as many as the block can have where the launch has few workgroups.
 int turns_of(const LoraParams& p, int block_rows, int64_t workgroups) {
   const int64_t most = std::min<int64_t>(std::min(block_rows, p.M), p.adapters);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, 2048 / workgroups));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / workgroups));
 }
 
 template <int RT, int NW, int S>
@@ -68,11 +69,10 @@ hipError_t launch_down(LoraParams p, hipStream_t stream) {
   hipLaunchKernelGGL(kern, dim3(blocks * p.tiles * p.turns * p.parts), dim3(64 * NW), LDS_BYTES, stream, p);
   return hipGetLastError();
 }
-int low_parts(int M) { return std::max(1, std::min(kMostParts, kDownGroups / ((M + 15) / 16))); }
 hipError_t launch_lora_down(const LoraParams& p, hipStream_t stream) {
   if (p.M <= 64 || p.rank <= 16) return launch_down<1, 4, 4>(p, stream);
-  if (p.rank <= 32) return launch_down<2, 4, 4>(p, stream);
-  if (p.rank <= 64) return launch_down<4, 4, 4>(p, stream);
+  if (p.rank <= 32) return launch_down<2, 4, 3>(p, stream);
+  if (p.rank <= 64) return launch_down<4, 4, 2>(p, stream);
   return launch_down<8, 4, 2>(p, stream);
 }
 template <int MB>
@@ -84,6 +84,17 @@ hipError_t launch_up(LoraParams p, hipStream_t stream) {
   return hipGetLastError();
 }
 hipError_t launch_lora_up(const LoraParams& p, hipStream_t stream) { return p.M <= 64 ? launch_up<1>(p, stream) : launch_up<4>(p, stream); }
+
+// Whether the projection runs on 256 x 256 tiles that add the adapters themselves.  Its sums start at beta / alpha times the bias, which has to be
+// finite, and it addresses the weights with 31-bit offsets.
+bool adds_in_tiles(const bolt_gemm_lora_desc& d) {
+  if (d.alpha == 0.f || !(std::fabs(d.beta) <= 1e30f * std::fabs(d.alpha)) || (int64_t)d.N * d.K * 2 > INT32_MAX) return false;
+  return blocks_of(d.M, 256) * blocks_of(d.N, 256) >= 200;
+}
+// (the tiles read low as halves)
+int low_parts(const bolt_gemm_lora_desc& d) {
+  return d.weights == BOLT_WEIGHTS_F16 && adds_in_tiles(d) ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(kMostParts, kDownGroups / blocks_of(d.M, 16)));
+}
 
 }  // namespace
 }  // namespace bolt
@@ -116,12 +127,13 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
   l.x = (const half_t*)A; l.ldx = d.lda;
   l.adapter = (const int*)ids;
   l.down = (const half_t*)down; l.up = (const half_t*)up; l.scales = (const float*)scales;
-  l.low = (float*)workspace;
+  l.low = workspace;
   l.none = none;
-  l.parts = low_parts(d.M);
+  l.parts = low_parts(d);
   l.M = d.M; l.N = d.N; l.K = d.K; l.adapters = d.adapters; l.rank = d.rank;
   if (launch_lora_down(l, st) != hipSuccess) return BOLT_ERR_LAUNCH;
-  if (d.M <= kFewRows) {
+  const bool few = d.M <= kFewRows, many = !w4 && adds_in_tiles(d);
+  if (few || many) {
     RowsParams p{};
     if (w4) {
       p = dense_w4_rows(base, A, W, bias, D, none);
@@ -136,6 +148,7 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
       p.alpha = d.alpha; p.beta = d.beta; p.act = d.act;
     }
     p.adapter = l.adapter; p.low = l.low; p.up = l.up; p.adapters = d.adapters; p.rank = d.rank; p.low_parts = l.parts;
+    if (many) return status_of(launch_many_rows_f16_lora(p, st));
     return status_of(w4 ? launch_few_rows_w4_lora(p, d.group, st) : launch_few_rows_f16_lora(p, st));
   }
   const bool apart = ws.share_at != ws.weights_at;

@@ -4,8 +4,8 @@
 // Rows come in blocks, and a block takes its adapters one after the other (usually one or two: the rows of a request lie together), over all
 // of its rows: the matrix core's columns are the rows, so what another adapter's rows get is simply not taken.  Where there are few blocks, a
 // block's adapters are dealt over `turns` workgroups, and the reduction of low over `parts` more: one compute unit alone reads some 30 GB/s, so that
-// 128 KB of one adapter take it 4 us.  low stays in FP32 sums, which whoever reads them adds up and rounds to FP16, as every operand of a second
-// product is here.
+// 128 KB of one adapter take it 4 us.  low is rounded to FP16, as every operand of a second product is here; of several parts whoever reads
+// them, which are FP32, adds them up first.
 #pragma once
 #include "routed_rows.hpp"
 
@@ -19,7 +19,7 @@ struct LoraParams {
   const half_t* up;       // [adapters][N][rank]
   const float* scales;    // [adapters], or null: 1
   const half_t* none;     // eight zeros
-  float* low;             // [parts][M][rank]
+  void* low;              // one part: [M][rank] halves, else [parts][M][rank] floats
   half_t* y;              // [M][N] (ldy)
   int64_t ldy;
   int M, N, K, adapters, rank;
@@ -123,7 +123,16 @@ __global__ __launch_bounds__(64 * NW) void lora_down_kernel(const LoraParams p) 
 #pragma unroll
       for (int w = 1; w < NW; ++w) v += *(const floatx4*)(sums + ((w * RT + t) * 64 + at) * 4);
       if (j >= rows || r >= p.rank || row_adapter(p.adapter, p.adapters, row0 + j, true) != a) continue;
-      *(floatx4*)(p.low + ((int64_t)part * p.M + row0 + j) * p.rank + r) = v * scale;
+      v *= scale;
+      const int64_t to = ((int64_t)part * p.M + row0 + j) * p.rank + r;
+      if (p.parts > 1) {
+        *(floatx4*)((float*)p.low + to) = v;
+      } else {
+        half4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (half_t)v[e];
+        *(half4*)((half_t*)p.low + to) = o;
+      }
     }
     __syncthreads();
   });
@@ -144,12 +153,12 @@ __global__ __launch_bounds__(256) void lora_up_kernel(const LoraParams p) {
   if (col0 >= p.N) return;  // (no barriers here)
   const int mine = row_adapter(p.adapter, p.adapters, row0 + lane, lane < rows);
   int of_row[MB];
-  const float* low[MB];
+  int64_t low[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
     const int j = b * 16 + l16;
     of_row[b] = __shfl(mine, j);
-    low[b] = p.low + (int64_t)(row0 + (j < rows ? j : rows - 1)) * p.rank + g * 8;
+    low[b] = (int64_t)(row0 + (j < rows ? j : rows - 1)) * p.rank + g * 8;
   }
   const int from = col0 + (l16 >> 2) * 16 + (l16 & 3);  // + 4 t: the column of this lane's weight row in tile t
   auto store = [&](int a, const floatx4 (&v)[4][MB]) {
@@ -180,7 +189,7 @@ __global__ __launch_bounds__(256) void lora_up_kernel(const LoraParams p) {
         u[t] = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + at);
       }
 #pragma unroll
-      for (int b = 0; b < MB; ++b) l[b] = low_operand(low[b] + at, p.parts, (int64_t)p.M * p.rank);
+      for (int b = 0; b < MB; ++b) l[b] = low_operand(p.low, low[b] + at, p.parts, (int64_t)p.M * p.rank);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll

@@ -24,8 +24,11 @@ namespace bolt {
 
 // WT: WEIGHTS_F8 for linear layers in E4M3 (ROWS_DENSE): bytes move as for FP16, a C phase has half the instructions, each of twice the depth and
 // twice the rate; sums start at zero and are scaled by row and column in the epilogue.
-template <int MODE, bool GATED, int WT = WEIGHTS_F16>
+// LORA (ROWS_DENSE, FP16): the rows' low-rank adapters are added to a tile's sums in front of its epilogue, by the waves' own matrix cores and
+// from global memory: no pass over the outputs.  A wave's sum is taken only where the row's adapter is the one at hand.
+template <int MODE, bool GATED, int WT = WEIGHTS_F16, bool LORA = false>
 __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
+  static_assert(!LORA || (WT == WEIGHTS_F16 && MODE == ROWS_DENSE), "adapters: linear layers with FP16 weights");
   static_assert(WT == WEIGHTS_F16 || (WT == WEIGHTS_F8 && MODE == ROWS_DENSE && !GATED), "E4M3: linear layers");
   using T = FpropPpTraits;
   constexpr int BM = 256, BN = T::BN, BK = T::BK, WTM = BM / 2, WTN = T::WTN;
@@ -171,6 +174,67 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
 
   // Halves: a wave group moves its rows through its own free stage (32 KB), R at a time, so that whole row segments are stored.
   // Floats (DOWN): a quad per lane straight to the slot's row, 64 bytes of a row by four lanes; slot[b] is that of row 16 b + lane % 16.
+  // The adapters of this wave's rows, asked for ahead of the k loop.
+  int mine[2] = {-1, -1};
+  auto find_adapters = [&](const Tile& t) {
+    static_assert(!LORA || WTM == 128, "two rows for each lane");
+#pragma unroll
+    for (int h = 0; h < 2; ++h) mine[h] = row_adapter(p.adapter, p.adapters, t.row0 + grp * WTM + h * 64 + lane, grp * WTM + h * 64 + lane < t.rows);
+  };
+  auto add_adapters = [&](const Tile& t) {
+    int elane = lane;
+    asm volatile("" : "+v"(elane));  // (as in the epilogue)
+    const int eg = elane >> 4, elr = elane & 15, r_half = grp * WTM;
+    unsigned long long left[2] = {__ballot(mine[0] >= 0), __ballot(mine[1] >= 0)};
+    while (left[0] | left[1]) {
+      const int a = left[0] ? __builtin_amdgcn_readlane(mine[0], __builtin_ctzll(left[0])) : __builtin_amdgcn_readlane(mine[1], __builtin_ctzll(left[1]));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) left[h] &= ~__ballot(mine[h] == a);
+      const half_t* const up = p.up + (int64_t)a * p.N * p.rank + eg * 8;
+      const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+      for (int k0 = 0; k0 < p.rank; k0 += 64) {  // (64 ranks at a time: registers)
+        half8 uf[2][FN];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const bool in = k0 + k * 32 + eg * 8 < p.rank;
+#pragma unroll
+          for (int c = 0; c < FN; ++c) {
+            const int n = t.c0 + wq * WTN + c * 16 + elr;
+            const half8 u = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + (in ? k0 + k * 32 : -eg * 8));
+            uf[k][c] = in ? u : zero;
+          }
+        }
+#pragma unroll
+        for (int b0 = 0; b0 < FM; b0 += 4) {
+          __builtin_amdgcn_sched_barrier(0);  // (four row blocks' operands at a time)
+          half8 lf[4][2];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const int r = r_half + (b0 + b) * 16 + elr;
+            const half_t* const low = (const half_t*)p.low + (int64_t)(t.row0 + (r < t.rows ? r : t.rows - 1)) * p.rank + eg * 8;  // (one part)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const bool in = k0 + k * 32 + eg * 8 < p.rank;
+              const half8 l = *(const half8*)(low + (in ? k0 + k * 32 : -eg * 8));
+              lf[b][k] = in ? l : zero;
+            }
+          }
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const int of_row = __shfl(mine[b0 >> 2], b * 16 + elr);
+#pragma unroll
+            for (int c = 0; c < FN; ++c) {
+              floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int k = 0; k < 2; ++k) sum = mfma_16x16x32(uf[k][c], lf[b][k], sum);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[c][b0 + b][e] += of_row == a ? sum[e] : 0.f;
+            }
+          }
+        }
+      }
+    }
+  };
   struct Scales {  // E4M3: of the lane's rows and columns
     float row[FM];
     floatx4 col[FN];
@@ -243,6 +307,7 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
       next = find_tile(tile + gridDim.x);
       if (MODE == ROWS_UP && grp == 1) next_row = find_row(next);
     }
+    if constexpr (LORA) find_adapters(cur);
     if (grp == 0) wait_loads_0();
     else wait_loads_x();
     wait_reads();
@@ -292,6 +357,7 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
         slot[b] = p.order[cur.row0 + (r < cur.rows ? r : cur.rows - 1)];
       }
     }
+    if constexpr (LORA) add_adapters(cur);
     Scales scales;
     half4 bias[FN];
     if constexpr (WT == WEIGHTS_F8) {
@@ -320,9 +386,9 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
   }
 }
 
-template <int MODE, bool GATED, int WT = WEIGHTS_F16>
+template <int MODE, bool GATED, int WT = WEIGHTS_F16, bool LORA = false>
 hipError_t launch_moe_pp(RowsParams p, hipStream_t stream) {
-  auto kern = moe_pp_kernel<MODE, GATED, WT>;
+  auto kern = moe_pp_kernel<MODE, GATED, WT, LORA>;
   static LdsOptIn opt_in;
   if (hipError_t e = opt_in.ensure((const void*)kern, FpropPpTraits::LDS_BYTES); e != hipSuccess) return e;
   constexpr int COLS = GATED ? FpropPpTraits::BN / 2 : FpropPpTraits::BN, kComputeUnits = 256;

@@ -62,7 +62,7 @@ struct RowsParams {
   int64_t ldadd;
   // low-rank adapters (linear layers)
   const int* adapter;          // of each row; none below zero and from `adapters` on
-  const float* low;            // [low_parts][M][rank]: their sum is scale * x . down^T of each row's adapter
+  const void* low;             // scale * x . down^T of each row's adapter: [M][rank] halves, or [low_parts][M][rank] floats to be added up
   const half_t* up;            // [adapters][N][rank]
   int adapters, rank, low_parts;
 };
@@ -128,27 +128,25 @@ __device__ __forceinline__ int row_adapter(const int* ids, int adapters, int row
   return id >= 0 && id < adapters ? id : -1;
 }
 
-// Eight values of a row of low, which is `parts` FP32 sums `part` floats apart, as the FP16 operand of the product with up.  All parts are asked
-// for at once.
+// Eight values from `at` on of low, as the FP16 operand of the product with up: halves where low is one part, else the sums of `parts` floats that
+// are `part` apart, all asked for at once.
 constexpr int kMostLowParts = 4;
-__device__ __forceinline__ half8 low_operand(const float* low, int parts, int64_t part) {
-  floatx4 a = *(const floatx4*)low, b = *(const floatx4*)(low + 4);
-  if (parts > 1) {
-    floatx4 more[kMostLowParts - 1][2];
+__device__ __forceinline__ half8 low_operand(const void* low, int64_t at, int parts, int64_t part) {
+  if (parts == 1) return *(const half8*)((const half_t*)low + at);
+  const float* const sums = (const float*)low + at;
+  floatx4 v[kMostLowParts][2];
 #pragma unroll
-    for (int i = 1; i < kMostLowParts; ++i) {
-      const float* const from = low + (i < parts ? i : 0) * part;
-      more[i - 1][0] = *(const floatx4*)from;
-      more[i - 1][1] = *(const floatx4*)(from + 4);
+  for (int i = 0; i < kMostLowParts; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v[i][h] = *(const floatx4*)(sums + (i < parts ? i : 0) * part + 4 * h);
+  floatx4 a = v[0][0], b = v[0][1];
+#pragma unroll
+  for (int i = 1; i < kMostLowParts; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[e] = i < parts ? a[e] + v[i][0][e] : a[e];
+      b[e] = i < parts ? b[e] + v[i][1][e] : b[e];
     }
-#pragma unroll
-    for (int i = 1; i < kMostLowParts; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        a[e] = i < parts ? a[e] + more[i - 1][0][e] : a[e];
-        b[e] = i < parts ? b[e] + more[i - 1][1][e] : b[e];
-      }
-  }
   half8 o;
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = (half_t)a[e], o[4 + e] = (half_t)b[e];
