@@ -459,7 +459,7 @@ typedef struct {
 } bolt_gemm_q8_desc;
 
 /* A: M x K (lda) bytes, W: N x K bytes; a_scales: M floats, w_scales: N floats, 16-byte aligned, either may be NULL (1 everywhere); bias: N halves or
- * NULL; D: M x N (ldd) FP16.  M may be 0.  The workspace is for sums that several workgroups share. */
+ * NULL; D: M x N (ldd) FP16.  M may be 0.  No layer needs a workspace so far (bolt_gemm_q8_workspace_bytes is 0, workspace may be NULL). */
 bolt_status bolt_gemm_q8(const bolt_gemm_q8_desc* desc, const void* A, const void* a_scales, const void* W, const void* w_scales, const void* bias, void* D,
                          void* workspace, size_t workspace_bytes, void* stream);
 size_t bolt_gemm_q8_workspace_bytes(const bolt_gemm_q8_desc* desc);

@@ -49,6 +49,21 @@ __device__ __forceinline__ floatx4 mfma_16x16x32(half8 a, half8 b, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
+// The forms for E4M3 operands, 32 values a lane in two pieces, the same 32 of the reduction on both sides: lane l supplies row (column) l % 16 or
+// l % 32; the result lies as with the FP16 forms.  Twice the operations per cycle.
+typedef half_t half16 __attribute__((ext_vector_type(16)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ intx8 f8_operand(half8 a, half8 b) {
+  return __builtin_bit_cast(intx8, (half16)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15));
+}
+// (no scales, both formats 0: E4M3)
+__device__ __forceinline__ floatx4 mfma_16x16x128_f8(half8 a0, half8 a1, half8 b0, half8 b1, floatx4 c) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_operand(a0, a1), f8_operand(b0, b1), c, 0, 0, 0, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16 mfma_32x32x64_f8(half8 a0, half8 a1, half8 b0, half8 b1, floatx16 c) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f8_operand(a0, a1), f8_operand(b0, b1), c, 0, 0, 0, 0, 0, 0);
+}
+
 // LDS operand tiles are [rows][BK] halves, K contiguous, addressed in 16-byte chunks of 8 halves.
 // The LDS has 64 banks of 4 bytes; 128-bit accesses are served 16 lanes at a time, so 16 lanes
 // should land in 16 different 16-byte bank groups, bank group = (byte address / 16) mod 16.

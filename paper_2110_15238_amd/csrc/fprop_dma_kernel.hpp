@@ -413,8 +413,9 @@ struct FpropDmaTraits {
 // wave's part on top of what it held.  Every load that the wave has requested has landed behind the last step, but for those of
 // `before_last`, which is called in front of the last MFMAs.
 // G: k-steps of 16 per register set of operand fragments; MOST: LDS reads behind one MFMA.
-template <int BM, int BN, int BK, int WAVES_M, int WAVES_N, int NS, int KG, int G, int MOST, bool WKN, typename XL, typename WL, int FM, int FN,
-          typename BeforeLast>
+// F8: operands of E4M3, moved as the halves that two of them fill; two k-steps make one matrix instruction.
+template <int BM, int BN, int BK, int WAVES_M, int WAVES_N, int NS, int KG, int G, int MOST, bool WKN, bool F8 = false, typename XL, typename WL, int FM,
+          int FN, typename BeforeLast>
 __device__ __forceinline__ void dma_main_loop(XL& xl, WL& wl, half_t* stages, const ConvGeom& cg, int kt_begin, int n_tiles, int wm, int wn, int lane,
                                               floatx16 (&acc)[FN][FM], BeforeLast&& before_last) {
   constexpr int WTM = BM / WAVES_M, WTN = BN / WAVES_N, STAGE = KG * (BM + BN) * BK;
@@ -438,6 +439,7 @@ __device__ __forceinline__ void dma_main_loop(XL& xl, WL& wl, half_t* stages, co
   // k-tiles.
   constexpr int KS = BK / 16, NG = KS / G;  // groups per k-tile
   static_assert(KS % G == 0 && (NG == 1 || NG == 2 || NG == 4), "fragment groups per k-tile; register sets alternate per group");
+  static_assert(!F8 || (G % 2 == 0 && !WKN), "E4M3: pairs of k-steps");
   half8 xf[2][G][FM], wf[2][G][FN];
   // Fragment R (x first) of the reads of group `grp` of the tile in stage `stg`.
   auto read_one = [&](int stg, int grp, auto rc, half8 (&x)[G][FM], half8 (&w)[G][FN]) {
@@ -490,13 +492,14 @@ __device__ __forceinline__ void dma_main_loop(XL& xl, WL& wl, half_t* stages, co
   auto group = [&](auto jc, auto setc, auto readsc, auto loadsc, int kt, bool more) {
     constexpr int j = decltype(jc)::value, cur = decltype(setc)::value, nxt = cur ^ 1, LOADS = decltype(loadsc)::value;
     constexpr bool last = j + 1 == NG;
-    constexpr int MF = G * FM * FN, RD = decltype(readsc)::value ? G * (FM + FN) : 0;
+    constexpr int KM = F8 ? 2 : 1, MF = G / KM * FM * FN, RD = decltype(readsc)::value ? G * (FM + FN) : 0;
     constexpr int S = (j + 1) % NG, L0 = S * L / NG, LD = LOADS ? (S + 1) * L / NG - L0 : 0;
     constexpr int PER = (RD + MF - 1) / MF > MOST ? (RD + MF - 1) / MF : MOST;
     __builtin_amdgcn_sched_barrier(0);
     for_constants<MF>([&](auto mc) {
-      constexpr int I = decltype(mc)::value, k = I / (FM * FN), a = I / FM % FN, b = I % FM;
-      acc[a][b] = mfma_32x32x16(wf[cur][k][a], xf[cur][k][b], acc[a][b]);
+      constexpr int I = decltype(mc)::value, k = I / (FM * FN) * KM, a = I / FM % FN, b = I % FM;
+      if constexpr (F8) acc[a][b] = mfma_32x32x64_f8(wf[cur][k][a], wf[cur][k + 1][a], xf[cur][k][b], xf[cur][k + 1][b], acc[a][b]);
+      else acc[a][b] = mfma_32x32x16(wf[cur][k][a], xf[cur][k][b], acc[a][b]);
       constexpr int r0 = I * PER < RD ? I * PER : RD, r1 = (I + 1) * PER < RD ? (I + 1) * PER : RD;
       for_constants<r1 - r0>([&](auto rc) {
         read_one(stage, last ? 0 : j + 1, std::integral_constant<int, r0 + decltype(rc)::value>{}, xf[nxt], wf[nxt]);

@@ -153,16 +153,6 @@ __device__ __forceinline__ half8 low_operand(const void* low, int64_t at, int pa
   return o;
 }
 
-// The 16 x 16 x 128 form for E4M3: lane l supplies 32 values of row (column) l % 16, the same 32 of the reduction on both sides; the
-// result lies as with the 16 x 16 x 32 form.  Twice the operations per cycle of FP16.
-__device__ __forceinline__ floatx4 mfma_16x16x128_f8(half8 a0, half8 a1, half8 b0, half8 b1, floatx4 c) {
-  typedef int intx8 __attribute__((ext_vector_type(8)));
-  typedef half_t half16 __attribute__((ext_vector_type(16)));
-  const half16 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
-  const half16 b = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
-  // (no scales, both formats 0: E4M3)
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(intx8, a), __builtin_bit_cast(intx8, b), c, 0, 0, 0, 0, 0, 0);
-}
 // The scales of four columns.
 __device__ __forceinline__ floatx4 column_scales(const RowsParams& p, int n) {
   return p.w_scales ? *(const floatx4*)(p.w_scales + n) : floatx4{1.f, 1.f, 1.f, 1.f};
