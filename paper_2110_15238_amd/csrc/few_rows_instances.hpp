@@ -32,8 +32,7 @@ hipError_t launch_shared_rows_w4_marked(const RowsParams& p, int group, hipStrea
 hipError_t launch_many_rows_f16(const RowsParams& p, int mode, bool gated, ManyTile tile, hipStream_t stream);
 
 // Linear layers of E4M3 operands: x, ldx, K and steps in pairs (halves); x_scales, w_scales.
-enum class TileF8 { ROWS32_COLS32, ROWS64_COLS32, ROWS64_COLS64, ROWS128_COLS64, ROWS128_COLS128, ROWS128_COLS256, ROWS256_COLS256 };
-hipError_t launch_few_rows_f8(const RowsParams& p, hipStream_t stream);
+enum class TileF8 { ROWS16_COLS32, ROWS32_COLS32, ROWS64_COLS32, ROWS64_COLS64, ROWS128_COLS64, ROWS128_COLS128, ROWS128_COLS256, ROWS256_COLS256 };
 hipError_t launch_rows_f8(const RowsParams& p, TileF8 tile, hipStream_t stream);
 
 // Linear layers of up to 16 rows whose sums take the rows' adapters (adapter, low, up, adapters, rank).

@@ -159,10 +159,6 @@ struct RowsWave {
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[t][b][e] += (float)scale[e] * sum[b][e];
         }
-      } else if constexpr (WT == WEIGHTS_F8) {
-#pragma unroll
-        for (int b = 0; b < MB; ++b)
-          acc[t][b] = mfma_16x16x128_f8(__builtin_bit_cast(half8, w.piece[t][0]), __builtin_bit_cast(half8, w.piece[t][1]), x.part[0][b], x.part[1][b], acc[t][b]);
       } else {
 #pragma unroll
         for (int s = 0; s < KS; ++s)
@@ -230,9 +226,7 @@ struct RowsWave {
       const int at = i & 63, b = (i >> 6) % MB, t = (i >> 6) / MB;
       const int j = b * 16 + (at & 15), col = col0 + t * 16 + (at >> 4) * 4;
       if (j >= rows || col >= outputs) continue;
-      floatx4 sum = sum_of(GATED ? 2 * t : t, b, at);
-      if constexpr (WT == WEIGHTS_F8) sum *= column_scales(p, col) * (p.x_scales ? p.x_scales[row0 + j] : 1.f);
-      floatx4 v = with_bias(sum, col);
+      floatx4 v = with_bias(sum_of(GATED ? 2 * t : t, b, at), col);
       v = apply_act4(v, p.act);
       if constexpr (GATED) v *= with_bias(sum_of(2 * t + 1, b, at), p.hidden + col);
       if constexpr (MODE == ROWS_DOWN) {
@@ -391,9 +385,9 @@ __global__ __launch_bounds__(64 * NW, WT == WEIGHTS_W4 && MODE != ROWS_DENSE && 
   }
 }
 
-// Tiles of 16 weight rows for a workgroup of a linear layer with FP16 or E4M3 weights, 1 or 2: whichever gives a compute unit fewer of them, 2 if
-// that is alike, since half as many workgroups then read the activations.  us, E4M3, 1 and 16 rows, 1 / 2 tiles: 4096 x 4096 5.7 and 6.2 / 6.7 and 7.9;
-// 6152 x 5008 9.7 and 13.3 / 9.5 and 11.2; 12288 x 4096 11.4 and 14.2 / 13.3 and 15.3; 1024 x 8192 6.8 and 9.5 / 10.3 and 12.9.
+// Tiles of 16 weight rows for a workgroup of a linear layer with FP16 weights, 1 or 2: whichever gives a compute unit fewer of them, 2 if
+// that is alike, since half as many workgroups then read the activations.  us for the same bytes, 1 and 16 rows, 1 / 2 tiles: 4096 x 2048 5.7 and 6.2 / 6.7 and 7.9;
+// 6152 x 2504 9.7 and 13.3 / 9.5 and 11.2; 12288 x 2048 11.4 and 14.2 / 13.3 and 15.3; 1024 x 4096 6.8 and 9.5 / 10.3 and 12.9.
 inline int few_rows_tiles(int N) {
   const int64_t one = (N + 16 * 256 - 1) / (16 * 256), two = (N + 32 * 256 - 1) / (32 * 256) * 2;
   return one < two ? 1 : 2;

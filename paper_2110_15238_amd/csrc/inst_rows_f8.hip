@@ -1,4 +1,4 @@
-// Products of more than 16 rows, E4M3 operands: linear layers.
+// Products of any rows, E4M3 operands: linear layers.
 #include "few_rows_instances.hpp"
 #include "moe_pp_kernel.hpp"
 #include "q8_tile_kernel.hpp"
@@ -7,6 +7,7 @@
 namespace bolt {
 hipError_t launch_rows_f8(const RowsParams& p, TileF8 tile, hipStream_t stream) {
   switch (tile) {
+    case TileF8::ROWS16_COLS32: return launch_shared_rows<WEIGHTS_F8, ROWS_DENSE, false, 1, 1, 1, 2, 4, 3>(p, stream);
     case TileF8::ROWS32_COLS32: return launch_shared_rows<WEIGHTS_F8, ROWS_DENSE, false, 1, 2, 1, 2, 4, 3>(p, stream);
     // rows, columns, waves along either, stages, sets
     case TileF8::ROWS64_COLS32: return launch_q8_tiles<64, 32, 2, 1, 3, 4>(p, stream);
