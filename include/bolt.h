@@ -432,7 +432,7 @@ size_t bolt_gemm_lora_workspace_bytes(const bolt_gemm_lora_desc* desc);
 
 /* v = x + residual, in FP32;  sum = v;  n = v / sqrt(mean(v^2) + eps) * (weight_offset + weight);  y = n;  scales[row] = max |n| / 448,
  * q = n / scale, all from the unrounded v.  A row whose largest |n| is below 2^-118 has zeros for q.  A row that holds an infinity or a NaN has a NaN
- * for its scale, and for all of its q.  Up to 2^31 - 65536 rows of up to 65536 values. */
+ * for its scale, and for all of its q.  Up to 2^31 - 65536 rows of up to 32768 values. */
 typedef struct {
   int32_t rows, width;             /* width a multiple of 8 */
   int32_t ldx, ldr, lds, ldy, ldq; /* row strides of x, residual, sum, y and q in elements, multiples of 8; of those that are not NULL */

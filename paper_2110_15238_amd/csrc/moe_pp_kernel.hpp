@@ -174,17 +174,14 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
 
   // Halves: a wave group moves its rows through its own free stage (32 KB), R at a time, so that whole row segments are stored.
   // Floats (DOWN): a quad per lane straight to the slot's row, 64 bytes of a row by four lanes; slot[b] is that of row 16 b + lane % 16.
-  // The adapters of this wave's rows, asked for ahead of the k loop.
-  int mine[2] = {-1, -1};
-  auto find_adapters = [&](const Tile& t) {
-    static_assert(!LORA || WTM == 128, "two rows for each lane");
-#pragma unroll
-    for (int h = 0; h < 2; ++h) mine[h] = row_adapter(p.adapter, p.adapters, t.row0 + grp * WTM + h * 64 + lane, grp * WTM + h * 64 + lane < t.rows);
-  };
   auto add_adapters = [&](const Tile& t) {
     int elane = lane;
     asm volatile("" : "+v"(elane));  // (as in the epilogue)
     const int eg = elane >> 4, elr = elane & 15, r_half = grp * WTM;
+    static_assert(!LORA || WTM == 128, "two rows for each lane");
+    int mine[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) mine[h] = row_adapter(p.adapter, p.adapters, t.row0 + r_half + h * 64 + elane, r_half + h * 64 + elane < t.rows);
     unsigned long long left[2] = {__ballot(mine[0] >= 0), __ballot(mine[1] >= 0)};
     while (left[0] | left[1]) {
       const int a = left[0] ? __builtin_amdgcn_readlane(mine[0], __builtin_ctzll(left[0])) : __builtin_amdgcn_readlane(mine[1], __builtin_ctzll(left[1]));
@@ -205,11 +202,11 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
           }
         }
 #pragma unroll
-        for (int b0 = 0; b0 < FM; b0 += 4) {
-          __builtin_amdgcn_sched_barrier(0);  // (four row blocks' operands at a time)
-          half8 lf[4][2];
+        for (int b0 = 0; b0 < FM; b0 += 2) {
+          __builtin_amdgcn_sched_barrier(0);  // (two row blocks' operands at a time)
+          half8 lf[2][2];
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
+          for (int b = 0; b < 2; ++b) {
             const int r = r_half + (b0 + b) * 16 + elr;
             const half_t* const low = (const half_t*)p.low + (int64_t)(t.row0 + (r < t.rows ? r : t.rows - 1)) * p.rank + eg * 8;  // (one part)
 #pragma unroll
@@ -220,8 +217,8 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
             }
           }
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            const int of_row = __shfl(mine[b0 >> 2], b * 16 + elr);
+          for (int b = 0; b < 2; ++b) {
+            const int of_row = __shfl(mine[b0 >> 2], (b0 + b) % 4 * 16 + elr);
 #pragma unroll
             for (int c = 0; c < FN; ++c) {
               floatx4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -307,7 +304,6 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
       next = find_tile(tile + gridDim.x);
       if (MODE == ROWS_UP && grp == 1) next_row = find_row(next);
     }
-    if constexpr (LORA) find_adapters(cur);
     if (grp == 0) wait_loads_0();
     else wait_loads_x();
     wait_reads();

@@ -8,7 +8,7 @@
 namespace bolt {
 namespace {
 
-constexpr int kMaxNormWidth = 16 * 64 * 8 * 8;  // 16 waves, eight pieces a lane
+constexpr int kMaxNormWidth = 16 * 64 * 4 * 8;  // 16 waves, four pieces a lane (eight do not fit their 128 registers)
 
 template <int WAVES, int V, bool NORM>
 hipError_t launch(const NormParams& p, hipStream_t stream) {
@@ -27,8 +27,7 @@ hipError_t launch_norm(const NormParams& p, hipStream_t stream) {
   if (chunks <= 512) return launch<4, 2, NORM>(p, stream);
   if (chunks <= 1024) return launch<4, 4, NORM>(p, stream);
   if (chunks <= 2048) return launch<16, 2, NORM>(p, stream);
-  if (chunks <= 4096) return launch<16, 4, NORM>(p, stream);
-  return launch<16, 8, NORM>(p, stream);
+  return launch<16, 4, NORM>(p, stream);
 }
 
 bool strides_ok(int width, std::initializer_list<int> strides) {
