@@ -32,14 +32,16 @@ hipError_t launch_shared_rows_w4_marked(const RowsParams& p, int group, hipStrea
 hipError_t launch_many_rows_f16(const RowsParams& p, int mode, bool gated, ManyTile tile, hipStream_t stream);
 
 // Linear layers of E4M3 operands: x, ldx, K and steps in pairs (halves); x_scales, w_scales.
-enum class TileF8 { ROWS16_COLS32, ROWS32_COLS32, ROWS64_COLS32, ROWS64_COLS64, ROWS128_COLS64, ROWS128_COLS128, ROWS128_COLS256, ROWS256_COLS256 };
-hipError_t launch_rows_f8(const RowsParams& p, TileF8 tile, hipStream_t stream);
+enum class RowsTile { ROWS16_COLS32, ROWS32_COLS32, ROWS64_COLS32, ROWS64_COLS64, ROWS128_COLS64, ROWS128_COLS128, ROWS128_COLS256, ROWS256_COLS256 };
+hipError_t launch_rows_f8(const RowsParams& p, RowsTile tile, hipStream_t stream);
+// Linear layers with FP16 weights, from 64 x 32 to 256 x 256 tiles, that compute the rows' share of their adapters (adapter, low, up, adapters, rank,
+// low_parts; on the largest tiles low is one part), or take it from p.add (not on the largest).
+hipError_t launch_rows_f16_adapters(const RowsParams& p, RowsTile tile, hipStream_t stream);
+hipError_t launch_rows_f16_add(const RowsParams& p, RowsTile tile, hipStream_t stream);
 
 // Linear layers of up to 16 rows whose sums take the rows' adapters (adapter, low, up, adapters, rank).
 hipError_t launch_few_rows_f16_lora(const RowsParams& p, hipStream_t stream);
 hipError_t launch_few_rows_w4_lora(const RowsParams& p, int group, hipStream_t stream);
-// The same for many rows, on 256 x 256 tiles.
-hipError_t launch_many_rows_f16_lora(const RowsParams& p, hipStream_t stream);
 
 // bolt_gemm_w4 behind its checks; `add` (M x N, ldadd, or null): added to A . W^T before alpha, from 17 rows on (csrc/moe_api.hip).
 bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d);

@@ -15,5 +15,4 @@ hipError_t launch_many_rows_f16(const RowsParams& p, int mode, bool gated, ManyT
   if (mode == ROWS_DOWN) return launch<ROWS_DOWN, false>(p, tile, stream);
   return gated ? launch<ROWS_UP, true>(p, tile, stream) : launch<ROWS_UP, false>(p, tile, stream);
 }
-hipError_t launch_many_rows_f16_lora(const RowsParams& p, hipStream_t stream) { return launch_moe_pp<ROWS_DENSE, false, WEIGHTS_F16, true>(p, stream); }
 }  // namespace bolt

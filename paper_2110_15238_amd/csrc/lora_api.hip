@@ -2,8 +2,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "few_rows_instances.hpp"
-#include "llm_checks.hpp"
+#include "layer_tiles.hpp"
 #include "lora_kernel.hpp"
 
 namespace bolt {
@@ -27,7 +26,7 @@ bolt_status check_gemm_lora(const bolt_gemm_lora_desc* d) {
   if (d->lda > kMaxLength || d->ldd > kMaxLength || d->rank > kMaxRank || d->M > kMaxRows) return BOLT_ERR_UNSUPPORTED;
   // the launches of 64 x 256 outputs and of 16 rows here, and those of the projection
   if (!launches(blocks_of(d->M, 16)) || !launches(blocks_of(d->M, 64) * blocks_of(d->N, 256))) return BOLT_ERR_UNSUPPORTED;
-  if (d->weights == BOLT_WEIGHTS_F16 && !launches(blocks_of(d->M, 32) * blocks_of(d->N, 32))) return BOLT_ERR_UNSUPPORTED;
+  if (d->weights == BOLT_WEIGHTS_F16 && !launches(blocks_of(d->M, 32) * blocks_of(d->N, 32))) return BOLT_ERR_UNSUPPORTED;  // (bolt_gemm_epilogue's)
   return BOLT_OK;
 }
 
@@ -85,15 +84,29 @@ hipError_t launch_up(LoraParams p, hipStream_t stream) {
 }
 hipError_t launch_lora_up(const LoraParams& p, hipStream_t stream) { return p.M <= 64 ? launch_up<1>(p, stream) : launch_up<4>(p, stream); }
 
-// Whether the projection runs on 256 x 256 tiles that add the adapters themselves.  Its sums start at beta / alpha times the bias, which has to be
-// finite, and it addresses the weights with 31-bit offsets.
-bool adds_in_tiles(const bolt_gemm_lora_desc& d) {
-  if (d.alpha == 0.f || !(std::fabs(d.beta) <= 1e30f * std::fabs(d.alpha)) || (int64_t)d.N * d.K * 2 > INT32_MAX) return false;
-  return blocks_of(d.M, 256) * blocks_of(d.N, 256) >= 200;
+// ---- which kernels run a projection with FP16 weights on more than 16 rows ----------------------------------------------------
+// A fit to 5 shapes (1024 to 8192 outputs, K 2048 to 11008) x 10 row counts from 17 to 3300, with adapters in the tiles and with their share from memory:
+// the choice takes the best tile of all 50.  us with adapters of rank 32 in runs, 64 x 32, 64 x 64, 128 x 64, 128 x 128, 128 x 256 and 256 x 256: 4096 x 4096, 64
+// rows 16.4 / 21.7 / 24.7 / 39 / 55 / -, 700 rows 79 / 57 / 49 / 39 / 51 / 81, 3300 rows 307 / 212 / 174 / 141 / 114 / 97.
+constexpr LayerTile kLayerTiles[] = {{RowsTile::ROWS64_COLS32, 64, 32, 4, 2.5, 0.70},      {RowsTile::ROWS64_COLS64, 64, 64, 2, 2.2, 0.49},
+                                     {RowsTile::ROWS128_COLS64, 128, 64, 2, 2.0, 0.68},    {RowsTile::ROWS128_COLS128, 128, 128, 1, 1.0, 0.58},
+                                     {RowsTile::ROWS128_COLS256, 128, 256, 1, 0.0, 0.90},  {RowsTile::ROWS256_COLS256, 256, 256, 1, 9.4, 1.26}};
+const LayerTile* projection_tile(const bolt_gemm_lora_desc& d) {
+  const bool bias_in_sum = d.alpha != 0.f && std::fabs(d.beta) <= 1e30f * std::fabs(d.alpha);
+  return layer_tile(kLayerTiles, d.M, d.N, (int64_t)d.K * 2, bias_in_sum);
 }
-// (the tiles read low as halves)
+// Whether the tiles compute the adapters' share.  Where the rows of a request lie together a tile has one or two adapters, which cost it 1 to 3 us (256 x 256:
+// 7); each further one 0.5 (2.4), and how many there are the host does not know: it asks that the most there can be cost no more than the share's way
+// through memory (lora_up_kernel: 6.5 us for 700 x 4104, 38 for 4096 x 8192).
+bool adapters_in_tiles(const bolt_gemm_lora_desc& d, const LayerTile& t) {
+  const double most = std::min(d.adapters, std::min(t.rows, d.M)) * (t.tile == RowsTile::ROWS256_COLS256 ? 2.4 : 0.5);
+  return layer_rounds(t, d.M, d.N) * most <= 3.5 + 1.1e-6 * d.M * d.N;
+}
+// Parts of low's reduction.  (256 x 256 tiles read low as halves.)
 int low_parts(const bolt_gemm_lora_desc& d) {
-  return d.weights == BOLT_WEIGHTS_F16 && adds_in_tiles(d) ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(kMostParts, kDownGroups / blocks_of(d.M, 16)));
+  if (d.weights == BOLT_WEIGHTS_F16 && d.M > kFewRows)
+    if (const LayerTile* t = projection_tile(d); t && t->tile == RowsTile::ROWS256_COLS256) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kMostParts, kDownGroups / blocks_of(d.M, 16)));
 }
 
 }  // namespace
@@ -121,6 +134,8 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
   const bool w4 = d.weights == BOLT_WEIGHTS_W4;
+  const LayerTile* const tile = w4 || d.M <= kFewRows ? nullptr : projection_tile(d);
+  if (!w4 && d.M > kFewRows && !tile) return BOLT_ERR_UNSUPPORTED;
   const bolt_gemm_w4_desc base = base_w4(d);
   const hipStream_t st = (hipStream_t)stream;
   LoraParams l{};
@@ -132,30 +147,31 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
   l.parts = low_parts(d);
   l.M = d.M; l.N = d.N; l.K = d.K; l.adapters = d.adapters; l.rank = d.rank;
   if (launch_lora_down(l, st) != hipSuccess) return BOLT_ERR_LAUNCH;
-  const bool few = d.M <= kFewRows, many = !w4 && adds_in_tiles(d);
-  if (few || many) {
-    RowsParams p{};
-    if (w4) {
-      p = dense_w4_rows(base, A, W, bias, D, none);
-    } else {
-      p.x = (const half_t*)A; p.ldx = d.lda;
-      p.w = (const unsigned char*)W; p.w_stride = (int64_t)d.N * d.K * 2;
-      p.none = none;
-      p.bias = bias ? (const half_t*)bias : none;
-      p.bias_on = bias ? 1 : 0;
-      p.y = D; p.ldy = d.ldd;
-      p.M = d.M; p.N = d.N; p.K = d.K; p.steps = (d.K + 63) / 64;
-      p.alpha = d.alpha; p.beta = d.beta; p.act = d.act;
-    }
-    p.adapter = l.adapter; p.low = l.low; p.up = l.up; p.adapters = d.adapters; p.rank = d.rank; p.low_parts = l.parts;
-    if (many) return status_of(launch_many_rows_f16_lora(p, st));
-    return status_of(w4 ? launch_few_rows_w4_lora(p, d.group, st) : launch_few_rows_f16_lora(p, st));
+  RowsParams p{};
+  if (w4) {
+    p = dense_w4_rows(base, A, W, bias, D, none);
+  } else {
+    p.x = (const half_t*)A; p.ldx = d.lda;
+    p.w = (const unsigned char*)W; p.w_stride = (int64_t)d.N * d.K * 2;
+    p.none = none;
+    p.bias = bias ? (const half_t*)bias : none;
+    p.bias_on = bias ? 1 : 0;
+    p.y = D; p.ldy = d.ldd;
+    p.M = d.M; p.N = d.N; p.K = d.K; p.steps = (d.K + 63) / 64;
+    p.alpha = d.alpha; p.beta = d.beta; p.act = d.act;
   }
+  p.adapter = l.adapter; p.low = l.low; p.up = l.up; p.adapters = d.adapters; p.rank = d.rank; p.low_parts = l.parts;
+  if (d.M <= kFewRows) return status_of(w4 ? launch_few_rows_w4_lora(p, d.group, st) : launch_few_rows_f16_lora(p, st));
+  if (tile && adapters_in_tiles(d, *tile)) return status_of(launch_rows_f16_adapters(p, tile->tile, st));
   const bool apart = ws.share_at != ws.weights_at;
   l.y = apart ? (half_t*)((char*)workspace + ws.share_at) : (half_t*)D;
   l.ldy = apart ? d.N : d.ldd;
   if (launch_lora_up(l, st) != hipSuccess) return BOLT_ERR_LAUNCH;
   if (w4) return run_gemm_w4(base, A, W, bias, l.y, (int)l.ldy, D, (char*)workspace + ws.weights_at, stream);
+  if (tile->tile != RowsTile::ROWS256_COLS256) {
+    p.add = (const half_t*)D; p.ldadd = d.ldd;
+    return status_of(launch_rows_f16_add(p, tile->tile, st));
+  }
   const bolt_gemm_desc g = {d.M, d.N, d.K, d.lda, d.K, d.ldd, d.alpha, d.beta, d.act, BOLT_LAYOUT_NK};
   return bolt_gemm_epilogue_residual(&g, A, W, bias, D, d.ldd, d.alpha, D, nullptr, nullptr, 0, stream);
 }

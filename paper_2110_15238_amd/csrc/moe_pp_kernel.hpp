@@ -182,53 +182,58 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
     int mine[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) mine[h] = row_adapter(p.adapter, p.adapters, t.row0 + r_half + h * 64 + elane, r_half + h * 64 + elane < t.rows);
+    // One adapter after the other, 64 ranks at a time: its up for all of the wave's row blocks, the rows' low two blocks at a time, the next two on
+    // their way while two are multiplied.
     unsigned long long left[2] = {__ballot(mine[0] >= 0), __ballot(mine[1] >= 0)};
     while (left[0] | left[1]) {
       const int a = left[0] ? __builtin_amdgcn_readlane(mine[0], __builtin_ctzll(left[0])) : __builtin_amdgcn_readlane(mine[1], __builtin_ctzll(left[1]));
 #pragma unroll
       for (int h = 0; h < 2; ++h) left[h] &= ~__ballot(mine[h] == a);
-      const half_t* const up = p.up + (int64_t)a * p.N * p.rank + eg * 8;
+      const half_t* const up = p.up + (int64_t)a * p.N * p.rank;
       const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-      for (int k0 = 0; k0 < p.rank; k0 += 64) {  // (64 ranks at a time: registers)
-        half8 uf[2][FN];
+      for (int k0 = 0; k0 < p.rank; k0 += 64) {
+        const int at[2] = {k0 + eg * 8, k0 + 32 + eg * 8};  // (ranks beyond the last are zero on both sides)
+        half8 uf[2][FN], lf[2][2][2];
+        auto load_low = [&](auto pc) {
+          constexpr int pair = decltype(pc)::value;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const bool in = k0 + k * 32 + eg * 8 < p.rank;
+          for (int b = 0; b < 2; ++b) {
+            const int r = r_half + (pair * 2 + b) * 16 + elr;
+            const half_t* const low = (const half_t*)p.low + (int64_t)(t.row0 + (r < t.rows ? r : t.rows - 1)) * p.rank;  // (one part)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) lf[pair & 1][b][k] = *(const half8*)(low + (at[k] < p.rank ? at[k] : 0));
+          }
+        };
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int c = 0; c < FN; ++c) {
             const int n = t.c0 + wq * WTN + c * 16 + elr;
-            const half8 u = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + (in ? k0 + k * 32 : -eg * 8));
-            uf[k][c] = in ? u : zero;
+            uf[k][c] = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + (at[k] < p.rank ? at[k] : 0));
           }
-        }
+        load_low(std::integral_constant<int, 0>{});
 #pragma unroll
-        for (int b0 = 0; b0 < FM; b0 += 2) {
-          __builtin_amdgcn_sched_barrier(0);  // (two row blocks' operands at a time)
-          half8 lf[2][2];
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int c = 0; c < FN; ++c) uf[k][c] = at[k] < p.rank ? uf[k][c] : zero;
+        for_constants<FM / 2>([&](auto pc) {
+          constexpr int pair = decltype(pc)::value;
+          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (pair + 1 < FM / 2) load_low(std::integral_constant<int, pair + 1>{});
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
-            const int r = r_half + (b0 + b) * 16 + elr;
-            const half_t* const low = (const half_t*)p.low + (int64_t)(t.row0 + (r < t.rows ? r : t.rows - 1)) * p.rank + eg * 8;  // (one part)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const bool in = k0 + k * 32 + eg * 8 < p.rank;
-              const half8 l = *(const half8*)(low + (in ? k0 + k * 32 : -eg * 8));
-              lf[b][k] = in ? l : zero;
-            }
-          }
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int of_row = __shfl(mine[b0 >> 2], (b0 + b) % 4 * 16 + elr);
+            constexpr int h = pair / 2;
+            const int of_row = __shfl(mine[h], (pair * 2 + b) % 4 * 16 + elr);
 #pragma unroll
             for (int c = 0; c < FN; ++c) {
               floatx4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int k = 0; k < 2; ++k) sum = mfma_16x16x32(uf[k][c], lf[b][k], sum);
+              for (int k = 0; k < 2; ++k) sum = mfma_16x16x32(uf[k][c], at[k] < p.rank ? lf[pair & 1][b][k] : zero, sum);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) acc[c][b0 + b][e] += of_row == a ? sum[e] : 0.f;
+              for (int e = 0; e < 4; ++e) acc[c][pair * 2 + b][e] += of_row == a ? sum[e] : 0.f;
             }
           }
-        }
+        });
       }
     }
   };

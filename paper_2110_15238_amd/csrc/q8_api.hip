@@ -1,8 +1,7 @@
 // C ABI of the linear layers whose operands are held in 8 bits.
 #include <algorithm>
 
-#include "few_rows_instances.hpp"
-#include "llm_checks.hpp"
+#include "layer_tiles.hpp"
 
 namespace bolt {
 namespace {
@@ -14,44 +13,18 @@ bolt_status check_gemm_q8(const bolt_gemm_q8_desc* d) {
   return BOLT_OK;
 }
 
-// ---- which kernel runs a layer ------------------------------------------------------------------------
-// More than 16 rows: estimated time in us: a tile's turns of its sets of waves, one workgroup on each of 256 compute units at a time, each turn as long as its own chain
-// of loads, reads and matrix instructions or as its operands take from the L2s (15 TB/s for all); and no less than the weights take from memory.  A fit to 7
-// shapes (1024 to 12288 outputs, K 2048 to 11008) x 7 row counts from 45 to 2048, weights from memory: the choice takes 1.01
-// times the best tile on average, 1.09 at most.  us, 32 x 32, 64 x 32, 64 x 64, 128 x 64, 128 x 128, 128 x 256 and 256 x 256: 4096 x 4096, 45 rows 6.7 /
-// 7.6 / 9.0 / 10.9 / 14.7 / 21 / 37, 333 rows 30 / 20 / 17 / 12.5 / 15.6 / 22 / 38, 2048 rows 184 / 96 / 62 / 49 / 35 / 30 / 41; 12288 x 4096, 1024 rows 302 / 179 / 126 / 91 /
-// 68 / 65 / 46.
-struct LayerTile {
-  TileF8 tile;
-  int rows, cols, sets;
-  double first_us, turn_us;
-};
-constexpr LayerTile kLayerTiles[] = {{TileF8::ROWS32_COLS32, 32, 32, 4, 3.3, 0.39},    {TileF8::ROWS64_COLS32, 64, 32, 4, 2.9, 0.62},
-                                     {TileF8::ROWS64_COLS64, 64, 64, 2, 3.0, 0.48},    {TileF8::ROWS128_COLS64, 128, 64, 2, 3.1, 0.70},
-                                     {TileF8::ROWS128_COLS128, 128, 128, 1, 2.85, 0.53}, {TileF8::ROWS128_COLS256, 128, 256, 1, 3.2, 0.82},
-                                     {TileF8::ROWS256_COLS256, 256, 256, 1, 7.0, 1.24}};
+// Tiles for more than 16 rows.  A fit to 7 shapes (1024 to 12288 outputs, K 2048 to 11008) x 7 row counts from 45 to 2048, weights from memory: the
+// choice takes 1.01 times the best tile on average, 1.09 at most.  us, 32 x 32, 64 x 32, 64 x 64, 128 x 64, 128 x 128, 128 x 256 and 256 x 256: 4096 x 4096, 45
+// rows 6.7 / 7.6 / 9.0 / 10.9 / 14.7 / 21 / 37, 333 rows 30 / 20 / 17 / 12.5 / 15.6 / 22 / 38, 2048 rows 184 / 96 / 62 / 49 / 35 / 30 / 41; 12288 x 4096, 1024 rows 302 /
+// 179 / 126 / 91 / 68 / 65 / 46.
+constexpr LayerTile kLayerTiles[] = {{RowsTile::ROWS32_COLS32, 32, 32, 4, 3.3, 0.39},      {RowsTile::ROWS64_COLS32, 64, 32, 4, 2.9, 0.62},
+                                     {RowsTile::ROWS64_COLS64, 64, 64, 2, 3.0, 0.48},      {RowsTile::ROWS128_COLS64, 128, 64, 2, 3.1, 0.70},
+                                     {RowsTile::ROWS128_COLS128, 128, 128, 1, 2.85, 0.53}, {RowsTile::ROWS128_COLS256, 128, 256, 1, 3.2, 0.82},
+                                     {RowsTile::ROWS256_COLS256, 256, 256, 1, 7.0, 1.24}};
 // Up to 16 rows: whole lines to LDS here too.  Weights that go to registers in the order of the operands (few_rows_kernel) take, 1 and 16 rows, here / so
 // on the better of one and two tiles of 16: 4096 x 4096 5.2 and 5.4 / 5.4 and 6.2; 6152 x 5008 8.2 and 9.5 / 8.9 and 11.2; 12288 x 4096 12.3 and 12.7 /
 // 11.3 and 14.1; 4096 x 11008 13.6 and 14.6 / 12.0 and 13.9; 1024 x 8192 6.8 and 6.9 / 6.9 and 9.3; 12288 x 512 4.4 and 4.3 / 4.2 and 4.4.
-constexpr LayerTile kFewRowsTile = {TileF8::ROWS16_COLS32, 16, 32, 4, 0.0, 0.0};
-double layer_us(const LayerTile& t, int64_t M, int64_t N, int64_t K) {
-  const int64_t blocks = blocks_of(M, t.rows) * blocks_of(N, t.cols), rounds = blocks / 256, rest = blocks % 256;
-  const double bytes = (t.rows + t.cols) * 128.0 * t.sets, turns = (double)blocks_of(blocks_of(K, 128), t.sets);
-  const auto turn = [&](int64_t workgroups) { return std::max(t.turn_us, workgroups * bytes / 15e6); };
-  const double us = t.first_us + turns * (rounds * turn(256) + (rest > 0 ? turn(rest) : 0.0));
-  return std::max(us, 2.5 + N * K / 4.5e6);
-}
-// Whether the tile's launch can be made; the 256 x 256 ones run on one workgroup per compute unit and address W with 31-bit offsets.
-bool layer_launches(const LayerTile& t, int64_t M, int64_t N, int64_t K) {
-  const int64_t blocks = blocks_of(M, t.rows) * blocks_of(N, t.cols);
-  return t.tile == TileF8::ROWS256_COLS256 ? blocks <= INT32_MAX && N * K <= INT32_MAX : launches(blocks);
-}
-const LayerTile* layer_tile(int64_t M, int64_t N, int64_t K) {
-  const LayerTile* best = nullptr;
-  for (const LayerTile& t : kLayerTiles)
-    if (layer_launches(t, M, N, K) && (!best || layer_us(t, M, N, K) < layer_us(*best, M, N, K))) best = &t;
-  return best;
-}
+constexpr RowsTile kFewRowsTile = RowsTile::ROWS16_COLS32;
 
 }  // namespace
 }  // namespace bolt
@@ -72,8 +45,8 @@ bolt_status bolt_gemm_q8(const bolt_gemm_q8_desc* desc, const void* A, const voi
   if (!A || !W || !D) return BOLT_ERR_INVALID_ARG;
   for (const void* at : {A, a_scales, W, w_scales, bias, (const void*)D, (const void*)workspace})
     if (!aligned16(at)) return BOLT_ERR_ALIGNMENT;
-  const LayerTile* const tile = desc->M > 16 ? layer_tile(desc->M, desc->N, desc->K) : &kFewRowsTile;
-  if (!tile) return BOLT_ERR_UNSUPPORTED;
+  const LayerTile* const tile = desc->M > 16 ? layer_tile(kLayerTiles, desc->M, desc->N, desc->K, true) : nullptr;
+  if (desc->M > 16 && !tile) return BOLT_ERR_UNSUPPORTED;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
   RowsParams p{};
@@ -87,7 +60,7 @@ bolt_status bolt_gemm_q8(const bolt_gemm_q8_desc* desc, const void* A, const voi
   p.M = desc->M; p.N = desc->N; p.K = desc->K / 2; p.steps = (int)blocks_of(p.K, 64);
   p.alpha = desc->alpha; p.beta = desc->beta; p.act = desc->act;
   const hipStream_t st = (hipStream_t)stream;
-  return status_of(launch_rows_f8(p, tile->tile, st));
+  return status_of(launch_rows_f8(p, tile ? tile->tile : kFewRowsTile, st));
 }
 
 }  // extern "C"

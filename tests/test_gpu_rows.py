@@ -173,7 +173,7 @@ def test_quantize_rows_special_rows_and_strides(bolt):
 # every tile by its own sizes, whole and ragged reductions, outputs that end inside a tile
 Q8 = [(1, 8, 16), (1, 264, 4096), (3, 1032, 528), (16, 4104, 1040), (13, 200, 11008), (17, 8, 16), (31, 4096, 2064), (45, 6152, 1008), (64, 1000, 4112),
       (100, 8192, 272), (129, 2056, 1040), (257, 4104, 784), (300, 520, 5008), (333, 12288, 144), (513, 1032, 2000), (1000, 3000, 912), (2048, 4096, 528),
-      (2100, 8200, 400)]
+      (2100, 8200, 400), (2050, 8200, 2000)]
 
 
 @pytest.mark.parametrize("M,N,K", Q8)
@@ -192,7 +192,7 @@ def test_gemm_q8(bolt, M, N, K, full, act):
 @pytest.mark.parametrize("act", ["relu", "gelu", "hardswish", "softplus"])
 @pytest.mark.parametrize("M", [5, 70, 2060])
 def test_gemm_q8_activations(bolt, M, act):
-    N, K = (136, 272) if M < 1000 else (8200, 144)
+    N, K = (136, 272) if M < 1000 else (8200, 1040)
     g = _gen(M)
     (A, sa), (W, sw), bias = _q8(g, M, K, std=3.0), _q8(g, N, K, std=0.1), _half(g, N)
     D = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K, act=act), A, sa, W, sw, bias, _nan(M, N))
@@ -200,7 +200,7 @@ def test_gemm_q8_activations(bolt, M, act):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 24, 48), (16, 136, 272), (17, 72, 144), (40, 1032, 1040), (65, 264, 80), (130, 2056, 400), (200, 12288, 272), (400, 4104, 272),
-                                   (700, 4104, 144), (2050, 8200, 272)])
+                                   (700, 4104, 144), (2050, 8200, 272), (2050, 8200, 1040)])
 def test_gemm_q8_is_exact_on_integers(bolt, M, N, K):
     """Small integers and scales that are powers of two: a value in a wrong place, a lost column or a scale of another row shows."""
     g = _gen(M + K)
@@ -217,7 +217,7 @@ def test_gemm_q8_is_exact_on_integers(bolt, M, N, K):
 
 @pytest.mark.parametrize("M", [4, 33, 300, 2060])
 def test_gemm_q8_strides_and_untouched_padding(bolt, M):
-    N, K, lda, ldd = (72, 208, 272, 136) if M < 1000 else (8200, 208, 272, 8264)
+    N, K, lda, ldd = (72, 208, 272, 136) if M < 1000 else (8200, 1040, 1104, 8264)
     g = _gen(M)
     (a, sa), (W, sw) = _q8(g, M, K), _q8(g, N, K)
     A = _nan(M, lda, dtype=F8)
@@ -231,7 +231,7 @@ def test_gemm_q8_strides_and_untouched_padding(bolt, M):
 @pytest.mark.parametrize("M", [9, 40, 200, 2060])
 def test_gemm_q8_rows_and_columns_do_not_meet(bolt, M):
     """A NaN in a row or in its scale spoils that row only, one in a weight row that column only."""
-    N, K = (136, 272) if M < 1000 else (8200, 272)
+    N, K = (136, 272) if M < 1000 else (8200, 1040)
     g = _gen(M)
     (A, sa), (W, sw) = _q8(g, M, K), _q8(g, N, K, std=0.1)
     clean = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K), A, sa, W, sw, None, _nan(M, N))
@@ -310,10 +310,12 @@ def test_gemm_lora(bolt, M, N, K, n, rank, weights, group, how):
     rows.within(D, *want())
 
 
-@pytest.mark.parametrize("M,N,K,n,rank", [(3300, 4200, 136, 3, 64), (3329, 4104, 72, 40, 72), (2100, 6152, 72, 500, 128), (3300, 4200, 64, 1, 8)])
+@pytest.mark.parametrize("M,N,K,n,rank", [(3300, 4200, 136, 3, 64), (3329, 4104, 72, 40, 72), (2100, 6152, 72, 500, 128), (3300, 4200, 64, 1, 8), (3300, 4200, 2056, 3, 64),
+                                           (3329, 4104, 2056, 5, 72), (3329, 4104, 2056, 40, 128), (700, 4104, 1032, 6, 128), (300, 4104, 1032, 3, 72),
+                                           (1500, 4104, 1032, 9, 24)])
 @pytest.mark.parametrize("how", ["runs", "mixed"])
 def test_gemm_lora_on_large_tiles(bolt, M, N, K, n, rank, how):
-    """Tiles that add the adapters themselves: one adapter, several in a tile, a hundred and more in a tile."""
+    """Every tile for many rows, with the adapters in it and, where there can be many, their share from memory: one adapter, several in a tile."""
     D, want, _ = _lora(bolt, M, N, K, n, rank, "f16", 0, how, act="relu")
     rows.within(D, *want())
 
@@ -352,7 +354,7 @@ def test_gemm_lora_activations(bolt, M, weights, group, act):
     rows.within(D, *want())
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 24, 40), (16, 136, 264), (17, 72, 136), (65, 264, 72), (300, 136, 264), (3300, 4200, 72)])
+@pytest.mark.parametrize("M,N,K", [(1, 24, 40), (16, 136, 264), (17, 72, 136), (65, 264, 72), (300, 136, 264), (700, 1032, 264), (3300, 4200, 72), (3300, 4200, 1032)])
 @pytest.mark.parametrize("how", ["runs", "mixed"])
 def test_gemm_lora_is_exact_on_integers(bolt, M, N, K, how):
     g = _gen(M + K)
@@ -380,13 +382,14 @@ def test_gemm_lora_strides_and_untouched_padding(bolt, M, weights, group):
     assert (D[:, 72:] == 7.0).all()
 
 
-def test_gemm_lora_large_tiles_strides(bolt):
-    D, want, _ = _lora(bolt, 3300, 4200, 72, 3, 16, "f16", 0, "mixed", lda=136, ldd=4264)
+@pytest.mark.parametrize("K", [72, 2056])
+def test_gemm_lora_large_tiles_strides(bolt, K):
+    D, want, _ = _lora(bolt, 3300, 4200, K, 3, 16, "f16", 0, "mixed", lda=K + 64, ldd=4264)
     rows.within(D[:, :4200], *want())
     assert (D[:, 4200:] == 7.0).all()
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 264, 520), (16, 264, 520), (40, 264, 520), (300, 264, 520), (3300, 4200, 72)])
+@pytest.mark.parametrize("M,N,K", [(1, 264, 520), (16, 264, 520), (40, 264, 520), (300, 264, 520), (3300, 4200, 72), (3300, 4200, 2056)])
 @pytest.mark.parametrize("weights,group", [("f16", 0), ("w4", 64)])
 def test_gemm_lora_without_adapters_is_the_projection(bolt, M, N, K, weights, group):
     """No row has an adapter, and all of them hold NaN: the outputs are those of the projection alone."""
@@ -406,7 +409,7 @@ def _w4_gen(c, M, N, K):
     return g
 
 
-@pytest.mark.parametrize("M,N,K", [(16, 264, 520), (40, 264, 520), (300, 264, 520), (3300, 4200, 72)])
+@pytest.mark.parametrize("M,N,K", [(16, 264, 520), (40, 264, 520), (300, 264, 520), (3300, 4200, 72), (3300, 4200, 2056)])
 @pytest.mark.parametrize("weights,group", [("f16", 0), ("w4", 64)])
 @pytest.mark.parametrize("where", ["down", "up", "scale", "row"])
 def test_gemm_lora_adapters_do_not_meet(bolt, M, N, K, weights, group, where):
@@ -429,9 +432,9 @@ def test_gemm_lora_adapters_do_not_meet(bolt, M, N, K, weights, group, where):
     assert not torch.isfinite(again[bad]).all(dim=1).any()
 
 
-@pytest.mark.parametrize("M,N", [(1, 4104), (29, 264), (300, 1032), (3300, 4200)])
+@pytest.mark.parametrize("M,N", [(1, 4104), (29, 264), (300, 1032), (700, 4104), (3300, 4200)])
 def test_gemm_lora_gives_the_same_bits_again(bolt, M, N):
-    D, _, c = _lora(bolt, M, N, 264, 7, 24, "f16", 0, "mixed")
+    D, _, c = _lora(bolt, M, N, 2056 if M > 3000 else 264, 7, 24, "f16", 0, "mixed")
     for _ in range(3):
         again = bolt.bolt_gemm_lora(c["d"], c["A"], c["W"], c["bias"], c["ids"], c["down"], c["up"], c["scales"], _nan(M, N), c["ws"].fill_(0xff))
         assert torch.equal(D, again)
