@@ -167,36 +167,50 @@ struct RowsWave {
       }
     }
   }
-  // The rows' adapters: acc += up[a] . low^T for every adapter a that one of the rows has, the waves by turns.  Each sum is taken only where the
-  // row's adapter is a: one adapter's infinity does not reach the others' rows.
+  // The rows' adapters: acc += up[a] . low^T for every adapter a that one of the rows has, dealt over the waves: two for a wave at most, whose
+  // operands are asked for together.  Each sum is taken only where the row's adapter is a: one adapter's infinity does not reach the others' rows.
   template <int NW>
   __device__ __forceinline__ void add_adapters(int col0, int wave, floatx4 (&acc)[R][MB]) const {
-    static_assert(MB == 1, "one block of 16 rows");
+    static_assert(MB == 1 && NW >= 8, "16 rows, no more than two adapters for a wave");
     const int mine = row_adapter(p.adapter, p.adapters, row0 + l16, l16 < rows);
     unsigned left = (unsigned)__ballot(mine >= 0) & 0xffffu;
-    const int64_t low = (int64_t)(row0 + (l16 < rows ? l16 : rows - 1)) * p.rank + g * 8;
+    int a[2] = {-1, -1};
     for (int turn = 0; left != 0; ++turn) {
-      const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
-      left &= ~(unsigned)__ballot(mine == a);
-      if (turn % NW != wave) continue;
-      const half_t* const up = p.up + (int64_t)a * p.N * p.rank + g * 8;
-      floatx4 sum[R] = {};
-      for (int k = 0; k < p.rank; k += 32) {
-        const bool in = k + g * 8 < p.rank;
-        const int at = in ? k : -g * 8;
-        const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0}, b = low_operand(p.low, low + at, p.low_parts, (int64_t)p.M * p.rank);
+      const int next = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
+      left &= ~(unsigned)__ballot(mine == next);
+      if (turn == wave) a[0] = next;
+      if (turn == wave + NW) a[1] = next;
+    }
+    if (a[0] < 0) return;
+    const int64_t low = (int64_t)(row0 + (l16 < rows ? l16 : rows - 1)) * p.rank;
+    floatx4 sum[2][R] = {};
+    for (int k = 0; k < p.rank; k += 32) {
+      const bool in = k + g * 8 < p.rank;
+      const int at = in ? k + g * 8 : 0;
+      const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+      half8 u[2][R];
+      auto load = [&](int i) {
+        const half_t* const up = p.up + (int64_t)a[i] * p.N * p.rank + at;
 #pragma unroll
         for (int t = 0; t < R; ++t) {
           const int n = col0 + t * 16 + l16;
-          const half8 u = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + at);
-          sum[t] = mfma_16x16x32(in ? u : zero, in ? b : zero, sum[t]);
+          u[i][t] = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank);
         }
+      };
+      load(0);
+      if (a[1] >= 0) load(1);
+      const half8 l = low_operand(p.low, low + at, p.low_parts, (int64_t)p.M * p.rank), b = in ? l : zero;
+#pragma unroll
+      for (int t = 0; t < R; ++t) sum[0][t] = mfma_16x16x32(in ? u[0][t] : zero, b, sum[0][t]);
+      if (a[1] >= 0) {
+#pragma unroll
+        for (int t = 0; t < R; ++t) sum[1][t] = mfma_16x16x32(in ? u[1][t] : zero, b, sum[1][t]);
       }
-#pragma unroll
-      for (int t = 0; t < R; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[t][0][e] += mine == a ? sum[t][e] : 0.f;
     }
+#pragma unroll
+    for (int t = 0; t < R; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[t][0][e] += mine < 0 ? 0.f : mine == a[0] ? sum[0][t][e] : mine == a[1] ? sum[1][t][e] : 0.f;
   }
   // part: [waves][R * MB][64 lanes][4] floats
   __device__ __forceinline__ void put_sums(float* part, int wave, const floatx4 (&acc)[R][MB]) const {
@@ -273,15 +287,13 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
     w.template load_rows<false>(wave + i * NW, xf[decltype(b)::value]);
   };
   auto multiply = [&](auto b) { w.template multiply<false>(0, wf[decltype(b)::value], xf[decltype(b)::value], acc); };
-  // The adapters' operands are asked for behind the first steps' and multiplied while those arrive.  (Sixteen waves have 128 registers each, too few
-  // for that: there they come last.)
-  auto adapters = [&](bool last) {
-    if constexpr (LORA)
-      if (last == (NW == 16)) w.template add_adapters<NW>(col0, wave, acc);
+  // LORA: the adapters' operands are asked for behind the first steps' and multiplied while those arrive.
+  auto adapters = [&] {
+    if constexpr (LORA) w.template add_adapters<NW>(col0, wave, acc);
   };
   if (n >= NB) {
     for_constants<NB>([&](auto b) { load(decltype(b)::value, b); });
-    adapters(false);
+    adapters();
     int c = 0;
     for (; c + 2 * NB <= n; c += NB)
       for_constants<NB>([&](auto b) {
@@ -300,7 +312,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
     for_constants<NB>([&](auto b) {
       if (decltype(b)::value < n) load(decltype(b)::value, b);
     });
-    adapters(false);
+    adapters();
     for_constants<NB>([&](auto b) {
       if (decltype(b)::value < n) multiply(b);
     });
@@ -310,7 +322,6 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
     w.template load_rows<true>(whole, xf[0]);
     w.template multiply<true>(whole, wf[0], xf[0], acc);
   }
-  adapters(true);
   w.put_sums(part, wave, acc);
   __syncthreads();
   w.template finish<NW>(part, col0, tid);
@@ -323,7 +334,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
 // (Two workgroups of eight waves share a compute unit with up to 128 registers, which the routed kernels of one group a step and two steps just miss if
 // left alone: one token, 8 of 64 experts, 2048 x 2048, no gate, 20.9 us so and 17.7 held to 128; 3 tokens, 3 of 44 experts, 1560 x 664, gated, 14.6
 // and 13.7.  Linear layers would spill.)
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX, bool LORA = false>
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
 __global__ __launch_bounds__(64 * NW, WT == WEIGHTS_W4 && MODE != ROWS_DENSE && NG == 1 && NX == 2 ? 4 : 1) void few_rows_walk_kernel(const RowsParams p) {
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int PART = NW * R * 64 * 4;
@@ -360,7 +371,6 @@ __global__ __launch_bounds__(64 * NW, WT == WEIGHTS_W4 && MODE != ROWS_DENSE && 
   for_constants<NX>([&](auto i) { w.template load_rows<true>(wave + decltype(i)::value * NW, xf[decltype(i)::value]); });
   auto tile = [&](int it, auto set) {
     floatx4 acc[R][1] = {};
-    if constexpr (LORA) w.template add_adapters<NW>((cb + it) * Wave::COLS, wave, acc);
     for_constants<NX>([&](auto i) {
       w.template multiply<true>(wave + decltype(i)::value * NW, wf[decltype(set)::value][decltype(i)::value], xf[decltype(i)::value], acc);
     });
@@ -405,9 +415,9 @@ hipError_t launch_few_rows(RowsParams p, hipStream_t stream) {
   hipLaunchKernelGGL(kern, dim3(p.row_blocks * p.col_blocks), dim3(64 * NW), LDS_BYTES, stream, p);
   return hipGetLastError();
 }
-template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX, bool LORA = false>
+template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NX>
 hipError_t launch_few_rows_walk(RowsParams p, hipStream_t stream) {
-  auto kern = few_rows_walk_kernel<WT, MODE, GATED, NG, R, NW, NX, LORA>;
+  auto kern = few_rows_walk_kernel<WT, MODE, GATED, NG, R, NW, NX>;
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int LDS_BYTES = 2 * NW * R * 64 * 16;
   static LdsOptIn opt_in;

@@ -18,12 +18,15 @@ hipError_t launch(const NormParams& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Waves and pieces by the width alone: few rows take about 4 us in any form (one round trip), many are fastest where a workgroup's lanes have two to
+// four pieces each.  us with the residual, FP16 rows, waves x pieces: 32768 x 1024 1 x 2 47, 2 x 2 48, 4 x 1 56; 32768 x 2048 2 x 2 92, 1 x 4 92, 4 x 1 96, 8 x 1
+// 110; 4099 x 5120 4 x 4 34.0, 8 x 2 35.3, 16 x 2 45; 4099 x 8192 4 x 4 48.6, 8 x 2 49.0, 16 x 2 55; 4099 x 12296 16 x 2 74, 8 x 4 90; 1 x 4096 3.9 to 4.2 in six forms.
 template <bool NORM>
 hipError_t launch_norm(const NormParams& p, hipStream_t stream) {
   const int chunks = p.width / 8;
   if (chunks <= 64) return launch<1, 1, NORM>(p, stream);
   if (chunks <= 128) return launch<1, 2, NORM>(p, stream);
-  if (chunks <= 256) return launch<4, 1, NORM>(p, stream);
+  if (chunks <= 256) return launch<2, 2, NORM>(p, stream);
   if (chunks <= 512) return launch<4, 2, NORM>(p, stream);
   if (chunks <= 1024) return launch<4, 4, NORM>(p, stream);
   if (chunks <= 2048) return launch<16, 2, NORM>(p, stream);
