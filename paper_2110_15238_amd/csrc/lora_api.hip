@@ -8,9 +8,13 @@
 namespace bolt {
 namespace {
 
-constexpr int kMaxRank = 128, kFewRows = 16;
+constexpr int kMaxRank = 128;
 // Workgroups of 16 rows from which low's reduction is not split any more, and into how many parts at most.
 constexpr int kDownGroups = 256, kMostParts = kMostLowParts;
+
+// Whether the projection runs on the kernel for up to 16 rows, which adds the adapters itself: some more rows too, where all of their blocks are on the
+// chip at once (2048 x 8192 in 4 bits with 32 adapters, 17 to 32 rows: 19.8 us so, 24 on tiles of 32 rows behind lora_up_kernel; FP16 25 and 25).
+bool on_few_rows(const bolt_gemm_lora_desc& d) { return d.M <= 16 || (d.M <= 64 && blocks_of(d.M, 16) * blocks_of(d.N, 16) <= 256); }
 
 bolt_gemm_w4_desc base_w4(const bolt_gemm_lora_desc& d) { return {d.M, d.N, d.K, d.lda, d.ldd, d.group, d.alpha, d.beta, d.act}; }
 
@@ -55,6 +59,19 @@ int turns_of(const LoraParams& p, int block_rows, int64_t workgroups) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / workgroups));
 }
 
+// Tiles of 16 ranks that a workgroup of lora_down_kernel has, 1, 2, 4 or 8: all of them, so that x is read once, unless that leaves compute units without
+// work though the reduction is split into kMostParts; rows that are as good as single have one.
+int down_tiles(int64_t M, int rank) {
+  if (M <= 64) return 1;
+  int tiles = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
+  while (tiles > 1 && blocks_of(M, 16) * blocks_of(rank, 16 * tiles) * kMostParts < 160) tiles /= 2;
+  return tiles;
+}
+// Parts of low's reduction, as many as the launch needs to fill the chip.
+int down_parts(int64_t M, int rank) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kMostParts, kDownGroups / (blocks_of(M, 16) * (M <= 64 ? 1 : blocks_of(rank, 16 * down_tiles(M, rank))))));
+}
+
 template <int RT, int NW, int S>
 hipError_t launch_down(LoraParams p, hipStream_t stream) {
   auto kern = lora_down_kernel<RT, NW, S>;
@@ -69,10 +86,12 @@ hipError_t launch_down(LoraParams p, hipStream_t stream) {
   return hipGetLastError();
 }
 hipError_t launch_lora_down(const LoraParams& p, hipStream_t stream) {
-  if (p.M <= 64 || p.rank <= 16) return launch_down<1, 4, 4>(p, stream);
-  if (p.rank <= 32) return launch_down<2, 4, 3>(p, stream);
-  if (p.rank <= 64) return launch_down<4, 4, 2>(p, stream);
-  return launch_down<8, 4, 2>(p, stream);
+  switch (down_tiles(p.M, p.rank)) {
+    case 1: return launch_down<1, 4, 4>(p, stream);
+    case 2: return launch_down<2, 4, 3>(p, stream);
+    case 4: return launch_down<4, 4, 2>(p, stream);
+    default: return launch_down<8, 4, 2>(p, stream);
+  }
 }
 template <int MB>
 hipError_t launch_up(LoraParams p, hipStream_t stream) {
@@ -82,7 +101,10 @@ hipError_t launch_up(LoraParams p, hipStream_t stream) {
   hipLaunchKernelGGL(lora_up_kernel<MB>, dim3(blocks * p.tiles * p.turns), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
-hipError_t launch_lora_up(const LoraParams& p, hipStream_t stream) { return p.M <= 64 ? launch_up<1>(p, stream) : launch_up<4>(p, stream); }
+// (64 rows for a workgroup read up less often, 16 make more workgroups)
+hipError_t launch_lora_up(const LoraParams& p, hipStream_t stream) {
+  return blocks_of(p.M, 64) * blocks_of(p.N, 256) < 256 ? launch_up<1>(p, stream) : launch_up<4>(p, stream);
+}
 
 // ---- which kernels run a projection with FP16 weights on more than 16 rows ----------------------------------------------------
 // A fit to 5 shapes (1024 to 8192 outputs, K 2048 to 11008) x 10 row counts from 17 to 3300, with adapters in the tiles and with their share from memory:
@@ -102,11 +124,11 @@ bool adapters_in_tiles(const bolt_gemm_lora_desc& d, const LayerTile& t) {
   const double most = std::min(d.adapters, std::min(t.rows, d.M)) * (t.tile == RowsTile::ROWS256_COLS256 ? 2.4 : 0.5);
   return layer_rounds(t, d.M, d.N) * most <= 3.5 + 1.1e-6 * d.M * d.N;
 }
-// Parts of low's reduction.  (256 x 256 tiles read low as halves.)
+// (256 x 256 tiles read low as halves.)
 int low_parts(const bolt_gemm_lora_desc& d) {
-  if (d.weights == BOLT_WEIGHTS_F16 && d.M > kFewRows)
+  if (d.weights == BOLT_WEIGHTS_F16 && !on_few_rows(d))
     if (const LayerTile* t = projection_tile(d); t && t->tile == RowsTile::ROWS256_COLS256) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kMostParts, kDownGroups / blocks_of(d.M, 16)));
+  return down_parts(d.M, d.rank);
 }
 
 }  // namespace
@@ -133,9 +155,9 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
   if (!workspace || workspace_bytes < (size_t)ws.bytes) return BOLT_ERR_WORKSPACE;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
-  const bool w4 = d.weights == BOLT_WEIGHTS_W4;
-  const LayerTile* const tile = w4 || d.M <= kFewRows ? nullptr : projection_tile(d);
-  if (!w4 && d.M > kFewRows && !tile) return BOLT_ERR_UNSUPPORTED;
+  const bool w4 = d.weights == BOLT_WEIGHTS_W4, few = on_few_rows(d);
+  const LayerTile* const tile = w4 || few ? nullptr : projection_tile(d);
+  if (!w4 && !few && !tile) return BOLT_ERR_UNSUPPORTED;
   const bolt_gemm_w4_desc base = base_w4(d);
   const hipStream_t st = (hipStream_t)stream;
   LoraParams l{};
@@ -161,7 +183,7 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
     p.alpha = d.alpha; p.beta = d.beta; p.act = d.act;
   }
   p.adapter = l.adapter; p.low = l.low; p.up = l.up; p.adapters = d.adapters; p.rank = d.rank; p.low_parts = l.parts;
-  if (d.M <= kFewRows) return status_of(w4 ? launch_few_rows_w4_lora(p, d.group, st) : launch_few_rows_f16_lora(p, st));
+  if (few) return status_of(w4 ? launch_few_rows_w4_lora(p, d.group, st) : launch_few_rows_f16_lora(p, st));
   if (tile && adapters_in_tiles(d, *tile)) return status_of(launch_rows_f16_adapters(p, tile->tile, st));
   const bool apart = ws.share_at != ws.weights_at;
   l.y = apart ? (half_t*)((char*)workspace + ws.share_at) : (half_t*)D;

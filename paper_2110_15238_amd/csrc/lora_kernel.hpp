@@ -175,25 +175,36 @@ __global__ __launch_bounds__(256) void lora_up_kernel(const LoraParams p) {
       }
     }
   };
+  // (low of all ranks once: what the rows have does not depend on the adapter at hand)
+  const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  half8 l[4][MB];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+      l[k][b] = zero;
+      if (k * 32 >= p.rank) continue;
+      const bool in = k * 32 + g * 8 < p.rank;
+      const half8 v = low_operand(p.low, low[b] + (in ? k * 32 : -g * 8), p.parts, (int64_t)p.M * p.rank);
+      l[k][b] = in ? v : zero;
+    }
   for_adapters(mine, turn, p.turns, [&](int a) {
     const half_t* const up = p.up + (int64_t)a * p.N * p.rank + g * 8;
     floatx4 sum[4][MB] = {};
-    for (int k = 0; k < p.rank; k += 32) {
-      const bool in = k + g * 8 < p.rank;
-      const int at = in ? k : -g * 8;
-      const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-      half8 l[MB], u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k * 32 >= p.rank) break;
+      const bool in = k * 32 + g * 8 < p.rank;
+      half8 u[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int n = from + 4 * t;
-        u[t] = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + at);
+        u[t] = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + (in ? k * 32 : -g * 8));
       }
-#pragma unroll
-      for (int b = 0; b < MB; ++b) l[b] = low_operand(p.low, low[b] + at, p.parts, (int64_t)p.M * p.rank);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int b = 0; b < MB; ++b) sum[t][b] = mfma_16x16x32(in ? u[t] : zero, in ? l[b] : zero, sum[t][b]);
+        for (int b = 0; b < MB; ++b) sum[t][b] = mfma_16x16x32(in ? u[t] : zero, l[k][b], sum[t][b]);
     }
     store(a, sum);
   });

@@ -123,6 +123,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * KG) void rows_tile_kernel(
           of_row[b] = __shfl(mine, b * 32 + l32);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
+            if (k0 + k * 16 >= p.rank) {  // (the same for all lanes)
+              low[b][k] = zero;
+              continue;
+            }
             const int at = k0 + k * 16 + g * 8;
             const half8 v = low_operand(p.low, (int64_t)(m < p.M ? m : p.M - 1) * p.rank + (at < p.rank ? at : 0), p.low_parts, (int64_t)p.M * p.rank);
             low[b][k] = at < p.rank ? v : zero;
@@ -136,6 +140,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * KG) void rows_tile_kernel(
             const int n = col0 + a * 32 + l32;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
+              if (k0 + k * 16 >= p.rank) {
+                u[a][k] = zero;
+                continue;
+              }
               const int at = k0 + k * 16 + g * 8;
               const half8 v = *(const half8*)(from + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + (at < p.rank ? at : 0));
               u[a][k] = at < p.rank ? v : zero;
