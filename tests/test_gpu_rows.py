@@ -573,3 +573,15 @@ def test_python_refuses_other_tensors(bolt):
             bolt.bolt_gemm_lora(l, **{**good, **bad})
     with pytest.raises(bolt.BoltError):
         bolt.bolt_gemm_lora(l, **{**good, "workspace": None})
+
+
+@pytest.mark.parametrize("weights", ["f16", "w4"])
+def test_example_runs(weights):
+    """The example checks its own rows against float64 and raises if they are off."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, os.path.join(root, "examples", "served_layer.py"), "--tokens", "1", "24", "300", "--width", "1024", "--hidden",
+                          "1536", "--weights", weights], capture_output=True, text=True, timeout=110)
+    assert out.returncode == 0 and out.stdout.count("us per pass") == 3, out.stdout + out.stderr
