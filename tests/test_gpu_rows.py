@@ -244,6 +244,16 @@ def test_gemm_q8_rows_and_columns_do_not_meet(bolt, M):
     assert torch.equal(D[keep_r][:, keep_c], clean[keep_r][:, keep_c])
 
 
+@pytest.mark.parametrize("M", [9, 40, 200, 2060])
+def test_gemm_q8_of_bias_alone(bolt, M):
+    """alpha 0: -1.5 times the bias is a number of FP32, rounded once."""
+    N, K = 4104, 272
+    g = _gen(M)
+    (A, sa), (W, sw), bias = _q8(g, M, K), _q8(g, N, K), _half(g, N)
+    D = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K, alpha=0.0, beta=-1.5), A, sa, W, sw, bias, _nan(M, N))
+    assert torch.equal(D, (bias.float() * -1.5).half().expand(M, N))
+
+
 def test_gemm_q8_of_weights_past_2_gib(bolt):
     """Offsets into W pass 31 bits; the 256 x 256 tiles, which the sizes would have, give way."""
     M, N, K = 260, 200008, 12288
@@ -438,6 +448,39 @@ def test_gemm_lora_gives_the_same_bits_again(bolt, M, N):
     for _ in range(3):
         again = bolt.bolt_gemm_lora(c["d"], c["A"], c["W"], c["bias"], c["ids"], c["down"], c["up"], c["scales"], _nan(M, N), c["ws"].fill_(0xff))
         assert torch.equal(D, again)
+
+
+@pytest.mark.parametrize("M,N,K", [(4, 264, 520), (29, 264, 520), (300, 1032, 264), (600, 1032, 264), (3300, 4200, 72), (3300, 4200, 2056)])
+@pytest.mark.parametrize("weights,group", [("f16", 0), ("w4", 64)])
+def test_gemm_lora_of_bias_alone(bolt, M, N, K, weights, group):
+    """alpha 0, with which no sum can start at beta / alpha times the bias: -1.5 times the bias is a number of FP32, rounded once."""
+    _, _, c = _lora(bolt, M, N, K, 5, 24, weights, group, "mixed")
+    d = bolt.gemm_lora_desc(M, N, K, 5, 24, weights=weights, group=group, alpha=0.0, beta=-1.5)
+    D = bolt.bolt_gemm_lora(d, c["A"], c["W"], c["bias"], c["ids"], c["down"], c["up"], c["scales"], _nan(M, N),
+                            _nan(bolt.bolt_gemm_lora_workspace_bytes(d), dtype=torch.uint8))
+    assert torch.equal(D, (c["bias"].float() * -1.5).half().expand(M, N))
+
+
+@pytest.mark.parametrize("M,N,K", [(4, 264, 520), (29, 1032, 520), (300, 1032, 264), (3300, 4200, 72)])
+@pytest.mark.parametrize("weights,group", [("f16", 0), ("w4", 64)])
+def test_gemm_lora_in_a_graph_of_other_requests(bolt, M, N, K, weights, group):
+    """What a graph has captured goes by the ids that a replay finds: one adapter for all rows, one each, none at all."""
+    _, _, c = _lora(bolt, M, N, K, 40, 24, weights, group, "runs")
+    call = lambda D: bolt.bolt_gemm_lora(c["d"], c["A"], c["W"], c["bias"], c["ids"], c["down"], c["up"], c["scales"], D, c["ws"])
+    D = _nan(M, N)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(D)
+    rows_of = torch.arange(M, device="cuda", dtype=torch.int32)
+    for ids in (rows_of % 40, rows_of * 0 + 39, rows_of * 0 - 1, rows_of * 40 // M):
+        c["ids"].copy_(ids)
+        want = call(_nan(M, N)).clone()
+        c["ws"].fill_(0xff)
+        D.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(D, want)
 
 
 def test_gemm_lora_of_adapters_past_2_gib(bolt):
