@@ -42,11 +42,14 @@ hipError_t launch_rows_f16_add(const RowsParams& p, RowsTile tile, hipStream_t s
 // Linear layers of up to 16 rows whose sums take the rows' adapters (adapter, low, up, adapters, rank).
 hipError_t launch_few_rows_f16_lora(const RowsParams& p, hipStream_t stream);
 hipError_t launch_few_rows_w4_lora(const RowsParams& p, int group, hipStream_t stream);
+// The same from 17 rows on, on 32 x 32, 32 x 64 or 64 x 128 tiles.
+hipError_t launch_shared_rows_w4_lora(const RowsParams& p, int group, SharedTile tile, hipStream_t stream);
 
 // bolt_gemm_w4 behind its checks; `add` (M x N, ldadd, or null): added to A . W^T before alpha, from 17 rows on (csrc/moe_api.hip).
 bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d);
 bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, const half_t* add, int ldadd, void* D,
                         void* workspace, void* stream);
+SharedTile tile_of_gemm_w4(const bolt_gemm_w4_desc& d);  // from 17 rows on, where the weights stay packed
 RowsParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, void* D, const half_t* none);
 
 // What bolt_gemm_epilogue's own choice of a kernel is estimated to take, in us; false where it has none (csrc/bolt_api.hip).

@@ -124,6 +124,17 @@ bool adapters_in_tiles(const bolt_gemm_lora_desc& d, const LayerTile& t) {
   const double most = std::min(d.adapters, std::min(t.rows, d.M)) * (t.tile == RowsTile::ROWS256_COLS256 ? 2.4 : 0.5);
   return layer_rounds(t, d.M, d.N) * most <= 3.5 + 1.1e-6 * d.M * d.N;
 }
+// The same for tiles on 4-bit weights, which have fewer waves to hide it behind: while the most adapters a tile can have are few, of low rank.  us, 64 rows
+// (32 x 32 and 32 x 64 tiles) and 300 (64 x 128), share through memory / in the tiles: 4096 x 4096, 2 adapters of rank 16 17.0 / 14.0 and 33.6 / 31.0, 8 17.5 /
+// 15.6 and 38.6 / 37.9, 32 18.6 / 17.7 and 44.2 / 44.3, 64 18.9 / 18.7 and 45.5 / 46.5; 6152 x 5000, 2 of rank 72 25.0 / 24.1 and 48.5 / 51.4, 8 31.0 / 30.6 and
+// 70.5 / 65.4, 32 38.6 / 41.1 and 103 / 102.  128 x 256 tiles lose with two of rank 16 already (12288 x 4096, 300 rows 64 / 75).
+bool adapters_in_w4_tiles(const bolt_gemm_lora_desc& d) {
+  const bolt_gemm_w4_desc base = base_w4(d);
+  const SharedTile tile = tile_of_gemm_w4(base);
+  if (bolt_gemm_w4_workspace_bytes(&base) > 0 || tile == SharedTile::ROWS128_COLS256) return false;
+  const int rows = tile_size(tile).rows;
+  return std::min(d.adapters, std::min(rows, d.M)) * blocks_of(d.rank, 32) <= (rows == 32 ? 16 : 8);
+}
 // (256 x 256 tiles read low as halves.)
 int low_parts(const bolt_gemm_lora_desc& d) {
   if (d.weights == BOLT_WEIGHTS_F16 && !on_few_rows(d))
@@ -185,6 +196,7 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
   p.adapter = l.adapter; p.low = l.low; p.up = l.up; p.adapters = d.adapters; p.rank = d.rank; p.low_parts = l.parts;
   if (few) return status_of(w4 ? launch_few_rows_w4_lora(p, d.group, st) : launch_few_rows_f16_lora(p, st));
   if (tile && adapters_in_tiles(d, *tile)) return status_of(launch_rows_f16_adapters(p, tile->tile, st));
+  if (w4 && adapters_in_w4_tiles(d)) return status_of(launch_shared_rows_w4_lora(p, d.group, tile_of_gemm_w4(base), st));
   const bool apart = ws.share_at != ws.weights_at;
   l.y = apart ? (half_t*)((char*)workspace + ws.share_at) : (half_t*)D;
   l.ldy = apart ? d.N : d.ldd;

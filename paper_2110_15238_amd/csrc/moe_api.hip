@@ -398,6 +398,8 @@ RowsParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void* 
   return p;
 }
 
+SharedTile tile_of_gemm_w4(const bolt_gemm_w4_desc& d) { return dense_tile(d.M, d.N, W4Format(d.N, d.K, d.group).steps, d.group).tile; }
+
 bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, const half_t* add, int ldadd, void* D,
                         void* workspace, void* stream) {
   const W4Format f(d.N, d.K, d.group);

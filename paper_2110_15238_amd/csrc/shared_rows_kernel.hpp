@@ -39,7 +39,87 @@ struct SharedRowsTraits {
   static_assert(LDS_BYTES <= 160 * 1024 && S >= 3, "stages");
 };
 
-template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S>
+// The rows' adapters (linear layers): acc += up[a] . low^T for every adapter a that one of the rows has, adapter i by set i % KG of the waves, 64 ranks at
+// a time: the rows' low once, then up of one adapter after the other, the next one's on its way.  A sum is taken only where the row's adapter is a.
+template <int MB, int R, int KG>
+__device__ __forceinline__ void add_adapters_by_sets(const RowsParams& p, int row0, int rows, int col0, int kg, int lane, floatx4 (&acc)[R][MB]) {
+  static_assert(MB <= 4, "a row for each lane");
+  const int g = lane >> 4, l16 = lane & 15;
+  const int mine = row_adapter(p.adapter, p.adapters, row0 + lane, lane < rows);
+  int of_row[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) of_row[b] = __shfl(mine, b * 16 + l16);
+  const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int k0 = 0; k0 < p.rank; k0 += 64) {
+    // (ranks beyond the last are zero on both sides)
+    const int at[2] = {k0 + g * 8, k0 + 32 + g * 8};
+    const bool two = k0 + 32 < p.rank;  // (the same for all lanes)
+    auto load = [&](int a, half8 (&u)[R][2]) {
+      const half_t* const up = p.up + (int64_t)a * p.N * p.rank;
+#pragma unroll
+      for (int t = 0; t < R; ++t) {
+        const int n = col0 + t * 16 + l16;
+        const half_t* const from = up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank;
+        u[t][0] = *(const half8*)(from + (at[0] < p.rank ? at[0] : 0));
+        u[t][1] = zero;
+        if (two) u[t][1] = *(const half8*)(from + (at[1] < p.rank ? at[1] : 0));
+      }
+    };
+    unsigned long long left = __ballot(mine >= 0);
+    int turn = 0;
+    auto take = [&] {  // this set's next adapter, -1 behind its last
+      while (left != 0) {
+        const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+        left &= ~__ballot(mine == a);
+        const bool ours = turn == kg;
+        turn = turn + 1 == KG ? 0 : turn + 1;
+        if (ours) return a;
+      }
+      return -1;
+    };
+    int now = take();
+    if (now < 0) return;
+    half8 up[2][R][2], low[MB][2];
+    load(now, up[0]);
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+      const int j = b * 16 + l16;
+      const int64_t row = (int64_t)(row0 + (j < rows ? j : rows - 1)) * p.rank;
+      const half8 v = low_operand(p.low, row + (at[0] < p.rank ? at[0] : 0), p.low_parts, (int64_t)p.M * p.rank);
+      low[b][0] = at[0] < p.rank ? v : zero;
+      low[b][1] = zero;
+      if (two) {
+        const half8 v = low_operand(p.low, row + (at[1] < p.rank ? at[1] : 0), p.low_parts, (int64_t)p.M * p.rank);
+        low[b][1] = at[1] < p.rank ? v : zero;
+      }
+    }
+    auto multiply = [&](int a, const half8 (&u)[R][2]) {
+#pragma unroll
+      for (int t = 0; t < R; ++t) {
+        const half8 u0 = at[0] < p.rank ? u[t][0] : zero, u1 = at[1] < p.rank ? u[t][1] : zero;
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+          floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+          sum = mfma_16x16x32(u0, low[b][0], sum);
+          sum = mfma_16x16x32(u1, low[b][1], sum);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][b][e] += of_row[b] == a ? sum[e] : 0.f;
+        }
+      }
+    };
+    while (now >= 0) {
+      const int next = take();
+      if (next >= 0) load(next, up[1]);
+      multiply(now, up[0]);
+      if (next < 0) break;
+      now = take();
+      if (now >= 0) load(now, up[0]);
+      multiply(next, up[1]);
+    }
+  }
+}
+
+template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S, bool LORA = false>
 __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<WT, MODE, GATED, NG, MB, R>& w, int wave_all, int cb, half_t* lds) {
   using T = SharedRowsTraits<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
   using Wave = RowsWave<WT, MODE, GATED, NG, MB, R>;
@@ -186,6 +266,8 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
   constexpr int AHEAD = (S - 2) * T::LOADS < 63 ? (S - 2) * T::LOADS : 63;
 #pragma unroll
   for (int t = 0; t < S - 1; ++t) load(t, ring + t * T::STAGE);
+  // (while the first steps' loads are on their way)
+  if constexpr (LORA) add_adapters_by_sets<MB, R, KG>(p, w.row0, w.rows, col0, kg, lane, acc);
   int stage = 0, fill = S - 1;
   const int all = KG > 1 ? p.steps / KG : turns;  // turns that every set has
   for (int t = 0; t < all; ++t) {
@@ -255,7 +337,7 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
   }
 }
 
-template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S>
+template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S, bool LORA = false>
 __global__ __launch_bounds__(64 * WN * KG) void shared_rows_kernel(const RowsParams p) {
   using T = SharedRowsTraits<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
   constexpr int BM = T::BM;
@@ -282,7 +364,7 @@ __global__ __launch_bounds__(64 * WN * KG) void shared_rows_kernel(const RowsPar
     w.row0 = at.lo + done;
     w.rows = at.n - done < BM ? at.n - done : BM;
   }
-  shared_rows_tile<WT, MODE, GATED, NG, MB, R, WN, KG, S>(p, w, __builtin_amdgcn_readfirstlane(tid >> 6), cb, lds);
+  shared_rows_tile<WT, MODE, GATED, NG, MB, R, WN, KG, S, LORA>(p, w, __builtin_amdgcn_readfirstlane(tid >> 6), cb, lds);
 }
 
 // The tiles of columns that hold marked weights (w4_unpack_kernel), all rows; a workgroup whose columns hold none reads 16 numbers and ends.
@@ -302,9 +384,10 @@ __global__ __launch_bounds__(64 * WN) void shared_rows_marked_kernel(const RowsP
   }
 }
 
-template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S>
+template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S, bool LORA = false>
 hipError_t launch_shared_rows(RowsParams p, hipStream_t stream) {
-  auto kern = shared_rows_kernel<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
+  static_assert(!LORA || (WT == WEIGHTS_W4 && MODE == ROWS_DENSE), "adapters: linear layers of 4-bit weights");
+  auto kern = shared_rows_kernel<WT, MODE, GATED, NG, MB, R, WN, KG, S, LORA>;
   using T = SharedRowsTraits<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
   static LdsOptIn opt_in;
   if (hipError_t e = opt_in.ensure((const void*)kern, T::LDS_BYTES); e != hipSuccess) return e;

@@ -330,6 +330,20 @@ def test_gemm_lora_on_large_tiles(bolt, M, N, K, n, rank, how):
     rows.within(D, *want())
 
 
+@pytest.mark.parametrize("M,N,K,n,rank", [(33, 4104, 1032, 4, 24), (64, 4104, 1032, 2, 128), (90, 2056, 520, 8, 40), (100, 8200, 264, 5, 16), (300, 4104, 1032, 2, 72),
+                                           (300, 4104, 520, 8, 8), (450, 4104, 1032, 1, 64)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("how", ["runs", "mixed"])
+def test_gemm_lora_of_few_adapters_on_packed_tiles(bolt, M, N, K, n, rank, group, how):
+    D, want, c = _lora(bolt, M, N, K, n, rank, "w4", group, how)
+    rows.within(D, *want())
+    # one adapter's infinity stays with its rows (infinities of both signs: no activation behind them, a ReLU makes zeros of NaN)
+    c["up"][0] = float("inf")
+    again = bolt.bolt_gemm_lora(c["d"], c["A"], c["W"], c["bias"], c["ids"], c["down"], c["up"], c["scales"], _nan(M, N), c["ws"].fill_(0xff))
+    others = c["ids"] != 0
+    assert torch.equal(again[others], D[others]) and not torch.isfinite(again[~others]).all()
+
+
 @pytest.mark.parametrize("how", ["runs", "mixed"])
 def test_gemm_lora_over_unpacked_weights(bolt, how):
     M, N, K = 4096, 8192, 1032

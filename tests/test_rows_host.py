@@ -135,7 +135,7 @@ def test_kernels_keep_their_working_set_in_registers():
     if not os.path.exists(build):
         pytest.skip("no build directory (library shipped pre-built)")
     seen = set()
-    for name in ("norm_api", "lora_api", "inst_rows_f8", "inst_rows_lora", "inst_few_rows_f16", "inst_few_rows_w4"):
+    for name in ("norm_api", "lora_api", "inst_rows_f8", "inst_rows_lora", "inst_few_rows_f16", "inst_few_rows_w4", "inst_shared_rows_lora"):
         for kernel, scratch in re.findall(r"Function Name: (\S+)\s+VGPRs: \d+\s+ScratchSize \[bytes/lane\]: (\d+)", open(os.path.join(build, name + ".usage")).read()):
             seen.add(kernel)
             assert int(scratch) <= (128 if "moe_pp_kernel" in kernel else 0), (kernel, scratch)
