@@ -4,7 +4,8 @@
  * epilogues, persistent back-to-back (b2b) GEMM / conv fusion, channel padding, and the
  * light-weight profiler that picks template parameters per shape; and next to them the operators of
  * language models that an FP16 GEMM alone does not cover: products with 4-bit weights, routing to
- * experts, the experts' products.
+ * experts, the experts' products, projections with low-rank adapters, the norm with its residual,
+ * rows in 8 bits and the products that read them.
  *
  * Conventions for every call
  *   - All tensor pointers are DEVICE pointers to IEEE binary16 data unless stated otherwise.
@@ -53,7 +54,7 @@ typedef enum {
   BOLT_ACT_GELU = 2,       /* 0.5 v (1 + erf(v / sqrt 2)) */
   BOLT_ACT_HARDSWISH = 3,  /* v * clamp(v + 3, 0, 6) / 6   */
   BOLT_ACT_SOFTPLUS = 4,   /* log(1 + exp v)               */
-  BOLT_ACT_SILU = 5        /* v / (1 + exp(-v)): bolt_gemm_w4 and bolt_moe_experts only */
+  BOLT_ACT_SILU = 5        /* v / (1 + exp(-v)): bolt_gemm_w4, bolt_gemm_q8, bolt_moe_experts only */
 } bolt_act;
 
 typedef enum {
@@ -408,8 +409,8 @@ size_t bolt_moe_workspace_bytes(const bolt_moe_desc* desc);
 /* ---- A projection shared by requests that each bring a low-rank adapter --------------------------------------------
  *   D[m] = act(alpha * (A[m] . W^T + scales[a] * (A[m] . down[a]^T) . up[a]^T) + beta * bias),  a = ids[m];
  * a row whose id is below zero, or no less than `adapters`, has no adapter and is A[m] . W^T alone.  scales[a] * (A[m] . down[a]^T) is rounded to
- * FP16 (the next product's operand; infinite beyond 65504); beyond 16 rows the adapters' share of a row is rounded to FP16 once more before it
- * is added.  An adapter's infinities and NaN reach its own rows only. */
+ * FP16 (the next product's operand; infinite beyond 65504).  Where more adapters can meet in a tile than it adds by itself, a row's share
+ * (... . up[a]^T) goes through memory and is rounded to FP16 once more.  An adapter's infinities and NaN reach its own rows only. */
 typedef struct {
   int32_t M, N, K;
   int32_t lda, ldd;       /* in elements; A and D are row-major */
@@ -421,7 +422,7 @@ typedef struct {
 } bolt_gemm_lora_desc;
 
 /* A: M x K (lda); W: N x K FP16, dense, or bolt_w4_pack(N, K, group, 1); bias: N halves or NULL; ids: M int32; down: [adapters][rank][K], up:
- * [adapters][N][rank], FP16; scales: `adapters` floats or NULL (1); D: M x N (ldd), not A.  K, N, lda, ldd multiples of 8.  M may be 0. */
+ * [adapters][N][rank], FP16; scales: `adapters` floats or NULL (1); D: M x N (ldd), overlaps no input.  K, N, lda, ldd multiples of 8.  M may be 0. */
 bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const void* W, const void* bias, const void* ids, const void* down,
                            const void* up, const void* scales, void* D, void* workspace, size_t workspace_bytes, void* stream);
 size_t bolt_gemm_lora_workspace_bytes(const bolt_gemm_lora_desc* desc);
@@ -431,8 +432,8 @@ size_t bolt_gemm_lora_workspace_bytes(const bolt_gemm_lora_desc* desc);
  * for every row. */
 
 /* v = x + residual, in FP32;  sum = v;  n = v / sqrt(mean(v^2) + eps) * (weight_offset + weight);  y = n;  scales[row] = max |n| / 448,
- * q = n / scale, all from the unrounded v.  A row whose largest |n| is below 2^-118 has zeros for q.  A row that holds an infinity or a NaN has a NaN
- * for its scale, and for all of its q.  Up to 2^31 - 65536 rows of up to 32768 values. */
+ * q = n / scale, all from the unrounded v.  A row whose largest |n| is below 2^-118 has zeros for q.  A row that holds an infinity or a NaN, or zeros
+ * alone with eps 0, has a NaN for its scale, and for all of its q.  Up to 2^31 - 65536 rows of up to 32768 values. */
 typedef struct {
   int32_t rows, width;             /* width a multiple of 8 */
   int32_t ldx, ldr, lds, ldy, ldq; /* row strides of x, residual, sum, y and q in elements, multiples of 8; of those that are not NULL */
@@ -441,8 +442,8 @@ typedef struct {
 } bolt_rms_norm_desc;
 
 /* x: rows x width; residual: the same, or NULL (none); weight: `width` halves; outputs, each may be NULL, y or q not both: sum and y: rows x
- * width FP16; q: rows x width bytes, scales: `rows` floats (with q).  One of sum and y may be x or the residual itself, with the same stride; buffers
- * must not overlap otherwise.  rows may be 0. */
+ * width FP16; q: rows x width bytes, scales: `rows` floats (with q).  sum and y may each be x or the residual itself, with the same stride (not both
+ * the same); outputs must not overlap anything otherwise.  rows may be 0. */
 bolt_status bolt_rms_norm(const bolt_rms_norm_desc* desc, const void* x, const void* residual, const void* weight, void* sum, void* y, void* q,
                           void* scales, void* stream);
 
@@ -459,7 +460,7 @@ typedef struct {
 } bolt_gemm_q8_desc;
 
 /* A: M x K (lda) bytes, W: N x K bytes; a_scales: M floats, w_scales: N floats, 16-byte aligned, either may be NULL (1 everywhere); bias: N halves or
- * NULL; D: M x N (ldd) FP16.  M may be 0.  No layer needs a workspace so far (bolt_gemm_q8_workspace_bytes is 0, workspace may be NULL). */
+ * NULL; D: M x N (ldd) FP16, overlaps no input.  M may be 0.  No layer needs a workspace so far (bolt_gemm_q8_workspace_bytes is 0, workspace may be NULL). */
 bolt_status bolt_gemm_q8(const bolt_gemm_q8_desc* desc, const void* A, const void* a_scales, const void* W, const void* w_scales, const void* bias, void* D,
                          void* workspace, size_t workspace_bytes, void* stream);
 size_t bolt_gemm_q8_workspace_bytes(const bolt_gemm_q8_desc* desc);

@@ -6,6 +6,9 @@
 // block's adapters are dealt over `turns` workgroups, and the reduction of low over `parts` more: one compute unit alone reads some 30 GB/s, so that
 // 128 KB of one adapter take it 4 us.  low is rounded to FP16, as every operand of a second product is here; of several parts whoever reads
 // them, which are FP32, adds them up first.
+// What bounds it: of few rows the chain of round trips (ids, operands, sums), of many the staging of x: down for one row of 4096 and rank 16 3.6 us on the
+// GPU, 29 rows of 5000 with 32 adapters of rank 32 4.6, 700 rows of 4096 with 6 of rank 24 5.0, 4096 rows of 4096 with 4 of rank 64, which it reads once, 18;
+// up for 29 rows of 6152 columns 6.0, for 4096 x 8192 38 (67 MB written).
 #pragma once
 #include "routed_rows.hpp"
 

@@ -13,6 +13,9 @@
 // blocks' padding), down 280 to 310 us (670 to 740: 400 MB of FP32 rows leave it).  The matrix cores work 69 and 50 % of the cycles at 1.7 to 1.8 GHz,
 // the L2s miss 31 and 37 % of the requests.  No effect: tiles from a counter instead of dealt out (7.1 rounds take 8), wave groups
 // without rows that leave their MFMAs out, XCDs that start apart, rows stored from registers or through LDS.
+// Linear layers of E4M3, 4096 x 8192 x 4096: 109 us (2.5 PFLOP/s; matrix cores 66 % of the cycles at 2.05 to 2.2 GHz, under the power limit).  FP16 with 4
+// adapters of rank 64 in runs, the same size: 230 us (1.2 PFLOP/s; 69 % at 1.6 to 1.75 GHz).  128 x 128 tiles on half the registers, two workgroups to
+// a compute unit, take as long for one round as for two and lose to rows_tile_kernel (4104 x 4096, 353 rows 50 us, 39 there).
 #pragma once
 #include <type_traits>
 #include <utility>

@@ -4,7 +4,8 @@
 // A workgroup computes 16 MB activation rows x 16 R WN weight rows.  The activation rows are shared by its waves.  The weights are not: a
 // wave owns 16 R weight rows, so 4-bit weights are decoded once per workgroup and never stored.  Both go to LDS directly, S - 1 steps
 // ahead (a round trip to memory is about 2000 cycles, a step over 32 rows some hundred): the weights into a piece that only their
-// wave reads, in the order it reads them, so that no register holds what is on its way and every load is one that can be counted.
+// wave reads (4-bit ones in the order it reads them, FP16 and E4M3 ones in whole lines), so that no register holds what is on its way and every
+// load is one that can be counted.
 // KG sets of WN waves split the reduction (step t to set t % KG) where there are few workgroups; their sums are added through LDS in a
 // fixed order.  One barrier per step.
 // What bounds it: of few rows the instructions of a step (decoding, LDS reads, matrix instructions one behind the other), which several
