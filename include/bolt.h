@@ -422,7 +422,8 @@ typedef struct {
 } bolt_gemm_lora_desc;
 
 /* A: M x K (lda); W: N x K FP16, dense, or bolt_w4_pack(N, K, group, 1); bias: N halves or NULL; ids: M int32; down: [adapters][rank][K], up:
- * [adapters][N][rank], FP16; scales: `adapters` floats or NULL (1); D: M x N (ldd), overlaps no input.  K, N, lda, ldd multiples of 8.  M may be 0. */
+ * [adapters][N][rank], FP16; scales: `adapters` floats or NULL (1); D: M x N (ldd), overlaps no input
+ * (BOLT_ERR_INVALID_ARG where it starts at the same address).  K, N, lda, ldd multiples of 8.  M may be 0. */
 bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const void* W, const void* bias, const void* ids, const void* down,
                            const void* up, const void* scales, void* D, void* workspace, size_t workspace_bytes, void* stream);
 size_t bolt_gemm_lora_workspace_bytes(const bolt_gemm_lora_desc* desc);
@@ -443,7 +444,7 @@ typedef struct {
 
 /* x: rows x width; residual: the same, or NULL (none); weight: `width` halves; outputs, each may be NULL, y or q not both: sum and y: rows x
  * width FP16; q: rows x width bytes, scales: `rows` floats (with q).  sum and y may each be x or the residual itself, with the same stride (not both
- * the same); outputs must not overlap anything otherwise.  rows may be 0. */
+ * the same); outputs must not overlap anything otherwise (BOLT_ERR_INVALID_ARG where they start at the same address).  rows may be 0. */
 bolt_status bolt_rms_norm(const bolt_rms_norm_desc* desc, const void* x, const void* residual, const void* weight, void* sum, void* y, void* q,
                           void* scales, void* stream);
 
@@ -460,7 +461,8 @@ typedef struct {
 } bolt_gemm_q8_desc;
 
 /* A: M x K (lda) bytes, W: N x K bytes; a_scales: M floats, w_scales: N floats, 16-byte aligned, either may be NULL (1 everywhere); bias: N halves or
- * NULL; D: M x N (ldd) FP16, overlaps no input.  M may be 0.  No layer needs a workspace so far (bolt_gemm_q8_workspace_bytes is 0, workspace may be NULL). */
+ * NULL; D: M x N (ldd) FP16, overlaps no input (BOLT_ERR_INVALID_ARG where it
+ * starts at the same address).  M may be 0.  No layer needs a workspace so far (bolt_gemm_q8_workspace_bytes is 0, workspace may be NULL). */
 bolt_status bolt_gemm_q8(const bolt_gemm_q8_desc* desc, const void* A, const void* a_scales, const void* W, const void* w_scales, const void* bias, void* D,
                          void* workspace, size_t workspace_bytes, void* stream);
 size_t bolt_gemm_q8_workspace_bytes(const bolt_gemm_q8_desc* desc);

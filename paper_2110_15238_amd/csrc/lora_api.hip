@@ -165,6 +165,7 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
   const bolt_gemm_lora_desc& d = *desc;
   const LoraWorkspace ws = lora_workspace(d);
   if (!workspace || workspace_bytes < (size_t)ws.bytes) return BOLT_ERR_WORKSPACE;
+  if (starts_at(D, {A, W, bias, ids, down, up, scales, workspace}) || starts_at(workspace, {A, W, bias, ids, down, up, scales})) return BOLT_ERR_INVALID_ARG;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
   const bool w4 = d.weights == BOLT_WEIGHTS_W4, few = on_few_rows(d);

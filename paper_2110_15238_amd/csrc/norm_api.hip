@@ -57,6 +57,11 @@ bolt_status bolt_rms_norm(const bolt_rms_norm_desc* desc, const void* x, const v
   if (!x || !weight || (!y && !q) || (q && !scales)) return BOLT_ERR_INVALID_ARG;
   for (const void* at : {x, residual, weight, (const void*)sum, (const void*)y, (const void*)q, (const void*)scales})
     if (!aligned16(at)) return BOLT_ERR_ALIGNMENT;
+  // sum and y in the place of an input: row by row, value by value
+  const auto in_place = [&](const void* out, int ld) { return d.rows == 1 || ((out != x || ld == d.ldx) && (out != residual || ld == ldr)); };
+  if (starts_at(sum, {y, weight, q, scales}) || starts_at(y, {weight, q, scales}) || starts_at(q, {x, residual, weight, scales}) ||
+      starts_at(scales, {x, residual, weight}) || (sum && !in_place(sum, lds)) || (y && !in_place(y, ldy)))
+    return BOLT_ERR_INVALID_ARG;
   NormParams p{};
   p.x = (const half_t*)x; p.residual = (const half_t*)residual; p.weight = (const half_t*)weight;
   p.sum = (half_t*)sum; p.y = (half_t*)y; p.q = (unsigned char*)q; p.scales = (float*)scales;
@@ -73,6 +78,7 @@ bolt_status bolt_quantize_rows(int32_t rows, int32_t width, int32_t ldx, int32_t
   if (!x || !q || !scales) return BOLT_ERR_INVALID_ARG;
   for (const void* at : {x, (const void*)q, (const void*)scales})
     if (!aligned16(at)) return BOLT_ERR_ALIGNMENT;
+  if (starts_at(q, {x, scales}) || starts_at(scales, {x})) return BOLT_ERR_INVALID_ARG;
   NormParams p{};
   p.x = (const half_t*)x; p.q = (unsigned char*)q; p.scales = (float*)scales;
   p.ldx = ldx; p.ldq = ldq;

@@ -45,6 +45,7 @@ bolt_status bolt_gemm_q8(const bolt_gemm_q8_desc* desc, const void* A, const voi
   if (!A || !W || !D) return BOLT_ERR_INVALID_ARG;
   for (const void* at : {A, a_scales, W, w_scales, bias, (const void*)D, (const void*)workspace})
     if (!aligned16(at)) return BOLT_ERR_ALIGNMENT;
+  if (starts_at(D, {A, a_scales, W, w_scales, bias})) return BOLT_ERR_INVALID_ARG;
   const LayerTile* const tile = desc->M > 16 ? layer_tile(kLayerTiles, desc->M, desc->N, desc->K, true) : nullptr;
   if (desc->M > 16 && !tile) return BOLT_ERR_UNSUPPORTED;
   const half_t* none = no_bias();

@@ -117,6 +117,30 @@ def test_gemm_lora_refusals(bolt):
     assert need > 0 and _lora(bolt, good, ws=None) == WORKSPACE and _lora(bolt, good, ws_bytes=need - 1) == WORKSPACE
 
 
+def test_outputs_in_the_place_of_inputs_are_refused(bolt):
+    """All but the norm's rows over its inputs; everything else stands at an address of its own."""
+    at = lambda *names: {n: 0x1000 * (i + 1) for i, n in enumerate(names)}
+    a = at("x", "residual", "weight", "sum", "y", "q", "scales")
+    d = bolt.rms_norm_desc(4, 64)
+    for out, other in (("sum", "y"), ("sum", "weight"), ("y", "weight"), ("sum", "q"), ("y", "q"), ("q", "x"), ("q", "residual"), ("q", "scales"), ("scales", "x"),
+                       ("scales", "y"), ("scales", "weight")):
+        assert _norm(bolt, d, **{**a, out: a[other]}) == INVALID
+    for out, ld in (("sum", "lds"), ("y", "ldy")):
+        for other in ("x", "residual"):
+            assert _norm(bolt, bolt.rms_norm_desc(4, 64, **{ld: 72}), **{**a, out: a[other]}) == INVALID
+    f = bolt.binding.raw().bolt_quantize_rows
+    assert f(4, 64, 64, 64, 0x1000, 0x1000, 0x2000, None) == INVALID and f(4, 64, 64, 64, 0x1000, 0x2000, 0x2000, None) == INVALID
+    assert f(4, 64, 64, 64, 0x1000, 0x2000, 0x1000, None) == INVALID
+    a = at("A", "sa", "W", "sw", "bias", "D")
+    for other in ("A", "sa", "W", "sw", "bias"):
+        assert _q8(bolt, bolt.gemm_q8_desc(4, 64, 64), **{**a, "D": a[other]}) == INVALID
+    a = at("A", "W", "bias", "ids", "down", "up", "scales", "D", "ws")
+    for other in ("A", "W", "bias", "ids", "down", "up", "scales"):
+        for out in ("D", "ws"):
+            assert _lora(bolt, bolt.gemm_lora_desc(4, 64, 64, 2, 16), **{**a, out: a[other]}) == INVALID
+    assert _lora(bolt, bolt.gemm_lora_desc(4, 64, 64, 2, 16), **{**a, "D": a["ws"]}) == INVALID
+
+
 @pytest.mark.parametrize("N,K,rank,weights,group", [(4096, 4096, 16, "f16", 0), (264, 520, 128, "f16", 0), (4096, 4096, 16, "w4", 64), (72, 4104, 24, "w4", 32)])
 def test_workspace_of_the_adapters_does_not_fall_as_rows_grow(bolt, N, K, rank, weights, group):
     held = [bolt.bolt_gemm_lora_workspace_bytes(bolt.gemm_lora_desc(M, N, K, 7, rank, weights=weights, group=group)) for M in (*range(1, 9000, 7), 1 << 17, 1 << 20)]
