@@ -28,29 +28,29 @@ hipError_t launch_few_rows_w4(const RowsParams& p, int mode, bool gated, int gro
 hipError_t launch_shared_rows_f16(const RowsParams& p, int mode, bool gated, hipStream_t stream);
 hipError_t launch_shared_rows_w4(const RowsParams& p, int mode, bool gated, int group, SharedTile tile, hipStream_t stream);
 // A linear layer's outputs whose tiles of 16 weight rows are marked in p.unpacked, and no others.
-hipError_t launch_shared_rows_w4_marked(const RowsParams& p, int group, hipStream_t stream);
+hipError_t launch_shared_rows_w4_marked(const LayerParams& p, int group, hipStream_t stream);
 hipError_t launch_many_rows_f16(const RowsParams& p, int mode, bool gated, ManyTile tile, hipStream_t stream);
 
 // Linear layers of E4M3 operands: x, ldx, K and steps in pairs (halves); x_scales, w_scales.
 enum class RowsTile { ROWS16_COLS32, ROWS32_COLS32, ROWS64_COLS32, ROWS64_COLS64, ROWS128_COLS64, ROWS128_COLS128, ROWS128_COLS256, ROWS256_COLS256 };
-hipError_t launch_rows_f8(const RowsParams& p, RowsTile tile, hipStream_t stream);
+hipError_t launch_rows_f8(const LayerParams& p, RowsTile tile, hipStream_t stream);
 // Linear layers with FP16 weights, from 64 x 32 to 256 x 256 tiles, that compute the rows' share of their adapters (adapter, low, up, adapters, rank,
 // low_parts; on the largest tiles low is one part), or take it from p.add (not on the largest).
-hipError_t launch_rows_f16_adapters(const RowsParams& p, RowsTile tile, hipStream_t stream);
-hipError_t launch_rows_f16_add(const RowsParams& p, RowsTile tile, hipStream_t stream);
+hipError_t launch_rows_f16_adapters(const LayerParams& p, RowsTile tile, hipStream_t stream);
+hipError_t launch_rows_f16_add(const LayerParams& p, RowsTile tile, hipStream_t stream);
 
 // Linear layers of up to 16 rows whose sums take the rows' adapters (adapter, low, up, adapters, rank).
-hipError_t launch_few_rows_f16_lora(const RowsParams& p, hipStream_t stream);
-hipError_t launch_few_rows_w4_lora(const RowsParams& p, int group, hipStream_t stream);
-// The same from 17 rows on, on 32 x 32, 32 x 64 or 64 x 128 tiles.
-hipError_t launch_shared_rows_w4_lora(const RowsParams& p, int group, SharedTile tile, hipStream_t stream);
+hipError_t launch_few_rows_f16_lora(const LayerParams& p, hipStream_t stream);
+hipError_t launch_few_rows_w4_lora(const LayerParams& p, int group, hipStream_t stream);
+// The same from 17 rows on, on one of the tiles of linear layers: with the share from p.add, or, where that is null and but for 128 x 256, computed there.
+hipError_t launch_shared_rows_w4_lora(const LayerParams& p, int group, SharedTile tile, hipStream_t stream);
 
 // bolt_gemm_w4 behind its checks; `add` (M x N, ldadd, or null): added to A . W^T before alpha, from 17 rows on (csrc/moe_api.hip).
 bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d);
 bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, const half_t* add, int ldadd, void* D,
                         void* workspace, void* stream);
 SharedTile tile_of_gemm_w4(const bolt_gemm_w4_desc& d);  // from 17 rows on, where the weights stay packed
-RowsParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, void* D, const half_t* none);
+LayerParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, void* D, const half_t* none);
 
 // What bolt_gemm_epilogue's own choice of a kernel is estimated to take, in us; false where it has none (csrc/bolt_api.hip).
 bool estimate_gemm(const bolt_gemm_desc& d, double* us);

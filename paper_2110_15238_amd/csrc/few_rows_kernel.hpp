@@ -170,7 +170,7 @@ struct RowsWave {
   // The rows' adapters: acc += up[a] . low^T for every adapter a that one of the rows has, dealt over the waves: two for a wave at most, whose
   // operands are asked for together.  Each sum is taken only where the row's adapter is a: one adapter's infinity does not reach the others' rows.
   template <int NW>
-  __device__ __forceinline__ void add_adapters(int col0, int wave, floatx4 (&acc)[R][MB]) const {
+  __device__ __forceinline__ void add_adapters(const LayerParams& p, int col0, int wave, floatx4 (&acc)[R][MB]) const {
     static_assert(MB == 1 && NW >= 8, "16 rows, no more than two adapters for a wave");
     const int mine = row_adapter(p.adapter, p.adapters, row0 + l16, l16 < rows);
     unsigned left = (unsigned)__ballot(mine >= 0) & 0xffffu;
@@ -257,7 +257,7 @@ struct RowsWave {
 
 // Deep reductions: a wave's steps pass through NB register sets, one tile of columns per workgroup.
 template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NB, bool LORA = false>
-__global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
+__global__ __launch_bounds__(64 * NW) void few_rows_kernel(const std::conditional_t<LORA, LayerParams, RowsParams> p) {
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   extern __shared__ __attribute__((aligned(16))) float part[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(64 * NW) void few_rows_kernel(const RowsParams p) {
   auto multiply = [&](auto b) { w.template multiply<false>(0, wf[decltype(b)::value], xf[decltype(b)::value], acc); };
   // LORA: the adapters' operands are asked for behind the first steps' and multiplied while those arrive.
   auto adapters = [&] {
-    if constexpr (LORA) w.template add_adapters<NW>(col0, wave, acc);
+    if constexpr (LORA) w.template add_adapters<NW>(p, col0, wave, acc);
   };
   if (n >= NB) {
     for_constants<NB>([&](auto b) { load(decltype(b)::value, b); });
@@ -404,7 +404,7 @@ inline int few_rows_tiles(int N) {
 }
 
 template <int WT, int MODE, bool GATED, int NG, int R, int NW, int NB, bool LORA = false>
-hipError_t launch_few_rows(RowsParams p, hipStream_t stream) {
+hipError_t launch_few_rows(std::conditional_t<LORA, LayerParams, RowsParams> p, hipStream_t stream) {
   auto kern = few_rows_kernel<WT, MODE, GATED, NG, R, NW, NB, LORA>;
   using Wave = RowsWave<WT, MODE, GATED, NG, 1, R>;
   constexpr int LDS_BYTES = NW * R * 64 * 16;

@@ -15,7 +15,7 @@ hipError_t launch_few_rows_f16(const RowsParams& p, int mode, bool gated, hipStr
   if (mode == ROWS_DOWN) return launch<ROWS_DOWN, false>(p, stream);
   return gated ? launch<ROWS_UP, true>(p, stream) : launch<ROWS_UP, false>(p, stream);
 }
-hipError_t launch_few_rows_f16_lora(const RowsParams& p, hipStream_t stream) {
+hipError_t launch_few_rows_f16_lora(const LayerParams& p, hipStream_t stream) {
   if (few_rows_tiles(p.N) == 1) return launch_few_rows<WEIGHTS_F16, ROWS_DENSE, false, 1, 1, 8, 3, true>(p, stream);
   return launch_few_rows<WEIGHTS_F16, ROWS_DENSE, false, 1, 2, 8, 3, true>(p, stream);
 }

@@ -36,12 +36,12 @@ hipError_t launch_few_rows_w4(const RowsParams& p, int mode, bool gated, int gro
 }
 // (One tile of columns per workgroup: the walking kernels would wait for the adapters of every tile.)
 template <int NG>
-static hipError_t launch_lora(const RowsParams& p, hipStream_t stream) {
+static hipError_t launch_lora(const LayerParams& p, hipStream_t stream) {
   constexpr int NB = NG == 4 ? 2 : 3;  // (registers, as above; of two tiles the adapters' operands take the third set's)
   if (few_rows_tiles(p.N) == 1) return launch_few_rows<WEIGHTS_W4, ROWS_DENSE, false, NG, 1, 8, NB, true>(p, stream);
   return launch_few_rows<WEIGHTS_W4, ROWS_DENSE, false, NG, 2, 8, 2, true>(p, stream);
 }
-hipError_t launch_few_rows_w4_lora(const RowsParams& p, int group, hipStream_t stream) {
+hipError_t launch_few_rows_w4_lora(const LayerParams& p, int group, hipStream_t stream) {
   if (group == 128) return launch_lora<1>(p, stream);
   if (group == 64) return launch_lora<2>(p, stream);
   return launch_lora<4>(p, stream);

@@ -5,7 +5,7 @@
 #include "shared_rows_kernel.hpp"
 
 namespace bolt {
-hipError_t launch_rows_f8(const RowsParams& p, RowsTile tile, hipStream_t stream) {
+hipError_t launch_rows_f8(const LayerParams& p, RowsTile tile, hipStream_t stream) {
   switch (tile) {
     case RowsTile::ROWS16_COLS32: return launch_shared_rows<WEIGHTS_F8, ROWS_DENSE, false, 1, 1, 1, 2, 4, 3>(p, stream);
     case RowsTile::ROWS32_COLS32: return launch_shared_rows<WEIGHTS_F8, ROWS_DENSE, false, 1, 2, 1, 2, 4, 3>(p, stream);

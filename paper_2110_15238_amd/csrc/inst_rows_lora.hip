@@ -5,7 +5,7 @@
 
 namespace bolt {
 template <int ADD>
-static hipError_t launch(const RowsParams& p, RowsTile tile, hipStream_t stream) {
+static hipError_t launch(const LayerParams& p, RowsTile tile, hipStream_t stream) {
   switch (tile) {
     // rows, columns, waves along either, stages, sets
     case RowsTile::ROWS64_COLS32: return launch_rows_tiles<WEIGHTS_F16, ADD, 64, 32, 2, 1, 3, 4>(p, stream);
@@ -15,9 +15,9 @@ static hipError_t launch(const RowsParams& p, RowsTile tile, hipStream_t stream)
     default: return launch_rows_tiles<WEIGHTS_F16, ADD, 128, 256, 2, 4, 3, 1>(p, stream);
   }
 }
-hipError_t launch_rows_f16_adapters(const RowsParams& p, RowsTile tile, hipStream_t stream) {
+hipError_t launch_rows_f16_adapters(const LayerParams& p, RowsTile tile, hipStream_t stream) {
   if (tile == RowsTile::ROWS256_COLS256) return launch_moe_pp<ROWS_DENSE, false, WEIGHTS_F16, true>(p, stream);
   return launch<FROM_ADAPTERS>(p, tile, stream);
 }
-hipError_t launch_rows_f16_add(const RowsParams& p, RowsTile tile, hipStream_t stream) { return launch<FROM_ADD>(p, tile, stream); }
+hipError_t launch_rows_f16_add(const LayerParams& p, RowsTile tile, hipStream_t stream) { return launch<FROM_ADD>(p, tile, stream); }
 }  // namespace bolt

@@ -24,7 +24,7 @@ static hipError_t launch_group(const RowsParams& p, int group, SharedTile tile, 
   if (group == 64) return launch<MODE, GATED, 2>(p, tile, stream);
   return launch<MODE, GATED, 4>(p, tile, stream);
 }
-hipError_t launch_shared_rows_w4_marked(const RowsParams& p, int group, hipStream_t stream) {
+hipError_t launch_shared_rows_w4_marked(const LayerParams& p, int group, hipStream_t stream) {
   if (group == 128) return launch_shared_rows_marked<1, 8, 2, 8, 3>(p, stream);
   if (group == 64) return launch_shared_rows_marked<2, 8, 2, 8, 3>(p, stream);
   return launch_shared_rows_marked<4, 8, 2, 8, 3>(p, stream);

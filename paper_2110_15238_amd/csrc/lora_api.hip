@@ -182,7 +182,7 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
   l.parts = low_parts(d);
   l.M = d.M; l.N = d.N; l.K = d.K; l.adapters = d.adapters; l.rank = d.rank;
   if (launch_lora_down(l, st) != hipSuccess) return BOLT_ERR_LAUNCH;
-  RowsParams p{};
+  LayerParams p{};
   if (w4) {
     p = dense_w4_rows(base, A, W, bias, D, none);
   } else {

@@ -380,9 +380,9 @@ bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d) {
   return BOLT_OK;
 }
 
-RowsParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, void* D, const half_t* none) {
+LayerParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, void* D, const half_t* none) {
   const W4Format f(d.N, d.K, d.group);
-  RowsParams p{};
+  LayerParams p{};
   p.x = (const half_t*)A;
   p.ldx = d.lda;
   p.w = (const unsigned char*)packed;
@@ -411,10 +411,10 @@ bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* p
   const hipStream_t st = (hipStream_t)stream;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
-  RowsParams p = dense_w4_rows(d, A, packed, bias, D, none);
+  LayerParams p = dense_w4_rows(d, A, packed, bias, D, none);
   p.add = add; p.ldadd = ldadd;
   if (d.M <= 16) return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, d.group, st));
-  if (packed_tiles) return status_of(launch_shared_rows_w4(p, ROWS_DENSE, false, d.group, tile.tile, st));
+  if (packed_tiles) return status_of(add ? launch_shared_rows_w4_lora(p, d.group, tile.tile, st) : launch_shared_rows_w4(p, ROWS_DENSE, false, d.group, tile.tile, st));
   if (launch_w4_unpack(packed, (half_t*)workspace, f, st) != hipSuccess) return BOLT_ERR_LAUNCH;
   if (d.act != BOLT_ACT_SILU) {
     const bolt_gemm_desc g = unpacked_desc(d);

@@ -29,8 +29,10 @@ namespace bolt {
 // twice the rate; sums start at zero and are scaled by row and column in the epilogue.
 // LORA (ROWS_DENSE, FP16): the rows' low-rank adapters are added to a tile's sums in front of its epilogue, by the waves' own matrix cores and
 // from global memory: no pass over the outputs.  A wave's sum is taken only where the row's adapter is the one at hand.
+template <int WT, bool LORA>
+using PpParams = std::conditional_t<WT == WEIGHTS_F8 || LORA, LayerParams, RowsParams>;
 template <int MODE, bool GATED, int WT = WEIGHTS_F16, bool LORA = false>
-__global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
+__global__ __launch_bounds__(512) void moe_pp_kernel(const PpParams<WT, LORA> p) {
   static_assert(!LORA || (WT == WEIGHTS_F16 && MODE == ROWS_DENSE), "adapters: linear layers with FP16 weights");
   static_assert(WT == WEIGHTS_F16 || (WT == WEIGHTS_F8 && MODE == ROWS_DENSE && !GATED), "E4M3: linear layers");
   using T = FpropPpTraits;
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
 
   // Halves: a wave group moves its rows through its own free stage (32 KB), R at a time, so that whole row segments are stored.
   // Floats (DOWN): a quad per lane straight to the slot's row, 64 bytes of a row by four lanes; slot[b] is that of row 16 b + lane % 16.
-  auto add_adapters = [&](const Tile& t) {
+  auto add_adapters = [&](const Tile& t, const auto& p) {
     int elane = lane;
     asm volatile("" : "+v"(elane));  // (as in the epilogue)
     const int eg = elane >> 4, elr = elane & 15, r_half = grp * WTM;
@@ -361,7 +363,7 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
         slot[b] = p.order[cur.row0 + (r < cur.rows ? r : cur.rows - 1)];
       }
     }
-    if constexpr (LORA) add_adapters(cur);
+    if constexpr (LORA) add_adapters(cur, p);
     Scales scales;
     half4 bias[FN];
     if constexpr (WT == WEIGHTS_F8) {
@@ -391,7 +393,7 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const RowsParams p) {
 }
 
 template <int MODE, bool GATED, int WT = WEIGHTS_F16, bool LORA = false>
-hipError_t launch_moe_pp(RowsParams p, hipStream_t stream) {
+hipError_t launch_moe_pp(PpParams<WT, LORA> p, hipStream_t stream) {
   auto kern = moe_pp_kernel<MODE, GATED, WT, LORA>;
   static LdsOptIn opt_in;
   if (hipError_t e = opt_in.ensure((const void*)kern, FpropPpTraits::LDS_BYTES); e != hipSuccess) return e;

@@ -50,7 +50,7 @@ bolt_status bolt_gemm_q8(const bolt_gemm_q8_desc* desc, const void* A, const voi
   if (desc->M > 16 && !tile) return BOLT_ERR_UNSUPPORTED;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
-  RowsParams p{};
+  LayerParams p{};
   p.x = (const half_t*)A; p.ldx = desc->lda / 2;
   p.w = (const unsigned char*)W; p.w_stride = (int64_t)desc->N * desc->K;
   p.x_scales = (const float*)a_scales; p.w_scales = (const float*)w_scales;

@@ -1,12 +1,15 @@
 // What the products over routed lists share: where rows come from and go to, the experts' blocks of rows, SiLU.
 #pragma once
+#include <type_traits>
+
 #include "fprop_dma_kernel.hpp"
 
 namespace bolt {
 
 // WEIGHTS_F8: weights and activations in E4M3.  They move as the halves that two of them fill, so lengths of rows and reductions count those
-// pairs; two pieces of an FP16 operand make one of v_mfma_f32_16x16x128_f8f6f4.
-enum { WEIGHTS_F16 = 0, WEIGHTS_W4 = 1, WEIGHTS_F8 = 2 };
+// pairs; two pieces of an FP16 operand make one of v_mfma_f32_16x16x128_f8f6f4.  (A named type: it is part of kernels' names, and one without a name is
+// counted differently by the compiler's host and device passes.)
+enum WeightKind { WEIGHTS_F16 = 0, WEIGHTS_W4 = 1, WEIGHTS_F8 = 2 };
 // Where a product's rows come from and go to.
 //   DENSE: row m of x, to row m of y.
 //   UP:    rows of the routed list: token order[i] / top_k of x, to row i of y (the list's order).
@@ -56,6 +59,10 @@ struct RowsParams {
   int row_blocks, col_blocks;
   const half_t* unpacked;      // [N][K], for the marks of w4_unpack_kernel
   int walk;                    // tiles of columns that a workgroup walks over
+};
+// What linear layers of E4M3 operands, and those whose rows have adapters, take besides.  (Apart: 90 bytes more of arguments cost the calls of a few us that
+// have no use for them 0.1 to 0.2 us.)
+struct LayerParams : RowsParams {
   const float* x_scales;       // E4M3: of the rows of x and of w, or null
   const float* w_scales;
   const half_t* add;           // [M][N] (ldadd), added to the sums before alpha, or null (linear layers of 4-bit weights, more than 16 rows)
@@ -154,7 +161,7 @@ __device__ __forceinline__ half8 low_operand(const void* low, int64_t at, int pa
 }
 
 // The scales of four columns.
-__device__ __forceinline__ floatx4 column_scales(const RowsParams& p, int n) {
+__device__ __forceinline__ floatx4 column_scales(const LayerParams& p, int n) {
   return p.w_scales ? *(const floatx4*)(p.w_scales + n) : floatx4{1.f, 1.f, 1.f, 1.f};
 }
 

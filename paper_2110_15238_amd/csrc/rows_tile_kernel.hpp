@@ -16,7 +16,7 @@ namespace bolt {
 enum { ADD_NOTHING = 0, FROM_ADD = 1, FROM_ADAPTERS = 2 };
 
 template <int WT, int ADD, int BM, int BN, int WAVES_M, int WAVES_N, int NS, int KG>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N * KG) void rows_tile_kernel(const RowsParams p) {
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N * KG) void rows_tile_kernel(const LayerParams p) {
   constexpr bool F8 = WT == WEIGHTS_F8;
   static_assert(WT != WEIGHTS_W4 && (!F8 || ADD == ADD_NOTHING), "kinds of layers");
   constexpr int BK = 64;  // (E4M3: pairs, 128 values)
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * KG) void rows_tile_kernel(
 }
 
 template <int WT, int ADD, int BM, int BN, int WAVES_M, int WAVES_N, int NS, int KG>
-hipError_t launch_rows_tiles(RowsParams p, hipStream_t stream) {
+hipError_t launch_rows_tiles(LayerParams p, hipStream_t stream) {
   using T = FpropDmaTraits<BM, BN, 64, WAVES_M, WAVES_N, 0, NS, KG>;
   static_assert(T::LDS_BYTES <= 160 * 1024, "stages");
   auto kern = rows_tile_kernel<WT, ADD, BM, BN, WAVES_M, WAVES_N, NS, KG>;

@@ -41,29 +41,33 @@ struct SharedRowsTraits {
 };
 
 // The rows' adapters (linear layers): acc += up[a] . low^T for every adapter a that one of the rows has, adapter i by set i % KG of the waves, 64 ranks at
-// a time: the rows' low once, then up of one adapter after the other, the next one's on its way.  A sum is taken only where the row's adapter is a.
+// a time (of 64 rows 32: registers): the rows' low once, then up of one adapter after the other, the next one's on its way.  A sum is taken only where the
+// row's adapter is a.
 template <int MB, int R, int KG>
-__device__ __forceinline__ void add_adapters_by_sets(const RowsParams& p, int row0, int rows, int col0, int kg, int lane, floatx4 (&acc)[R][MB]) {
+__device__ __forceinline__ void add_adapters_by_sets(const LayerParams& p, int row0, int rows, int col0, int kg, int lane, floatx4 (&acc)[R][MB]) {
   static_assert(MB <= 4, "a row for each lane");
+  constexpr int KD = MB < 4 ? 2 : 1;  // matrix instructions, 32 ranks each
   const int g = lane >> 4, l16 = lane & 15;
   const int mine = row_adapter(p.adapter, p.adapters, row0 + lane, lane < rows);
   int of_row[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) of_row[b] = __shfl(mine, b * 16 + l16);
   const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int k0 = 0; k0 < p.rank; k0 += 64) {
+  for (int k0 = 0; k0 < p.rank; k0 += 32 * KD) {
     // (ranks beyond the last are zero on both sides)
-    const int at[2] = {k0 + g * 8, k0 + 32 + g * 8};
-    const bool two = k0 + 32 < p.rank;  // (the same for all lanes)
-    auto load = [&](int a, half8 (&u)[R][2]) {
+    auto at = [&](int k) { return k0 + 32 * k + g * 8; };
+    auto any = [&](int k) { return k0 + 32 * k < p.rank; };  // (the same for all lanes)
+    auto load = [&](int a, half8 (&u)[R][KD]) {
       const half_t* const up = p.up + (int64_t)a * p.N * p.rank;
 #pragma unroll
       for (int t = 0; t < R; ++t) {
         const int n = col0 + t * 16 + l16;
         const half_t* const from = up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank;
-        u[t][0] = *(const half8*)(from + (at[0] < p.rank ? at[0] : 0));
-        u[t][1] = zero;
-        if (two) u[t][1] = *(const half8*)(from + (at[1] < p.rank ? at[1] : 0));
+#pragma unroll
+        for (int k = 0; k < KD; ++k) {
+          u[t][k] = zero;
+          if (any(k)) u[t][k] = *(const half8*)(from + (at(k) < p.rank ? at(k) : 0));
+        }
       }
     };
     unsigned long long left = __ballot(mine >= 0);
@@ -80,33 +84,32 @@ __device__ __forceinline__ void add_adapters_by_sets(const RowsParams& p, int ro
     };
     int now = take();
     if (now < 0) return;
-    half8 up[2][R][2], low[MB][2];
+    half8 up[2][R][KD], low[MB][KD];
     load(now, up[0]);
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
       const int j = b * 16 + l16;
       const int64_t row = (int64_t)(row0 + (j < rows ? j : rows - 1)) * p.rank;
-      const half8 v = low_operand(p.low, row + (at[0] < p.rank ? at[0] : 0), p.low_parts, (int64_t)p.M * p.rank);
-      low[b][0] = at[0] < p.rank ? v : zero;
-      low[b][1] = zero;
-      if (two) {
-        const half8 v = low_operand(p.low, row + (at[1] < p.rank ? at[1] : 0), p.low_parts, (int64_t)p.M * p.rank);
-        low[b][1] = at[1] < p.rank ? v : zero;
+#pragma unroll
+      for (int k = 0; k < KD; ++k) {
+        low[b][k] = zero;
+        if (any(k)) {
+          const half8 v = low_operand(p.low, row + (at(k) < p.rank ? at(k) : 0), p.low_parts, (int64_t)p.M * p.rank);
+          low[b][k] = at(k) < p.rank ? v : zero;
+        }
       }
     }
-    auto multiply = [&](int a, const half8 (&u)[R][2]) {
+    auto multiply = [&](int a, const half8 (&u)[R][KD]) {
 #pragma unroll
-      for (int t = 0; t < R; ++t) {
-        const half8 u0 = at[0] < p.rank ? u[t][0] : zero, u1 = at[1] < p.rank ? u[t][1] : zero;
+      for (int t = 0; t < R; ++t)
 #pragma unroll
         for (int b = 0; b < MB; ++b) {
           floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-          sum = mfma_16x16x32(u0, low[b][0], sum);
-          sum = mfma_16x16x32(u1, low[b][1], sum);
+#pragma unroll
+          for (int k = 0; k < KD; ++k) sum = mfma_16x16x32(at(k) < p.rank ? u[t][k] : zero, low[b][k], sum);
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[t][b][e] += of_row[b] == a ? sum[e] : 0.f;
         }
-      }
     };
     while (now >= 0) {
       const int next = take();
@@ -120,8 +123,11 @@ __device__ __forceinline__ void add_adapters_by_sets(const RowsParams& p, int ro
   }
 }
 
-template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S, bool LORA = false>
-__device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<WT, MODE, GATED, NG, MB, R>& w, int wave_all, int cb, half_t* lds) {
+// MORE (linear layers of 4-bit weights): the adapters' share, from p.add where that is given, else, up to 64 rows, computed here.
+template <int WT, bool MORE>
+using SharedParams = std::conditional_t<WT == WEIGHTS_F8 || MORE, LayerParams, RowsParams>;
+template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S, bool MORE = false>
+__device__ __forceinline__ void shared_rows_tile(const SharedParams<WT, MORE>& p, RowsWave<WT, MODE, GATED, NG, MB, R>& w, int wave_all, int cb, half_t* lds) {
   using T = SharedRowsTraits<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
   using Wave = RowsWave<WT, MODE, GATED, NG, MB, R>;
   constexpr int BM = T::BM, KS = T::KS;
@@ -268,7 +274,8 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
 #pragma unroll
   for (int t = 0; t < S - 1; ++t) load(t, ring + t * T::STAGE);
   // (while the first steps' loads are on their way)
-  if constexpr (LORA) add_adapters_by_sets<MB, R, KG>(p, w.row0, w.rows, col0, kg, lane, acc);
+  if constexpr (MORE && MB <= 4)
+    if (!p.add) add_adapters_by_sets<MB, R, KG>(p, w.row0, w.rows, col0, kg, lane, acc);
   int stage = 0, fill = S - 1;
   const int all = KG > 1 ? p.steps / KG : turns;  // turns that every set has
   for (int t = 0; t < all; ++t) {
@@ -316,7 +323,7 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
         return v;
       };
       if constexpr (WT == WEIGHTS_F8) acc[a][b] *= column_scales(p, col) * (p.x_scales ? p.x_scales[w.row0 + j] : 1.f);
-      if constexpr (WT == WEIGHTS_W4 && MODE == ROWS_DENSE) {
+      if constexpr (MORE) {
         if (p.add) {
           const half4 more = *(const half4*)(p.add + to * p.ldadd + col);
 #pragma unroll
@@ -338,8 +345,8 @@ __device__ __forceinline__ void shared_rows_tile(const RowsParams& p, RowsWave<W
   }
 }
 
-template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S, bool LORA = false>
-__global__ __launch_bounds__(64 * WN * KG) void shared_rows_kernel(const RowsParams p) {
+template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S, bool MORE = false>
+__global__ __launch_bounds__(64 * WN * KG, MORE && MB <= 4 ? 4 : 1) void shared_rows_kernel(const SharedParams<WT, MORE> p) {
   using T = SharedRowsTraits<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
   constexpr int BM = T::BM;
   extern __shared__ __attribute__((aligned(16))) half_t lds[];
@@ -365,12 +372,12 @@ __global__ __launch_bounds__(64 * WN * KG) void shared_rows_kernel(const RowsPar
     w.row0 = at.lo + done;
     w.rows = at.n - done < BM ? at.n - done : BM;
   }
-  shared_rows_tile<WT, MODE, GATED, NG, MB, R, WN, KG, S, LORA>(p, w, __builtin_amdgcn_readfirstlane(tid >> 6), cb, lds);
+  shared_rows_tile<WT, MODE, GATED, NG, MB, R, WN, KG, S, MORE>(p, w, __builtin_amdgcn_readfirstlane(tid >> 6), cb, lds);
 }
 
 // The tiles of columns that hold marked weights (w4_unpack_kernel), all rows; a workgroup whose columns hold none reads 16 numbers and ends.
 template <int NG, int MB, int R, int WN, int S>
-__global__ __launch_bounds__(64 * WN) void shared_rows_marked_kernel(const RowsParams p) {
+__global__ __launch_bounds__(64 * WN) void shared_rows_marked_kernel(const LayerParams p) {
   using T = SharedRowsTraits<WEIGHTS_W4, ROWS_DENSE, false, NG, MB, R, WN, 1, S>;
   extern __shared__ __attribute__((aligned(16))) half_t lds[];
   const int tid = threadIdx.x, lane = tid & 63, cb = blockIdx.x;
@@ -381,14 +388,15 @@ __global__ __launch_bounds__(64 * WN) void shared_rows_marked_kernel(const RowsP
     RowsWave<WEIGHTS_W4, ROWS_DENSE, false, NG, MB, R> w(p, lane);
     w.row0 = rb * T::BM;
     w.rows = p.M - w.row0 < T::BM ? p.M - w.row0 : T::BM;
-    shared_rows_tile<WEIGHTS_W4, ROWS_DENSE, false, NG, MB, R, WN, 1, S>(p, w, __builtin_amdgcn_readfirstlane(tid >> 6), cb, lds);
+    static_assert(MB > 4, "a share is in memory, if there is one");
+    shared_rows_tile<WEIGHTS_W4, ROWS_DENSE, false, NG, MB, R, WN, 1, S, true>(p, w, __builtin_amdgcn_readfirstlane(tid >> 6), cb, lds);
   }
 }
 
-template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S, bool LORA = false>
-hipError_t launch_shared_rows(RowsParams p, hipStream_t stream) {
-  static_assert(!LORA || (WT == WEIGHTS_W4 && MODE == ROWS_DENSE), "adapters: linear layers of 4-bit weights");
-  auto kern = shared_rows_kernel<WT, MODE, GATED, NG, MB, R, WN, KG, S, LORA>;
+template <int WT, int MODE, bool GATED, int NG, int MB, int R, int WN, int KG, int S, bool MORE = false>
+hipError_t launch_shared_rows(SharedParams<WT, MORE> p, hipStream_t stream) {
+  static_assert(!MORE || (WT == WEIGHTS_W4 && MODE == ROWS_DENSE), "adapters: linear layers of 4-bit weights");
+  auto kern = shared_rows_kernel<WT, MODE, GATED, NG, MB, R, WN, KG, S, MORE>;
   using T = SharedRowsTraits<WT, MODE, GATED, NG, MB, R, WN, KG, S>;
   static LdsOptIn opt_in;
   if (hipError_t e = opt_in.ensure((const void*)kern, T::LDS_BYTES); e != hipSuccess) return e;
@@ -398,7 +406,7 @@ hipError_t launch_shared_rows(RowsParams p, hipStream_t stream) {
   return hipGetLastError();
 }
 template <int NG, int MB, int R, int WN, int S>
-hipError_t launch_shared_rows_marked(RowsParams p, hipStream_t stream) {
+hipError_t launch_shared_rows_marked(LayerParams p, hipStream_t stream) {
   auto kern = shared_rows_marked_kernel<NG, MB, R, WN, S>;
   using T = SharedRowsTraits<WEIGHTS_W4, ROWS_DENSE, false, NG, MB, R, WN, 1, S>;
   static LdsOptIn opt_in;
