@@ -42,14 +42,14 @@ hipError_t launch_rows_f16_add(const LayerParams& p, RowsTile tile, hipStream_t 
 // Linear layers of up to 16 rows whose sums take the rows' adapters (adapter, low, up, adapters, rank).
 hipError_t launch_few_rows_f16_lora(const LayerParams& p, hipStream_t stream);
 hipError_t launch_few_rows_w4_lora(const LayerParams& p, int group, hipStream_t stream);
-// The same from 17 rows on, on one of the tiles of linear layers: with the share from p.add, or, where that is null and but for 128 x 256, computed there.
+// The same on one of the tiles of linear layers: with the share from p.add, or, where that is null and but for 128 x 256, computed there.
 hipError_t launch_shared_rows_w4_lora(const LayerParams& p, int group, SharedTile tile, hipStream_t stream);
 
-// bolt_gemm_w4 behind its checks; `add` (M x N, ldadd, or null): added to A . W^T before alpha, from 17 rows on (csrc/moe_api.hip).
+// bolt_gemm_w4 behind its checks; `add` (M x N, ldadd, or null): added to A . W^T before alpha (csrc/moe_api.hip).
 bolt_status check_gemm_w4(const bolt_gemm_w4_desc* d);
 bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, const half_t* add, int ldadd, void* D,
                         void* workspace, void* stream);
-SharedTile tile_of_gemm_w4(const bolt_gemm_w4_desc& d);  // from 17 rows on, where the weights stay packed
+SharedTile tile_of_gemm_w4(const bolt_gemm_w4_desc& d);  // where the weights stay packed
 LayerParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, void* D, const half_t* none);
 
 // What bolt_gemm_epilogue's own choice of a kernel is estimated to take, in us; false where it has none (csrc/bolt_api.hip).

@@ -14,7 +14,14 @@ constexpr int kDownGroups = 256, kMostParts = kMostLowParts;
 
 // Whether the projection runs on the kernel for up to 16 rows, which adds the adapters itself: some more rows too, where all of their blocks are on the
 // chip at once (2048 x 8192 in 4 bits with 32 adapters, 17 to 32 rows: 19.8 us so, 24 on tiles of 32 rows behind lora_up_kernel; FP16 25 and 25).
-bool on_few_rows(const bolt_gemm_lora_desc& d) { return d.M <= 16 || (d.M <= 64 && blocks_of(d.M, 16) * blocks_of(d.N, 16) <= 256); }
+// Of wide projections, more than two tiles of 16 columns for each compute unit, the tiles have more than 8 rows (12 where groups of 32 make decoding dearer):
+// us, 9 and 16 rows with 32 adapters of rank 24, few rows / tiles: FP16 8200 x 4096 24.8 and 29.1 / 22.0 and 22.5, 12288 x 5000 38.6 and 46.9 / 37.6 and 41.2;
+// 4 bits, groups of 128, 21.1 and 24.9 / 18.6 and 19.9, 22.2 and 25.4 / 21.0 and 22.8, of 32 21.9 and 26.4 / 20.4 and 21.8, 22.7 and 26.8 / 23.3 and 25.0;
+// FP16 6152 x 5000 with rank 16, 16 rows 20.4 / 22.7.
+bool on_few_rows(const bolt_gemm_lora_desc& d) {
+  const bool narrow = d.N <= 16 * 512, dear = d.weights == BOLT_WEIGHTS_W4 && d.group == 32;
+  return (d.M <= 16 && (narrow || d.M <= (dear ? 12 : 8))) || (d.M <= 64 && blocks_of(d.M, 16) * blocks_of(d.N, 16) <= 256);
+}
 
 bolt_gemm_w4_desc base_w4(const bolt_gemm_lora_desc& d) { return {d.M, d.N, d.K, d.lda, d.ldd, d.group, d.alpha, d.beta, d.act}; }
 

@@ -403,17 +403,18 @@ SharedTile tile_of_gemm_w4(const bolt_gemm_w4_desc& d) { return dense_tile(d.M, 
 bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, const half_t* add, int ldadd, void* D,
                         void* workspace, void* stream) {
   const W4Format f(d.N, d.K, d.group);
-  const DenseTile& tile = d.M > 16 ? dense_tile(d.M, d.N, f.steps, d.group) : kDenseTiles[0];
+  const bool tiled = d.M > 16 || add;  // (the kernel of few rows takes no share)
+  const DenseTile& tile = tiled ? dense_tile(d.M, d.N, f.steps, d.group) : kDenseTiles[0];
   // The kernels of many rows start their sums at beta / alpha times the bias, which has to be finite.
   const bool bias_in_sum = d.alpha != 0.f && std::fabs(d.beta) <= 1e30f * std::fabs(d.alpha);
-  const bool packed_tiles = d.M > 16 && (!bias_in_sum || !dense_unpacks(d));
+  const bool packed_tiles = tiled && (!bias_in_sum || !dense_unpacks(d));
   if (packed_tiles && !launches(blocks_of(d.M, tile.rows) * blocks_of(d.N, tile.cols))) return BOLT_ERR_UNSUPPORTED;
   const hipStream_t st = (hipStream_t)stream;
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
   LayerParams p = dense_w4_rows(d, A, packed, bias, D, none);
   p.add = add; p.ldadd = ldadd;
-  if (d.M <= 16) return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, d.group, st));
+  if (!tiled) return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, d.group, st));
   if (packed_tiles) return status_of(add ? launch_shared_rows_w4_lora(p, d.group, tile.tile, st) : launch_shared_rows_w4(p, ROWS_DENSE, false, d.group, tile.tile, st));
   if (launch_w4_unpack(packed, (half_t*)workspace, f, st) != hipSuccess) return BOLT_ERR_LAUNCH;
   if (d.act != BOLT_ACT_SILU) {

@@ -344,6 +344,18 @@ def test_gemm_lora_of_few_adapters_on_packed_tiles(bolt, M, N, K, n, rank, group
     assert torch.equal(again[others], D[others]) and not torch.isfinite(again[~others]).all()
 
 
+@pytest.mark.parametrize("M,N,K,n,rank", [(8, 8200, 264, 5, 24), (9, 8200, 264, 5, 24), (12, 12296, 136, 16, 8), (13, 12296, 136, 40, 72), (16, 8208, 1032, 3, 16), (16, 8192, 264, 3, 16)])
+@pytest.mark.parametrize("weights,group", [("f16", 0), ("w4", 32), ("w4", 128)])
+@pytest.mark.parametrize("how", ["runs", "mixed"])
+def test_gemm_lora_of_wide_projections(bolt, M, N, K, n, rank, weights, group, how):
+    """Few rows, on the kernel for them and on tiles; a share that goes through memory, and alpha 0."""
+    D, want, c = _lora(bolt, M, N, K, n, rank, weights, group, how)
+    rows.within(D, *want())
+    c["d"].alpha = 0.0
+    D = bolt.bolt_gemm_lora(c["d"], c["A"], c["W"], c["bias"], c["ids"], c["down"], c["up"], c["scales"], _nan(M, N), c["ws"])
+    assert torch.equal(D, (c["bias"].float() * -1.5).half().expand(M, N))
+
+
 @pytest.mark.parametrize("how", ["runs", "mixed"])
 def test_gemm_lora_over_unpacked_weights(bolt, how):
     M, N, K = 4096, 8192, 1032
