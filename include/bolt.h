@@ -409,8 +409,9 @@ size_t bolt_moe_workspace_bytes(const bolt_moe_desc* desc);
 /* ---- A projection shared by requests that each bring a low-rank adapter --------------------------------------------
  *   D[m] = act(alpha * (A[m] . W^T + scales[a] * (A[m] . down[a]^T) . up[a]^T) + beta * bias),  a = ids[m];
  * a row whose id is below zero, or no less than `adapters`, has no adapter and is A[m] . W^T alone.  scales[a] * (A[m] . down[a]^T) is rounded to
- * FP16 (the next product's operand; infinite beyond 65504).  Where more adapters can meet in a tile than it adds by itself, a row's share
- * (... . up[a]^T) goes through memory and is rounded to FP16 once more.  An adapter's infinities and NaN reach its own rows only. */
+ * FP16 (the next product's operand; infinite beyond 65504); a row's share (... . up[a]^T) is FP32, as all sums are.  Where more adapters can meet in a
+ * tile than it adds by itself, by the sizes and `adapters`, the share goes through the workspace: a row's last bits can depend on how many adapters
+ * and rows there are, its range does not.  An adapter's infinities and NaN reach its own rows only. */
 typedef struct {
   int32_t M, N, K;
   int32_t lda, ldd;       /* in elements; A and D are row-major */

@@ -12,12 +12,10 @@ static hipError_t launch(const LayerParams& p, RowsTile tile, hipStream_t stream
     case RowsTile::ROWS64_COLS64: return launch_rows_tiles<WEIGHTS_F16, ADD, 64, 64, 2, 2, 3, 2>(p, stream);
     case RowsTile::ROWS128_COLS64: return launch_rows_tiles<WEIGHTS_F16, ADD, 128, 64, 4, 1, 3, 2>(p, stream);
     case RowsTile::ROWS128_COLS128: return launch_rows_tiles<WEIGHTS_F16, ADD, 128, 128, 2, 2, 3, 1>(p, stream);
-    default: return launch_rows_tiles<WEIGHTS_F16, ADD, 128, 256, 2, 4, 3, 1>(p, stream);
+    case RowsTile::ROWS128_COLS256: return launch_rows_tiles<WEIGHTS_F16, ADD, 128, 256, 2, 4, 3, 1>(p, stream);
+    default: return launch_moe_pp<ROWS_DENSE, false, WEIGHTS_F16, ADD>(p, stream);
   }
 }
-hipError_t launch_rows_f16_adapters(const LayerParams& p, RowsTile tile, hipStream_t stream) {
-  if (tile == RowsTile::ROWS256_COLS256) return launch_moe_pp<ROWS_DENSE, false, WEIGHTS_F16, true>(p, stream);
-  return launch<FROM_ADAPTERS>(p, tile, stream);
-}
+hipError_t launch_rows_f16_adapters(const LayerParams& p, RowsTile tile, hipStream_t stream) { return launch<FROM_ADAPTERS>(p, tile, stream); }
 hipError_t launch_rows_f16_add(const LayerParams& p, RowsTile tile, hipStream_t stream) { return launch<FROM_ADD>(p, tile, stream); }
 }  // namespace bolt

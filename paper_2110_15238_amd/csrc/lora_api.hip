@@ -35,27 +35,24 @@ bolt_status check_gemm_lora(const bolt_gemm_lora_desc* d) {
   }
   if ((d->N | d->K | d->lda | d->ldd | d->rank) & 7) return BOLT_ERR_ALIGNMENT;
   if (d->lda > kMaxLength || d->ldd > kMaxLength || d->rank > kMaxRank || d->M > kMaxRows) return BOLT_ERR_UNSUPPORTED;
-  // the launches of 64 x 256 outputs and of 16 rows here, and those of the projection
+  // the launches of 64 x 256 outputs and of 16 rows
   if (!launches(blocks_of(d->M, 16)) || !launches(blocks_of(d->M, 64) * blocks_of(d->N, 256))) return BOLT_ERR_UNSUPPORTED;
-  if (d->weights == BOLT_WEIGHTS_F16 && !launches(blocks_of(d->M, 32) * blocks_of(d->N, 32))) return BOLT_ERR_UNSUPPORTED;  // (bolt_gemm_epilogue's)
   return BOLT_OK;
 }
 
-// The workspace: low [parts][M][rank]; of 4-bit weights that may be unpacked the unpacked ones and the adapters' share [M][N] (which otherwise goes through D:
-// there the rows with weights beyond FP16's range are computed a second time).
+// The workspace: low [parts][M][rank], the adapters' share [M][N] in FP32 (whichever kernel runs, so that the size does not fall as M grows) and 4-bit
+// weights that may be unpacked.
 struct LoraWorkspace {
-  int64_t weights_at, share_at, bytes;
+  int64_t share_at, weights_at, bytes;
 };
 LoraWorkspace lora_workspace(const bolt_gemm_lora_desc& d) {
   LoraWorkspace w;
   // (a bound of parts * M that does not fall as M grows)
-  w.weights_at = w.share_at = w.bytes = round_up(std::max<int64_t>(d.M, std::min<int64_t>((int64_t)kMostParts * d.M, 16 * kDownGroups)) * d.rank * 4, 256);
+  w.share_at = round_up(std::max<int64_t>(d.M, std::min<int64_t>((int64_t)kMostParts * d.M, 16 * kDownGroups)) * d.rank * 4, 256);
+  w.weights_at = w.bytes = w.share_at + round_up((int64_t)d.M * d.N * 4, 256);
   if (d.weights == BOLT_WEIGHTS_W4) {
     const bolt_gemm_w4_desc base = base_w4(d);
-    if (const size_t unpacked = bolt_gemm_w4_workspace_bytes(&base); unpacked > 0) {
-      w.share_at = w.weights_at + round_up((int64_t)unpacked, 256);
-      w.bytes = w.share_at + round_up((int64_t)d.M * d.N * 2, 256);
-    }
+    w.bytes += round_up((int64_t)bolt_gemm_w4_workspace_bytes(&base), 256);
   }
   return w;
 }
@@ -121,13 +118,14 @@ hipError_t launch_lora_up(const LoraParams& p, hipStream_t stream) {
 constexpr LayerTile kLayerTiles[] = {{RowsTile::ROWS64_COLS32, 64, 32, 4, 2.5, 0.70},      {RowsTile::ROWS64_COLS64, 64, 64, 2, 2.2, 0.49},
                                      {RowsTile::ROWS128_COLS64, 128, 64, 2, 2.0, 0.68},    {RowsTile::ROWS128_COLS128, 128, 128, 1, 1.0, 0.58},
                                      {RowsTile::ROWS128_COLS256, 128, 256, 1, 0.0, 0.90},  {RowsTile::ROWS256_COLS256, 256, 256, 1, 9.4, 1.26}};
-const LayerTile* projection_tile(const bolt_gemm_lora_desc& d) {
+template <typename D>
+const LayerTile* projection_tile(const D& d) {
   const bool bias_in_sum = d.alpha != 0.f && std::fabs(d.beta) <= 1e30f * std::fabs(d.alpha);
   return layer_tile(kLayerTiles, d.M, d.N, (int64_t)d.K * 2, bias_in_sum);
 }
 // Whether the tiles compute the adapters' share.  Where the rows of a request lie together a tile has one or two adapters, which cost it 1 to 3 us (256 x 256:
 // 7); each further one 0.5 (2.4), and how many there are the host does not know: it asks that the most there can be cost no more than the share's way
-// through memory (lora_up_kernel: 6.5 us for 700 x 4104, 38 for 4096 x 8192).
+// through memory (lora_up_kernel: 47 us for 4096 x 8192).
 bool adapters_in_tiles(const bolt_gemm_lora_desc& d, const LayerTile& t) {
   const double most = std::min(d.adapters, std::min(t.rows, d.M)) * (t.tile == RowsTile::ROWS256_COLS256 ? 2.4 : 0.5);
   return layer_rounds(t, d.M, d.N) * most <= 3.5 + 1.1e-6 * d.M * d.N;
@@ -151,6 +149,12 @@ int low_parts(const bolt_gemm_lora_desc& d) {
 }
 
 }  // namespace
+
+hipError_t launch_projection_f16_add(const LayerParams& p, hipStream_t stream) {
+  const LayerTile* const tile = projection_tile(p);
+  return tile ? launch_rows_f16_add(p, tile->tile, stream) : hipErrorInvalidConfiguration;
+}
+
 }  // namespace bolt
 
 using namespace bolt;
@@ -206,17 +210,11 @@ bolt_status bolt_gemm_lora(const bolt_gemm_lora_desc* desc, const void* A, const
   if (few) return status_of(w4 ? launch_few_rows_w4_lora(p, d.group, st) : launch_few_rows_f16_lora(p, st));
   if (tile && adapters_in_tiles(d, *tile)) return status_of(launch_rows_f16_adapters(p, tile->tile, st));
   if (w4 && adapters_in_w4_tiles(d)) return status_of(launch_shared_rows_w4_lora(p, d.group, tile_of_gemm_w4(base), st));
-  const bool apart = ws.share_at != ws.weights_at;
-  l.y = apart ? (half_t*)((char*)workspace + ws.share_at) : (half_t*)D;
-  l.ldy = apart ? d.N : d.ldd;
+  l.share = (float*)((char*)workspace + ws.share_at);
   if (launch_lora_up(l, st) != hipSuccess) return BOLT_ERR_LAUNCH;
-  if (w4) return run_gemm_w4(base, A, W, bias, l.y, (int)l.ldy, D, (char*)workspace + ws.weights_at, stream);
-  if (tile->tile != RowsTile::ROWS256_COLS256) {
-    p.add = (const half_t*)D; p.ldadd = d.ldd;
-    return status_of(launch_rows_f16_add(p, tile->tile, st));
-  }
-  const bolt_gemm_desc g = {d.M, d.N, d.K, d.lda, d.K, d.ldd, d.alpha, d.beta, d.act, BOLT_LAYOUT_NK};
-  return bolt_gemm_epilogue_residual(&g, A, W, bias, D, d.ldd, d.alpha, D, nullptr, nullptr, 0, stream);
+  if (w4) return run_gemm_w4(base, A, W, bias, l.share, D, (char*)workspace + ws.weights_at, stream);
+  p.add = l.share;
+  return status_of(launch_rows_f16_add(p, tile->tile, st));
 }
 
 }  // extern "C"

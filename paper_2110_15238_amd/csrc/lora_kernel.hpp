@@ -8,7 +8,7 @@
 // them, which are FP32, adds them up first.
 // What bounds it: of few rows the chain of round trips (ids, operands, sums), of many the staging of x: down for one row of 4096 and rank 16 3.6 us on the
 // GPU, 29 rows of 5000 with 32 adapters of rank 32 4.6, 700 rows of 4096 with 6 of rank 24 5.0, 4096 rows of 4096 with 4 of rank 64, which it reads once, 18;
-// up for 29 rows of 6152 columns 6.0, for 4096 x 8192 38 (67 MB written).
+// up for 29 rows of 6152 columns 6.0, for 4096 x 8192 47 (134 MB written; 37 when it wrote halves).
 #pragma once
 #include "routed_rows.hpp"
 
@@ -23,8 +23,7 @@ struct LoraParams {
   const float* scales;    // [adapters], or null: 1
   const half_t* none;     // eight zeros
   void* low;              // one part: [M][rank] halves, else [parts][M][rank] floats
-  half_t* y;              // [M][N] (ldy)
-  int64_t ldy;
+  float* share;           // [M][N]
   int M, N, K, adapters, rank;
   int parts, turns, tiles, blocks;  // tiles: of 16 RT ranks (down) or of columns (up); blocks: of rows
 };
@@ -141,9 +140,10 @@ __global__ __launch_bounds__(64 * NW) void lora_down_kernel(const LoraParams p) 
   });
 }
 
-// y = up[a] . low of every row, zero for rows without an adapter: 16 MB rows x 256 columns for a workgroup, 64 columns for each of its four
-// waves.  The columns of a wave's four tiles are interleaved, so that a lane holds 16 neighbouring ones of a row and four lanes a whole line.
-// Each row is stored by the workgroup that has its adapter's turn, those without one by the first.
+// share = up[a] . low of every row, zero for rows without an adapter: 16 MB rows x 256 columns for a workgroup, 64 columns for each of its four
+// waves, of which four lanes store 64 bytes of a row at a time.
+// Each row is stored by the workgroup that has its adapter's turn, those without one by the first.  It stays FP32: what the layer adds it to, and alpha,
+// can bring a sum beyond binary16's range back into it, and tiles that compute the share themselves hold it so.
 template <int MB>
 __global__ __launch_bounds__(256) void lora_up_kernel(const LoraParams p) {
   constexpr int BM = 16 * MB;
@@ -163,18 +163,14 @@ __global__ __launch_bounds__(256) void lora_up_kernel(const LoraParams p) {
     of_row[b] = __shfl(mine, j);
     low[b] = (int64_t)(row0 + (j < rows ? j : rows - 1)) * p.rank + g * 8;
   }
-  const int from = col0 + (l16 >> 2) * 16 + (l16 & 3);  // + 4 t: the column of this lane's weight row in tile t
   auto store = [&](int a, const floatx4 (&v)[4][MB]) {
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
       if (b * 16 + l16 >= rows || of_row[b] != a) continue;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = col0 + g * 16 + h * 8;
-        half8 o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (half_t)v[2 * h][b][e], o[4 + e] = (half_t)v[2 * h + 1][b][e];
-        if (c < p.N) *(half8*)(p.y + (int64_t)(row0 + b * 16 + l16) * p.ldy + c) = o;
+      for (int t = 0; t < 4; ++t) {
+        const int c = col0 + t * 16 + g * 4;
+        if (c < p.N) *(floatx4*)(p.share + (int64_t)(row0 + b * 16 + l16) * p.N + c) = v[t][b];
       }
     }
   };
@@ -201,7 +197,7 @@ __global__ __launch_bounds__(256) void lora_up_kernel(const LoraParams p) {
       half8 u[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const int n = from + 4 * t;
+        const int n = col0 + t * 16 + l16;
         u[t] = *(const half8*)(up + (int64_t)(n < p.N ? n : p.N - 1) * p.rank + (in ? k * 32 : -g * 8));
       }
 #pragma unroll

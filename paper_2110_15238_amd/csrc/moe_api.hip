@@ -400,8 +400,8 @@ LayerParams dense_w4_rows(const bolt_gemm_w4_desc& d, const void* A, const void*
 
 SharedTile tile_of_gemm_w4(const bolt_gemm_w4_desc& d) { return dense_tile(d.M, d.N, W4Format(d.N, d.K, d.group).steps, d.group).tile; }
 
-bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, const half_t* add, int ldadd, void* D,
-                        void* workspace, void* stream) {
+bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* packed, const void* bias, const float* add, void* D, void* workspace,
+                        void* stream) {
   const W4Format f(d.N, d.K, d.group);
   const bool tiled = d.M > 16 || add;  // (the kernel of few rows takes no share)
   const DenseTile& tile = tiled ? dense_tile(d.M, d.N, f.steps, d.group) : kDenseTiles[0];
@@ -413,20 +413,21 @@ bolt_status run_gemm_w4(const bolt_gemm_w4_desc& d, const void* A, const void* p
   const half_t* none = no_bias();
   if (!none) return BOLT_ERR_LAUNCH;
   LayerParams p = dense_w4_rows(d, A, packed, bias, D, none);
-  p.add = add; p.ldadd = ldadd;
+  p.add = add;
   if (!tiled) return status_of(launch_few_rows_w4(p, ROWS_DENSE, false, d.group, st));
   if (packed_tiles) return status_of(add ? launch_shared_rows_w4_lora(p, d.group, tile.tile, st) : launch_shared_rows_w4(p, ROWS_DENSE, false, d.group, tile.tile, st));
   if (launch_w4_unpack(packed, (half_t*)workspace, f, st) != hipSuccess) return BOLT_ERR_LAUNCH;
-  if (d.act != BOLT_ACT_SILU) {
-    const bolt_gemm_desc g = unpacked_desc(d);
-    const bolt_status s = add ? bolt_gemm_epilogue_residual(&g, A, workspace, bias, add, ldadd, d.alpha, D, nullptr, nullptr, 0, stream)
-                              : bolt_gemm_epilogue(&g, A, workspace, bias, D, nullptr, nullptr, 0, stream);
-    if (s != BOLT_OK) return s;
-  } else {
-    RowsParams u = p;
-    u.w = (const unsigned char*)workspace;
-    u.w_stride = (int64_t)p.N * p.K * 2;
+  LayerParams u = p;
+  u.w = (const unsigned char*)workspace;
+  u.w_stride = (int64_t)p.N * p.K * 2;
+  u.steps = (int)blocks_of(p.K, 64);
+  if (add) {
+    if (launch_projection_f16_add(u, st) != hipSuccess) return BOLT_ERR_LAUNCH;
+  } else if (d.act == BOLT_ACT_SILU) {
     if (launch_many_rows_f16(u, ROWS_DENSE, false, ManyTile::ROWS256, st) != hipSuccess) return BOLT_ERR_LAUNCH;
+  } else {
+    const bolt_gemm_desc g = unpacked_desc(d);
+    if (bolt_status s = bolt_gemm_epilogue(&g, A, workspace, bias, D, nullptr, nullptr, 0, stream); s != BOLT_OK) return s;
   }
   p.unpacked = (const half_t*)workspace;
   return status_of(launch_shared_rows_w4_marked(p, d.group, st));
@@ -469,7 +470,7 @@ bolt_status bolt_gemm_w4(const bolt_gemm_w4_desc* desc, const void* A, const voi
   const size_t need = bolt_gemm_w4_workspace_bytes(desc);
   if (need > 0 && (!workspace || workspace_bytes < need)) return BOLT_ERR_WORKSPACE;
   if (!aligned16(workspace)) return BOLT_ERR_ALIGNMENT;
-  return run_gemm_w4(*desc, A, packed, bias, nullptr, 0, D, workspace, stream);
+  return run_gemm_w4(*desc, A, packed, bias, nullptr, D, workspace, stream);
 }
 
 size_t bolt_moe_route_workspace_bytes(const bolt_moe_route_desc* desc) {

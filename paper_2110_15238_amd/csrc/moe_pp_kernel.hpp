@@ -27,13 +27,14 @@ namespace bolt {
 
 // WT: WEIGHTS_F8 for linear layers in E4M3 (ROWS_DENSE): bytes move as for FP16, a C phase has half the instructions, each of twice the depth and
 // twice the rate; sums start at zero and are scaled by row and column in the epilogue.
-// LORA (ROWS_DENSE, FP16): the rows' low-rank adapters are added to a tile's sums in front of its epilogue, by the waves' own matrix cores and
-// from global memory: no pass over the outputs.  A wave's sum is taken only where the row's adapter is the one at hand.
-template <int WT, bool LORA>
-using PpParams = std::conditional_t<WT == WEIGHTS_F8 || LORA, LayerParams, RowsParams>;
-template <int MODE, bool GATED, int WT = WEIGHTS_F16, bool LORA = false>
-__global__ __launch_bounds__(512) void moe_pp_kernel(const PpParams<WT, LORA> p) {
-  static_assert(!LORA || (WT == WEIGHTS_F16 && MODE == ROWS_DENSE), "adapters: linear layers with FP16 weights");
+// ADD (ROWS_DENSE, FP16): the rows' low-rank adapters are added to a tile's sums in front of its epilogue.  FROM_ADAPTERS by the waves' own matrix
+// cores and from global memory, with no pass over the outputs; a wave's sum is taken only where the row's adapter is the one at hand.  FROM_ADD takes the
+// share from memory, where lora_up_kernel left it.
+template <int WT, int ADD>
+using PpParams = std::conditional_t<WT == WEIGHTS_F8 || ADD != ADD_NOTHING, LayerParams, RowsParams>;
+template <int MODE, bool GATED, int WT = WEIGHTS_F16, int ADD = ADD_NOTHING>
+__global__ __launch_bounds__(512) void moe_pp_kernel(const PpParams<WT, ADD> p) {
+  static_assert(ADD == ADD_NOTHING || (WT == WEIGHTS_F16 && MODE == ROWS_DENSE), "adapters: linear layers with FP16 weights");
   static_assert(WT == WEIGHTS_F16 || (WT == WEIGHTS_F8 && MODE == ROWS_DENSE && !GATED), "E4M3: linear layers");
   using T = FpropPpTraits;
   constexpr int BM = 256, BN = T::BN, BK = T::BK, WTM = BM / 2, WTN = T::WTN;
@@ -177,13 +178,11 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const PpParams<WT, LORA> p)
     }
   };
 
-  // Halves: a wave group moves its rows through its own free stage (32 KB), R at a time, so that whole row segments are stored.
-  // Floats (DOWN): a quad per lane straight to the slot's row, 64 bytes of a row by four lanes; slot[b] is that of row 16 b + lane % 16.
   auto add_adapters = [&](const Tile& t, const auto& p) {
     int elane = lane;
     asm volatile("" : "+v"(elane));  // (as in the epilogue)
     const int eg = elane >> 4, elr = elane & 15, r_half = grp * WTM;
-    static_assert(!LORA || WTM == 128, "two rows for each lane");
+    static_assert(ADD == ADD_NOTHING || WTM == 128, "two rows for each lane");
     int mine[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) mine[h] = row_adapter(p.adapter, p.adapters, t.row0 + r_half + h * 64 + elane, r_half + h * 64 + elane < t.rows);
@@ -242,10 +241,32 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const PpParams<WT, LORA> p)
       }
     }
   };
+  // (16 of the lane's 32 quads at a time, and nothing kept from one turn to the next: more does not fit the registers)
+  auto add_share = [&](const Tile& t, const auto& p) {
+    constexpr int ASKED = 16;
+    const char* const share = (const char*)(p.add + (int64_t)t.row0 * p.N);  // (256 rows of 2^21 floats: offsets of 32 bits)
+    for_constants<FN * FM / ASKED>([&](auto turn) {
+      int elane = lane;
+      asm volatile("" : "+v"(elane));
+      floatx4 more[ASKED];
+      for_constants<ASKED>([&](auto i) {
+        constexpr int q = decltype(turn)::value * ASKED + decltype(i)::value;
+        const int r = grp * WTM + q % FM * 16 + (elane & 15), c = t.c0 + column(q / FM, elane >> 4);
+        more[i] = *(const floatx4*)(share + ((unsigned)(r < t.rows ? r : t.rows - 1) * (unsigned)p.N + (unsigned)(c < p.N ? c : 0)) * 4u);
+      });
+      for_constants<ASKED>([&](auto i) {
+        constexpr int q = decltype(turn)::value * ASKED + decltype(i)::value;
+        acc[q / FM][q % FM] += more[i];
+        asm volatile("" : "+v"(acc[q / FM][q % FM]));  // (added here, not where the epilogue uses it)
+      });
+    });
+  };
   struct Scales {  // E4M3: of the lane's rows and columns
     float row[FM];
     floatx4 col[FN];
   };
+  // Halves: a wave group moves its rows through its own free stage (32 KB), R at a time, so that whole row segments are stored.
+  // Floats (DOWN): a quad per lane straight to the slot's row, 64 bytes of a row by four lanes; slot[b] is that of row 16 b + lane % 16.
   auto epilogue = [&](const Tile& t, const int (&slot)[FM], const Scales& scales, const half4 (&bias)[FN]) {
     int elane = lane;
     asm volatile("" : "+v"(elane));  // (as in fprop_pp_kernel: the addresses below are not to live through the k loop)
@@ -363,7 +384,8 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const PpParams<WT, LORA> p)
         slot[b] = p.order[cur.row0 + (r < cur.rows ? r : cur.rows - 1)];
       }
     }
-    if constexpr (LORA) add_adapters(cur, p);
+    if constexpr (ADD == FROM_ADAPTERS) add_adapters(cur, p);
+    if constexpr (ADD == FROM_ADD) add_share(cur, p);
     Scales scales;
     half4 bias[FN];
     if constexpr (WT == WEIGHTS_F8) {
@@ -392,9 +414,9 @@ __global__ __launch_bounds__(512) void moe_pp_kernel(const PpParams<WT, LORA> p)
   }
 }
 
-template <int MODE, bool GATED, int WT = WEIGHTS_F16, bool LORA = false>
-hipError_t launch_moe_pp(PpParams<WT, LORA> p, hipStream_t stream) {
-  auto kern = moe_pp_kernel<MODE, GATED, WT, LORA>;
+template <int MODE, bool GATED, int WT = WEIGHTS_F16, int ADD = ADD_NOTHING>
+hipError_t launch_moe_pp(PpParams<WT, ADD> p, hipStream_t stream) {
+  auto kern = moe_pp_kernel<MODE, GATED, WT, ADD>;
   static LdsOptIn opt_in;
   if (hipError_t e = opt_in.ensure((const void*)kern, FpropPpTraits::LDS_BYTES); e != hipSuccess) return e;
   constexpr int COLS = GATED ? FpropPpTraits::BN / 2 : FpropPpTraits::BN, kComputeUnits = 256;

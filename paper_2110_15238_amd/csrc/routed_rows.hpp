@@ -65,8 +65,7 @@ struct RowsParams {
 struct LayerParams : RowsParams {
   const float* x_scales;       // E4M3: of the rows of x and of w, or null
   const float* w_scales;
-  const half_t* add;           // [M][N] (ldadd), added to the sums before alpha, or null (linear layers of 4-bit weights, more than 16 rows)
-  int64_t ldadd;
+  const float* add;            // [M][N], added to the sums before alpha (the adapters' share, where it goes through memory), or null
   // low-rank adapters (linear layers)
   const int* adapter;          // of each row; none below zero and from `adapters` on
   const void* low;             // scale * x . down^T of each row's adapter: [M][rank] halves, or [low_parts][M][rank] floats to be added up
@@ -164,6 +163,9 @@ __device__ __forceinline__ half8 low_operand(const void* low, int64_t at, int pa
 __device__ __forceinline__ floatx4 column_scales(const LayerParams& p, int n) {
   return p.w_scales ? *(const floatx4*)(p.w_scales + n) : floatx4{1.f, 1.f, 1.f, 1.f};
 }
+
+// Where a kernel of tiles takes the adapters' share from: nowhere, LayerParams::add, or low and up (computed in the tile).
+enum LayerShare { ADD_NOTHING = 0, FROM_ADD = 1, FROM_ADAPTERS = 2 };
 
 // Direct-to-LDS loads from any address: lane l's 16 (4) bytes go to `to` + 16 l (4 l).
 __device__ __forceinline__ void lds_load16(const void* from, half_t* to) {

@@ -13,8 +13,6 @@
 
 namespace bolt {
 
-enum { ADD_NOTHING = 0, FROM_ADD = 1, FROM_ADAPTERS = 2 };
-
 template <int WT, int ADD, int BM, int BN, int WAVES_M, int WAVES_N, int NS, int KG>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * KG) void rows_tile_kernel(const LayerParams p) {
   constexpr bool F8 = WT == WEIGHTS_F8;
@@ -53,7 +51,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * KG) void rows_tile_kernel(
   half4 bias[FN][4];
   floatx4 col_scale[F8 ? FN : 1][4];
   float row_scale[F8 ? FM : 1];
-  half4 add[ADD == FROM_ADD ? FN : 1][4][FM];
+  floatx4 add[ADD == FROM_ADD ? FN : 1][4][FM];
   dma_main_loop<BM, BN, BK, WAVES_M, WAVES_N, NS, KG, (F8 && T::G < 2 ? 2 : T::G), (T::DEEP || T::NW < 8 ? 2 : 3), false, F8>(
       xl, wl, lds + kg * T::GROUP_HALVES, none, kg, (p.steps + KG - 1) / KG, wm, wn, lane, acc, [&] {
         if (kg > 0) return;
@@ -75,7 +73,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * KG) void rows_tile_kernel(
 #pragma unroll
               for (int q = 0; q < 4; ++q) {
                 const int c = n0 + column(a, q);
-                add[a][q][b] = *(const half4*)(p.add + (int64_t)row * p.ldadd + (c < p.N ? c : 0));
+                add[a][q][b] = *(const floatx4*)(p.add + (int64_t)row * p.N + (c < p.N ? c : 0));
               }
         }
       });
@@ -199,9 +197,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * KG) void rows_tile_kernel(
         for (int b = 0; b < FM; ++b) {
           floatx4 v = {acc[a][b][q * 4], acc[a][b][q * 4 + 1], acc[a][b][q * 4 + 2], acc[a][b][q * 4 + 3]};
           if constexpr (F8) v *= col_scale[a][q] * row_scale[b];
-          if constexpr (ADD == FROM_ADD)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += (float)add[a][q][b][e];
+          if constexpr (ADD == FROM_ADD) v += add[a][q][b];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = p.alpha * v[e] + p.beta * (float)bias[a][q][e];
           v = apply_act4(v, p.act);

@@ -305,16 +305,39 @@ __device__ __forceinline__ void shared_rows_tile(const SharedParams<WT, MORE>& p
         for (int b = 0; b < MB; ++b) acc[a][b] += *(const floatx4*)(sums + ((k * WN + wave) * R * MB + a * MB + b) * 256 + lane * 4);
   }
 
+  int g = w.g, l16 = w.l16;
+  if constexpr (MORE) {
+    // (the lane's number anew: kept through the loop above it would be spilled)
+    int elane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+    asm volatile("" : "+v"(elane));
+    g = elane >> 4;
+    l16 = elane & 15;
+    // the share from memory, all of a lane's quads asked for together
+    if (p.add) {
+      const float* const share = p.add + (int64_t)w.row0 * p.N;
+#pragma unroll
+      for (int a = 0; a < R; ++a) {
+        const int col = col0 + a * 16 + g * 4, n = col < p.N ? col : 0;
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+          const int j = b * 16 + l16;
+          acc[a][b] += *(const floatx4*)(share + ((unsigned)(j < w.rows ? j : w.rows - 1) * (unsigned)p.N + (unsigned)n));  // (128 rows of 2^21 at most)
+          asm volatile("" : "+v"(acc[a][b]));  // (added here, not where it is stored)
+        }
+      }
+    }
+  }
+
   // ---- out: four columns of one row per accumulator ------------------------------------------------------------------
   const int outputs = GATED ? p.hidden : p.N;
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
-    const int j = b * 16 + w.l16;
+    const int j = b * 16 + l16;
     if (j >= w.rows) continue;
     const int64_t to = MODE == ROWS_DOWN ? p.order[w.row0 + j] : w.row0 + j;
 #pragma unroll
     for (int a = 0; a < R; a += GATED ? 2 : 1) {
-      const int col = col0 + (GATED ? a / 2 : a) * 16 + w.g * 4;
+      const int col = col0 + (GATED ? a / 2 : a) * 16 + g * 4;
       if (col >= outputs) continue;
       auto with_bias = [&](floatx4 v, int n) {
         const half4 hb = *(const half4*)(p.bias + (w.expert * (int64_t)p.N + n) * p.bias_on);
@@ -323,13 +346,6 @@ __device__ __forceinline__ void shared_rows_tile(const SharedParams<WT, MORE>& p
         return v;
       };
       if constexpr (WT == WEIGHTS_F8) acc[a][b] *= column_scales(p, col) * (p.x_scales ? p.x_scales[w.row0 + j] : 1.f);
-      if constexpr (MORE) {
-        if (p.add) {
-          const half4 more = *(const half4*)(p.add + to * p.ldadd + col);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[a][b][e] += (float)more[e];
-        }
-      }
       floatx4 v = with_bias(acc[a][b], col);
       v = apply_act4(v, p.act);
       if constexpr (GATED) v *= with_bias(acc[a + 1][b], p.hidden + col);

@@ -1,0 +1,28 @@
+"""Sizes of 8-bit layers and of projections with adapters, each with the kernel that it is meant for: the GPU tests run them, a host test checks that the
+library's choice of a kernel still gives them these, so that a new estimate of the times does not leave a kernel without a test."""
+
+# Projections whose adapters' share goes through memory, by a table of `n` adapters: (M, N, K, n, rank, weights, group), the kernel that adds it.  The rows ask
+# for two of them only; with a table of these two the same rows are computed in the tiles, but on packed tiles of 128 x 256 and on unpacked weights.
+SHARE = [
+    ((115, 1000, 600, 40, 24, "f16", 0), "rows_tile_kernel<0,1,64,32,2,1,3,4>"),
+    ((10, 8200, 264, 9, 24, "f16", 0), "rows_tile_kernel<0,1,64,64,2,2,3,2>"),
+    ((300, 4104, 1032, 40, 72, "f16", 0), "rows_tile_kernel<0,1,128,64,4,1,3,2>"),
+    ((700, 4104, 264, 40, 40, "f16", 0), "rows_tile_kernel<0,1,128,128,2,2,3,1>"),
+    ((1500, 4104, 1032, 90, 24, "f16", 0), "rows_tile_kernel<0,1,128,256,2,4,3,1>"),
+    ((1100, 10248, 1288, 90, 40, "f16", 0), "moe_pp_kernel<0,0,0,1>"),
+    ((10, 12296, 264, 16, 128, "w4", 128), "shared_rows_kernel<1,0,0,1,2,1,4,2,3,1>"),
+    ((40, 4104, 520, 40, 72, "w4", 32), "shared_rows_kernel<1,0,0,4,2,1,4,2,3,1>"),
+    ((103, 16, 280, 52, 8, "w4", 64), "shared_rows_kernel<1,0,0,2,2,1,2,4,3,1>"),
+    ((100, 4104, 264, 40, 24, "w4", 64), "shared_rows_kernel<1,0,0,2,2,1,4,2,3,1>"),
+    ((300, 8200, 264, 40, 24, "w4", 32), "shared_rows_kernel<1,0,0,4,4,1,8,1,3,1>"),
+    ((300, 8200, 264, 40, 24, "w4", 64), "shared_rows_kernel<1,0,0,2,4,1,8,1,3,1>"),
+    ((400, 4104, 264, 40, 24, "w4", 128), "shared_rows_kernel<1,0,0,1,4,1,8,1,3,1>"),
+    ((500, 12296, 264, 40, 24, "w4", 32), "shared_rows_kernel<1,0,0,4,8,2,8,1,3,1>"),
+    ((500, 12296, 264, 40, 24, "w4", 64), "shared_rows_kernel<1,0,0,2,8,2,8,1,3,1>"),
+    ((500, 12296, 264, 40, 24, "w4", 128), "shared_rows_kernel<1,0,0,1,8,2,8,1,3,1>"),
+    ((2207, 256, 3696, 9, 88, "w4", 32), "rows_tile_kernel<0,1,64,64,2,2,3,2>"),
+    ((4752, 344, 3800, 5, 32, "w4", 128), "rows_tile_kernel<0,1,128,64,4,1,3,2>"),
+    ((1950, 1040, 1064, 58, 16, "w4", 64), "rows_tile_kernel<0,1,128,128,2,2,3,1>"),
+    ((2901, 4232, 152, 5, 80, "w4", 128), "rows_tile_kernel<0,1,128,256,2,4,3,1>"),
+    ((1300, 10248, 1288, 90, 40, "w4", 32), "moe_pp_kernel<0,0,0,1>"),
+]

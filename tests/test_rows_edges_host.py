@@ -1,0 +1,46 @@
+"""CPU-only: which kernels run 8-bit layers and projections with adapters, in a process whose HIP runtime is tests/hip_recorder.c."""
+import os
+
+import pytest
+
+import rows_cases as cases
+from test_host_launches import run  # noqa: F401  (the fixture)
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+pytestmark = pytest.mark.skipif(not os.path.exists(os.path.join(ROOT, "paper_2110_15238_amd", "libbolt.so")),
+                                reason="libbolt.so not built (run __graft_entry__.build())")
+
+CALLS = """
+import re
+at = lambda i: 0x100000 * (i + 1)
+
+def kernels():  # name<template arguments> of what was launched
+    out = []
+    for name in rec.recorder_launches().decode().split():
+        m = re.match(r"_ZN4bolt(\\d+)", name)
+        n, rest = int(m.group(1)), name[m.end():]
+        if rest.startswith("_GLOBAL__N_1"): m = re.match(r"_GLOBAL__N_1(\\d+)", rest); n, rest = int(m.group(1)), rest[m.end():]
+        args = re.match(r"I((?:L[ib]n?\\d+E)*)", rest[n:])
+        out.append(rest[:n] + "<" + ",".join(re.findall(r"L[ib](n?\\d+)E", args.group(1) if args else "")) + ">")
+    return out
+
+def q8(M, N, K, **k):
+    d = b.gemm_q8_desc(M, N, K, **k)
+    s = lib.bolt_gemm_q8(C.byref(d), at(0), at(1), at(2), at(3), at(4), at(5), None, 0, None)
+    return s, kernels()
+
+def lora(M, N, K, n, rank, weights="f16", group=0, **k):
+    d = b.gemm_lora_desc(M, N, K, n, rank, weights=weights, group=group, **k)
+    s = lib.bolt_gemm_lora(C.byref(d), *map(at, range(9)), 1 << 60, None)
+    return s, kernels()
+"""
+
+
+def test_projections_whose_share_goes_through_memory(run):  # noqa: F811
+    run(CALLS + """
+for size, kernel in %r:
+    s, k = lora(*size)
+    assert s == 0 and any(x.startswith("lora_up_kernel") for x in k) and kernel in k, (size, k)
+    small = lora(*size[:3], 2, *size[4:])[1]
+    assert any(x.startswith("lora_up_kernel") for x in small) == (size[5] == "w4" and ("w4_unpack_kernel" in str(k) or ",8,2,8,1,3,1>" in kernel)), (size, small)
+""" % (cases.SHARE,))
