@@ -17,8 +17,8 @@
  *     that is 0).
  *   - The return value is the only error channel.  Descriptors are validated before anything is
  *     launched, so every error except BOLT_ERR_LAUNCH can be produced without a GPU.
- *   - Accumulation is FP32 on the matrix cores; the epilogue runs in FP32 and converts once to
- *     FP16 with round-to-nearest-even.
+ *   - Accumulation is FP32 on the matrix cores (of E4M3 products with the limit that bolt_gemm_q8
+ *     states); the epilogue runs in FP32 and converts once to FP16 with round-to-nearest-even.
  *   - Alignment (Section 3.2.3, "Kernel padding"): 128-bit accesses need every channel count,
  *     reduction length and leading dimension to be a multiple of 8, else BOLT_ERR_ALIGNMENT;
  *     pad with bolt_pad_channels_nhwc first.  The one exception is the input channel count of
@@ -453,7 +453,9 @@ bolt_status bolt_rms_norm(const bolt_rms_norm_desc* desc, const void* x, const v
  * (an infinity: infinite scale).  For activations that no norm precedes, and for weights [N][K], whose scales are then the columns' of the product. */
 bolt_status bolt_quantize_rows(int32_t rows, int32_t width, int32_t ldx, int32_t ldq, const void* x, void* q, void* scales, void* stream);
 
-/* D[m][n] = act(alpha * a_scales[m] * w_scales[n] * sum over k of A[m][k] * W[n][k] + beta * bias[n]), A and W in E4M3. */
+/* D[m][n] = act(alpha * a_scales[m] * w_scales[n] * sum over k of A[m][k] * W[n][k] + beta * bias[n]), A and W in E4M3.
+ * The sum is FP32 over groups of eight neighbouring k.  Within a group the matrix cores align the products to that of the largest exponent, 2^E, and cut each
+ * towards zero below 2^(E - 13): seven of eight can lose less than that each.  Next to FP16's rounding it shows where few groups cancel (K below some hundred). */
 typedef struct {
   int32_t M, N, K;
   int32_t lda, ldd; /* in elements; A, W (N x K, dense) and D are row-major.  N, ldd multiples of 8, K, lda of 16 */
