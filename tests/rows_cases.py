@@ -26,3 +26,10 @@ SHARE = [
     ((2901, 4232, 152, 5, 80, "w4", 128), "rows_tile_kernel<0,1,128,256,2,4,3,1>"),
     ((1300, 10248, 1288, 90, 40, "w4", 32), "moe_pp_kernel<0,0,0,1>"),
 ]
+
+# 8-bit layers on 256 x 256 tiles: one round and several, six rows in the last row block, eight columns in the last tile, reductions that end inside a step,
+# one of a single step.
+Q8_LARGE = [(262, 22344, 1296), (527, 13456, 1296), (19742, 1032, 1040), (4365, 16688, 144), (16866, 8200, 16)]
+
+# Weights on both sides of 2 GiB, (N, K) of E4M3 and of FP16 ones: 256 x 256 tiles address them with 31 bits and give way beyond.
+Q8_WEIGHTS, F16_WEIGHTS = ((131064, 16384), (131080, 16384)), ((65528, 16384), (65544, 16384))

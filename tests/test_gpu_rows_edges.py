@@ -68,3 +68,96 @@ def test_q8_of_short_reductions(bolt, M, N, K):  # noqa: F811
     A, W = near(M), near(N)
     D = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K), A, None, W, None, None, _nan(M, N))
     assert torch.equal(D, (A.double() @ W.double().t().contiguous()).half())
+
+
+# ---- 8-bit layers on 256 x 256 tiles ------------------------------------------------------------------------------------
+def _rows_of(M):
+    """The rows that are compared: all of few, of many those of the first row block, of some in the middle and of the last."""
+    return torch.arange(M, device="cuda") if M < 1000 else torch.cat([torch.arange(a, b, device="cuda") for a, b in ((0, 300), (M // 2, M // 2 + 200), (M - 300, M))])
+
+
+@pytest.mark.parametrize("M,N,K", cases.Q8_LARGE)
+@pytest.mark.parametrize("act,full", [("none", False), ("silu", True), ("gelu", True), ("softplus", True)])
+def test_large_q8(bolt, M, N, K, act, full):  # noqa: F811
+    g = _gen(M + N + K)
+    (A, sa), (W, sw) = _q8(g, M, K), _q8(g, N, K, std=1 / math.sqrt(K))
+    bias = _half(g, N) if full else None
+    d = bolt.gemm_q8_desc(M, N, K, act=act, alpha=0.75 if full else 1.0, beta=-1.5)
+    D, at = bolt.bolt_gemm_q8(d, A, sa, W, sw, bias, _nan(M, N)), _rows_of(M)
+    rows.within(D[at], *_layer(A[at], sa[at], W, sw, None if bias is None else bias.double(), act, d.alpha, d.beta))
+
+
+@pytest.mark.parametrize("M,N,K", cases.Q8_LARGE)
+def test_large_q8_is_exact_on_integers(bolt, M, N, K):  # noqa: F811
+    """Small integers and scales that are powers of two, all rows and columns: a value in a wrong place, a lost column or a scale of another row shows."""
+    g = _gen(M + K)
+    integers = lambda R: torch.randint(-2, 3, (R, K), device="cuda", generator=g).float().to(F8)
+    powers = lambda R: 2.0 ** torch.randint(-2, 1, (R,), device="cuda", generator=g).float()
+    A, W, sa, sw, bias = integers(M), integers(N), powers(M), powers(N), torch.randint(-4, 5, (N,), device="cuda", generator=g).half()
+    sums = A.float() @ W.float().t()  # (whole numbers far below 2^24: exact)
+    assert sums.abs().max() <= 1024
+    D = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K), A, sa, W, sw, None, _nan(M, N))
+    assert torch.equal(D, (sums * sa[:, None] * sw[None, :]).half())
+    D = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K, act="relu"), A, None, W, None, bias, _nan(M, N))
+    assert torch.equal(D, (sums + bias.float()).clamp(min=0).half())
+
+
+@pytest.mark.parametrize("M,N,K", [(262, 22344, 1296), (19742, 1032, 1040)])
+def test_large_q8_strides_and_untouched_padding(bolt, M, N, K):  # noqa: F811
+    lda, ldd = K + 48, N + 56
+    g = _gen(M)
+    (a, sa), (W, sw) = _q8(g, M, K), _q8(g, N, K)
+    A = _nan(M, lda, dtype=F8)
+    A.view(torch.uint8)[:, :K] = a.view(torch.uint8)
+    D, at = torch.full((M, ldd), 7.0, dtype=torch.float16, device="cuda"), _rows_of(M)
+    bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K, lda=lda, ldd=ldd), A, sa, W, sw, None, D)
+    rows.within(D[at][:, :N], *_layer(a[at], sa[at], W, sw, None))
+    assert (D[:, N:] == 7.0).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(262, 22344, 1296), (19742, 1032, 1040), (4365, 16688, 144)])
+def test_large_q8_rows_and_columns_do_not_meet(bolt, M, N, K):  # noqa: F811
+    """A NaN in a row or an infinity in its scale spoils that row only, a NaN in a weight row that column only."""
+    g = _gen(M)
+    (A, sa), (W, sw) = _q8(g, M, K), _q8(g, N, K, std=0.1)
+    clean = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K), A, sa, W, sw, None, _nan(M, N))
+    A.view(torch.uint8)[M - 2, 5], W.view(torch.uint8)[N - 2, K - 1] = 0x7f, 0x7f
+    sa[7] = float("inf")
+    D = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K), A, sa, W, sw, None, _nan(M, N))
+    keep_r, keep_c = torch.ones(M, dtype=torch.bool, device="cuda"), torch.ones(N, dtype=torch.bool, device="cuda")
+    keep_r[M - 2] = keep_r[7] = keep_c[N - 2] = False
+    assert torch.isnan(D[M - 2]).all() and torch.isnan(D[:, N - 2]).all() and not torch.isfinite(D[7]).any()
+    assert torch.equal(D[keep_r][:, keep_c], clean[keep_r][:, keep_c])
+
+
+@pytest.mark.parametrize("M,N,K", cases.Q8_LARGE)
+def test_large_q8_of_bias_alone(bolt, M, N, K):  # noqa: F811
+    """alpha 0: -1.5 times the bias is a number of FP32, rounded once."""
+    g = _gen(M)
+    (A, sa), (W, sw), bias = _q8(g, M, K), _q8(g, N, K), _half(g, N)
+    D = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K, alpha=0.0, beta=-1.5), A, sa, W, sw, bias, _nan(M, N))
+    assert torch.equal(D, (bias.float() * -1.5).half().expand(M, N))
+
+
+# ---- weights on both sides of 2 GiB -------------------------------------------------------------------------------------
+@pytest.mark.parametrize("N,K", cases.Q8_WEIGHTS)
+def test_q8_of_weights_about_2_gib(bolt, N, K):  # noqa: F811
+    """On 256 x 256 tiles up to the last byte that 31 bits reach, on others beyond."""
+    M, g = 520, _gen(8)
+    W = torch.randint(0, 256, (N, K), dtype=torch.uint8, device="cuda", generator=g).bitwise_and_(0xb7).view(F8)  # (below 1, of both signs)
+    A, sa = _q8(g, M, K)
+    D = bolt.bolt_gemm_q8(bolt.gemm_q8_desc(M, N, K), A, sa, W, None, None, _nan(M, N))
+    for at in (slice(0, 300), slice(N // 2, N // 2 + 300), slice(N - 300, N)):
+        rows.within(D[:, at], *_layer(A, sa, W[at], None, None))
+
+
+@pytest.mark.parametrize("N,K", cases.F16_WEIGHTS)
+@pytest.mark.parametrize("n", [2, 600])
+def test_projections_of_weights_about_2_gib(bolt, N, K, n):  # noqa: F811
+    M, rank, g = 520, 8, _gen(9)
+    A, W, down, up = _half(g, M, K), _half(g, N, K, std=0.01), _half(g, n, rank, K, std=0.01), _half(g, n, N, rank, std=0.1)
+    ids = torch.randint(-1, 2, (M,), dtype=torch.int32, device="cuda", generator=g)
+    d = bolt.gemm_lora_desc(M, N, K, n, rank)
+    D = bolt.bolt_gemm_lora(d, A, W, None, ids, down, up, None, _nan(M, N), _nan(bolt.bolt_gemm_lora_workspace_bytes(d), dtype=torch.uint8))
+    for at in (slice(0, 300), slice(N // 2, N // 2 + 300), slice(N - 300, N)):
+        rows.within(D[:, at], *rows.lora(A.double(), W[at].double(), None, ids, down[:2], up[:2, at], None, "none", apart=False))

@@ -44,3 +44,24 @@ for size, kernel in %r:
     small = lora(*size[:3], 2, *size[4:])[1]
     assert any(x.startswith("lora_up_kernel") for x in small) == (size[5] == "w4" and ("w4_unpack_kernel" in str(k) or ",8,2,8,1,3,1>" in kernel)), (size, small)
 """ % (cases.SHARE,))
+
+
+def test_8_bit_layers_on_the_largest_tiles(run):  # noqa: F811
+    run(CALLS + """
+for size in %r:
+    for alpha in (1.0, 0.0):
+        assert q8(*size, alpha=alpha) == (0, ["moe_pp_kernel<0,0,2,0>"]), size
+""" % (cases.Q8_LARGE,))
+
+
+@pytest.mark.parametrize("M", [520, 4096])
+def test_the_largest_tiles_give_way_where_weights_pass_31_bits(run, M):  # noqa: F811
+    """Sixteen columns fewer and the estimate takes them: it is the limit that keeps them off the larger weights."""
+    run(CALLS + """
+M, (below, beyond), (f16_below, f16_beyond) = %d, %r, %r
+assert below[0] * below[1] < 2 ** 31 <= beyond[0] * beyond[1] and f16_below[0] * f16_below[1] * 2 < 2 ** 31 <= f16_beyond[0] * f16_beyond[1] * 2
+assert q8(M, *below) == (0, ["moe_pp_kernel<0,0,2,0>"]) and q8(M, *beyond) == (0, ["rows_tile_kernel<2,0,128,256,2,4,3,1>"])
+for n, how in ((2, 2), (600, 1)):
+    assert lora(M, *f16_below, n, 8)[1][-1] == "moe_pp_kernel<0,0,0,%%d>" %% how
+    assert lora(M, *f16_beyond, n, 8)[1][-1] == "rows_tile_kernel<0,%%d,128,256,2,4,3,1>" %% how
+""" % (M, cases.Q8_WEIGHTS, cases.F16_WEIGHTS))
