@@ -27,6 +27,28 @@ SHARE = [
     ((1300, 10248, 1288, 90, 40, "w4", 32), "moe_pp_kernel<0,0,0,1>"),
 ]
 
+# The same, computed in the tiles.
+_FEW_W4 = {32: (4, 2, 2), 64: (2, 3, 2), 128: (1, 3, 2)}  # groups of a step, register sets with one and with two tiles of columns
+IN_TILES = [
+    ((40, 520, 1032, 3, 24, "f16", 0), "few_rows_kernel<0,0,0,1,1,8,3,1>"),
+    ((11, 4672, 520, 5, 40, "f16", 0), "few_rows_kernel<0,0,0,1,2,8,3,1>"),
+    ((115, 1000, 600, 2, 72, "f16", 0), "rows_tile_kernel<0,2,64,32,2,1,3,4>"),
+    ((10, 8200, 264, 3, 24, "f16", 0), "rows_tile_kernel<0,2,64,64,2,2,3,2>"),
+    ((300, 4104, 1032, 3, 72, "f16", 0), "rows_tile_kernel<0,2,128,64,4,1,3,2>"),
+    ((700, 4104, 264, 3, 40, "f16", 0), "rows_tile_kernel<0,2,128,128,2,2,3,1>"),
+    ((1500, 4104, 1032, 3, 24, "f16", 0), "rows_tile_kernel<0,2,128,256,2,4,3,1>"),
+    ((1100, 10248, 1288, 3, 96, "f16", 0), "moe_pp_kernel<0,0,0,2>"),
+    ((19742, 1032, 520, 2, 24, "f16", 0), "moe_pp_kernel<0,0,0,2>"),
+]
+for _group, (_ng, _one, _two) in _FEW_W4.items():
+    IN_TILES += [
+        ((40, 520, 1032, 3, 24, "w4", _group), "few_rows_kernel<1,0,0,%d,1,8,%d,1>" % (_ng, _one)),
+        ((9, 4672, 520, 5, 40, "w4", _group), "few_rows_kernel<1,0,0,%d,2,8,%d,1>" % (_ng, _two)),
+        ((66, 24, 440, 2, 8, "w4", _group), "shared_rows_kernel<1,0,0,%d,2,1,2,4,3,1>" % _ng),
+        ((40, 4104, 520, 3, 72, "w4", _group), "shared_rows_kernel<1,0,0,%d,2,1,4,2,3,1>" % _ng),
+        ((300, 8200, 264, 3, 24, "w4", _group), "shared_rows_kernel<1,0,0,%d,4,1,8,1,3,1>" % _ng),
+    ]
+
 # 8-bit layers on 256 x 256 tiles: one round and several, six rows in the last row block, eight columns in the last tile, reductions that end inside a step,
 # one of a single step.
 Q8_LARGE = [(262, 22344, 1296), (527, 13456, 1296), (19742, 1032, 1040), (4365, 16688, 144), (16866, 8200, 16)]

@@ -11,7 +11,7 @@ import rows_ref as rows
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
-from test_gpu_rows import F8, _gen, _half, _nan, _q8, _w4, bolt  # noqa: E402, F401
+from test_gpu_rows import F8, _gen, _half, _lora, _nan, _q8, _w4, _w4_gen, bolt  # noqa: E402, F401
 
 
 # ---- the adapters' share through memory ---------------------------------------------------------------------------------
@@ -37,6 +37,45 @@ def test_the_share_has_the_range_of_fp32_whatever_the_table(bolt, size):  # noqa
         d = bolt.gemm_lora_desc(M, N, K, held, rank, weights=weights, group=group, alpha=2.0 ** -7, beta=-1.5)
         ws = _nan(bolt.bolt_gemm_lora_workspace_bytes(d), dtype=torch.uint8)
         rows.within(bolt.bolt_gemm_lora(d, A, W, bias, ids, down, up, scales, _nan(M, N), ws), want, bound, "%d adapters" % held)
+
+
+@pytest.mark.parametrize("size", [c[0] for c in cases.IN_TILES])
+@pytest.mark.parametrize("how", ["runs", "mixed"])
+def test_the_share_in_the_tiles(bolt, size, how):  # noqa: F811
+    M, N, K, n, rank, weights, group = size
+    D, _, c = _lora(bolt, M, N, K, n, rank, weights, group, how)
+    W64 = c["W"].double() if weights == "f16" else _w4(bolt, _w4_gen(c, M, N, K), N, K, group)[1]
+    rows.within(D, *rows.lora(c["A"].double(), W64, c["bias"].double(), c["ids"], c["down"], c["up"], c["scales"], "none", 0.75, -1.5, apart=False))
+
+
+@pytest.mark.parametrize("size", [c[0] for c in cases.SHARE + cases.IN_TILES])
+def test_the_share_is_not_rounded(bolt, size):  # noqa: F811
+    """Whole numbers, all rows of A alike, and a bias that takes the share away but for what binary16 would lose of it: sums are exact in FP32, so that the
+    one rounding left is the result's."""
+    M, N, K, n, rank, weights, group = size
+    g = _gen(M + N)
+    whole = lambda most, *s: torch.randint(-most, most + 1, s, device="cuda", generator=g).half()
+    A, down = whole(1, 1, K).expand(M, K).contiguous(), whole(1, n, rank, K)
+    up = whole(max(1, min(2000, int(8000 * 1.7 / math.sqrt(K * 0.44 * rank)))), n, N, rank)
+    if weights == "w4":
+        q = torch.randint(0, 256, (1, N, K // 2), dtype=torch.uint8, device="cuda", generator=g)
+        scale = torch.ones((1, N, -(-K // group)), dtype=torch.float16, device="cuda")
+        W = bolt.bolt_w4_pack(N, K, group, q, scale, None, _nan(bolt.bolt_w4_packed_bytes(N, K, group), dtype=torch.uint8))
+        W64 = ref.w4_matrix(q[0], scale[0], None, group)
+    else:
+        W = whole(8, N, K)
+        W64 = W.double()
+    low = down[0].double() @ A[0].double()
+    share = up[0].double() @ low
+    bias = -share.half()
+    assert low.abs().max() <= 2048 and share.abs().max() < 65504 and (share.half().double() != share).any()
+    ids = torch.randint(-1, 1, (M,), dtype=torch.int32, device="cuda", generator=g)
+    d = bolt.gemm_lora_desc(M, N, K, n, rank, weights=weights, group=group)
+    D = bolt.bolt_gemm_lora(d, A, W, bias, ids, down, up, None, _nan(M, N), _nan(bolt.bolt_gemm_lora_workspace_bytes(d), dtype=torch.uint8))
+    base = W64 @ A[0].double() + bias.double()
+    assert (base + share).abs().max() <= 2048
+    for id_, want in ((-1, base), (0, base + share)):
+        assert torch.equal(D[ids == id_], want.half().expand(int((ids == id_).sum()), N)), id_
 
 
 # ---- 8-bit layers --------------------------------------------------------------------------------------------------------

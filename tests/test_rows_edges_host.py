@@ -46,6 +46,24 @@ for size, kernel in %r:
 """ % (cases.SHARE,))
 
 
+def test_projections_whose_tiles_compute_the_share(run):  # noqa: F811
+    run(CALLS + """
+for size, kernel in %r:
+    s, k = lora(*size)
+    assert s == 0 and len(k) == 2 and k[1] == kernel, (size, k)
+""" % (cases.IN_TILES,))
+
+
+def test_every_kernel_that_adds_adapters_has_a_size():
+    """None of the instances that csrc/inst_*lora.hip and csrc/inst_few_rows_*.hip hold for adapters is left out of the two lists."""
+    named = {k for _, k in cases.SHARE + cases.IN_TILES}
+    for tile in ("64,32,2,1,3,4", "64,64,2,2,3,2", "128,64,4,1,3,2", "128,128,2,2,3,1", "128,256,2,4,3,1"):
+        assert {"rows_tile_kernel<0,1,%s>" % tile, "rows_tile_kernel<0,2,%s>" % tile} <= named
+    assert {"moe_pp_kernel<0,0,0,1>", "moe_pp_kernel<0,0,0,2>"} <= named
+    for family, least in (("few_rows_kernel<0", 2), ("few_rows_kernel<1", 6), ("shared_rows_kernel<1", 10)):
+        assert len({k for k in named if k.startswith(family)}) >= least, family
+
+
 def test_8_bit_layers_on_the_largest_tiles(run):  # noqa: F811
     run(CALLS + """
 for size in %r:
