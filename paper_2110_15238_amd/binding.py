@@ -697,8 +697,14 @@ def moe_experts(desc: MoeDesc, x, w_up, b_up, w_down, b_down, ids, weights, offs
 # ---- rows in 8 bits: the norm that writes them, the linear layer that reads them; projections with low-rank adapters ------------
 
 
+def _in_32_bits(*sizes):
+    """The sizes, if the C calls' 32 bits hold them: ctypes would cut others short without a word."""
+    assert -2 ** 31 <= min(sizes) and max(sizes) < 2 ** 31, "sizes and strides are counted in 32 bits: %s" % (sizes,)
+    return sizes
+
+
 def rms_norm_desc(rows, width, ldx=None, ldr=None, lds=None, ldy=None, ldq=None, eps=1e-5, weight_offset=0.0) -> RmsNormDesc:
-    return RmsNormDesc(rows, width, *(width if ld is None else ld for ld in (ldx, ldr, lds, ldy, ldq)), eps, weight_offset)
+    return RmsNormDesc(*_in_32_bits(rows, width, *(width if ld is None else ld for ld in (ldx, ldr, lds, ldy, ldq))), eps, weight_offset)
 
 
 def rms_norm(desc: RmsNormDesc, x, residual, weight, sum=None, y=None, q=None, scales=None):
@@ -724,16 +730,16 @@ def quantize_rows(x, q, scales):
     """x: float16 [rows][width], rows of any stride -> q: float8_e4m3fn [rows][width], scales: float32 [rows]."""
     rows, width = x.shape
     assert q.shape == x.shape and all(t.stride(1) == 1 or width == 1 for t in (x, q)), "x and q: rows x width, values of a row next to each other"
-    ldx, ldq = (t.stride(0) if rows > 1 else width for t in (x, q))
+    sizes = _in_32_bits(rows, width, *(t.stride(0) if rows > 1 else width for t in (x, q)))
     torch = _torch or _load_torch()
     assert x.is_cuda and x.dtype is torch.float16 and q.is_cuda and q.dtype is torch.float8_e4m3fn, "expects CUDA float16 rows and float8_e4m3fn ones"
-    _check(_lib.bolt_quantize_rows(rows, width, ldx, ldq, x.data_ptr(), q.data_ptr(), _buffer(scales, "float32", rows, "scales"), _stream()),
+    _check(_lib.bolt_quantize_rows(*sizes, x.data_ptr(), q.data_ptr(), _buffer(scales, "float32", rows, "scales"), _stream()),
            "bolt_quantize_rows")
     return q, scales
 
 
 def gemm_q8_desc(M, N, K, lda=None, ldd=None, alpha=1.0, beta=1.0, act="none") -> GemmQ8Desc:
-    return GemmQ8Desc(M, N, K, K if lda is None else lda, N if ldd is None else ldd, alpha, beta, ACT[act])
+    return GemmQ8Desc(*_in_32_bits(M, N, K, K if lda is None else lda, N if ldd is None else ldd), alpha, beta, ACT[act])
 
 
 def gemm_q8_workspace_bytes(desc: GemmQ8Desc) -> int:
@@ -757,7 +763,7 @@ def gemm_q8(desc: GemmQ8Desc, A, a_scales, W, w_scales, bias, D, workspace=None)
 
 
 def gemm_lora_desc(M, N, K, adapters, rank, weights="f16", group=0, lda=None, ldd=None, alpha=1.0, beta=1.0, act="none") -> GemmLoraDesc:
-    return GemmLoraDesc(M, N, K, K if lda is None else lda, N if ldd is None else ldd, WEIGHTS[weights], group, adapters, rank, alpha, beta,
+    return GemmLoraDesc(*_in_32_bits(M, N, K, K if lda is None else lda, N if ldd is None else ldd, WEIGHTS[weights], group, adapters, rank), alpha, beta,
                         ACT[act])
 
 

@@ -83,3 +83,21 @@ for n, how in ((2, 2), (600, 1)):
     assert lora(M, *f16_below, n, 8)[1][-1] == "moe_pp_kernel<0,0,0,%%d>" %% how
     assert lora(M, *f16_beyond, n, 8)[1][-1] == "rows_tile_kernel<0,%%d,128,256,2,4,3,1>" %% how
 """ % (M, cases.Q8_WEIGHTS, cases.F16_WEIGHTS))
+
+
+@pytest.mark.parametrize("size", [2 ** 31, 2 ** 32 + 64])
+def test_sizes_past_32_bits_are_refused(size):
+    """What the C calls' 32 bits would cut short (2^32 + 64 to 64: other rows, or fewer) is refused, row strides of tensors among it."""
+    torch = pytest.importorskip("torch")
+    import paper_2110_15238_amd as bolt
+    for make, names in ((bolt.rms_norm_desc, ("rows", "width", "ldx", "ldr", "lds", "ldy", "ldq")), (bolt.gemm_q8_desc, ("M", "N", "K", "lda", "ldd")),
+                        (bolt.gemm_lora_desc, ("M", "N", "K", "lda", "ldd", "adapters", "rank"))):
+        good = {n: 64 for n in names if not n.startswith("ld")}
+        make(**good)
+        for name in names:
+            with pytest.raises(AssertionError, match="32 bits"):
+                make(**{**good, name: size})
+    rows = lambda n, ld, dtype: torch.empty_strided((n, 64), (ld, 1), dtype=dtype, device="meta")
+    for x, q, n in ((size, 64, 2), (64, size, 2), (64, 64, size)):
+        with pytest.raises(AssertionError, match="32 bits"):
+            bolt.bolt_quantize_rows(rows(n, x, torch.float16), rows(n, q, torch.float8_e4m3fn), torch.empty(2, device="meta"))
