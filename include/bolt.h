@@ -435,7 +435,8 @@ size_t bolt_gemm_lora_workspace_bytes(const bolt_gemm_lora_desc* desc);
 
 /* v = x + residual, in FP32;  sum = v;  n = v / sqrt(mean(v^2) + eps) * (weight_offset + weight);  y = n;  scales[row] = max |n| / 448,
  * q = n / scale, all from the unrounded v.  A row whose largest |n| is below 2^-118 has zeros for q.  A row that holds an infinity or a NaN, or zeros
- * alone with eps 0, has a NaN for its scale, and for all of its q.  Up to 2^31 - 65536 rows of up to 32768 values. */
+ * alone with eps 0, has a NaN for its scale, and for all of its q.  q is rounded from n * (448 / max |n|), two roundings of FP32 from n / scale.  Up to
+ * 2^31 - 65536 rows of up to 32768 values; rows for bolt_gemm_q8 need a width that is a multiple of 16. */
 typedef struct {
   int32_t rows, width;             /* width a multiple of 8 */
   int32_t ldx, ldr, lds, ldy, ldq; /* row strides of x, residual, sum, y and q in elements, multiples of 8; of those that are not NULL */

@@ -8,7 +8,8 @@
 // them, which are FP32, adds them up first.
 // What bounds it: of few rows the chain of round trips (ids, operands, sums), of many the staging of x: down for one row of 4096 and rank 16 3.6 us on the
 // GPU, 29 rows of 5000 with 32 adapters of rank 32 4.6, 700 rows of 4096 with 6 of rank 24 5.0, 4096 rows of 4096 with 4 of rank 64, which it reads once, 18;
-// up for 29 rows of 6152 columns 6.0, for 4096 x 8192 47 (134 MB written; 37 when it wrote halves).
+// up for 29 rows of 6152 columns 6.0, for 700 x 4104 with 64 of rank 24 7.8, for 4096 x 8192 with 4 of rank 64 45, with 64 of them 73 (134 MB written; with
+// halves 6.8, 36 and 59).
 #pragma once
 #include "routed_rows.hpp"
 

@@ -319,10 +319,10 @@ Choice choose_w4(const Spread& s, int weight_rows) {
   else if (fills(16, 128)) t = SharedTile::ROWS16_COLS128;
   return {Family::SHARED, t, {}};
 }
-// FP16, us for the first experts above, few rows / shared rows / 64 x 128 / 128 x 128 / 256 x 256: 32 tokens 82 / 90; 128 tokens 116 / 109 / 96 / 98 /
-// 109; 512 tokens 183 / 183 / 117 / 140 / 122; 1024 tokens - / - / 142 / 151 / 182; 2048 tokens - / - / 238 / 214 / 189; 4096 tokens - / - / 398 / 348 /
-// 285; and 1000 wide, 2504 hidden, no gate, 8 experts, 2 per token: 64 tokens 31 / 31 / 47, 256 tokens - / 51 / 51 / 70 / 100, 1024 tokens - / - /
-// 90 / 84 / 114, 4096 tokens - / - / 221 / 200 / 160.
+// FP16, us for the first experts above, few rows / shared rows / 64 x 128 / 128 x 128 / 256 x 256: 32 tokens 80 / 83 / 81 / 89 / 100; 128 tokens 117 / 102 /
+// 99 / 99 / 110; 256 tokens 170 / 109 / 110 / 116 / 115; 512 tokens 276 / 145 / 117 / 140 / 140; 1024 tokens 489 / 220 / 143 / 149 / 182; 2048 tokens - / - / 238 /
+// 214 / 189; 4096 tokens - / - / 398 / 348 / 285; and 1000 wide, 2504 hidden, no gate, 8 experts, 2 per token: 32 tokens 24 / 29 / 41 / 64 / 94, 64 tokens 30 /
+// 28 / 33 / 55 / 86, 128 tokens 42 / 30 / 36 / 56 / 88, 256 tokens 54 / 44 / 40 / 59 / 91, 1024 tokens 159 / 119 / 94 / 89 / 119, 4096 tokens - / - / 221 / 200 / 160.
 // It does not look at the reduction's length.  Short ones, gated, 4 of 55 experts, 2000 wide, 464 hidden, 64 / 128 / 256 rows: 1024 tokens 130 / 136 /
 // 119, 2048 tokens 178 / 169 / 128, 4096 tokens 295 / 256 / 220, 8192 tokens 514 / 427 / 369; 5 of 9 experts, 448 x 424: 2048 tokens 44 / 43 / 48, 8192
 // tokens 145 / 123 / 117.  Over 108 sizes (9 shapes, 1 to 8192 tokens) the choice takes 1.03 times the best family for both products, 1.39 at

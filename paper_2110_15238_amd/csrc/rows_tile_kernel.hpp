@@ -5,9 +5,11 @@
 //   Adapters: FROM_ADD takes the rows' share from memory, where lora_up_kernel left it; FROM_ADAPTERS computes it, a wave for its own part of the
 //   tile, 64 ranks at a time: the rows' low once, then up of one adapter after the other, the next one's on its way.  A sum is taken only where the
 //   row's adapter is the one at hand.
-// What bounds it: operands on their way from the L2s, up to some 68 GB/s for a compute unit, so the reduction is split over
+// What bounds it: a workgroup's own steps.  A compute unit takes in some 50 to 70 GB/s of operands with 33 workgroups on the chip as with 198, so it is not what
+// the L2s give all of them together; whether loads, LDS reads or matrix instructions hold a step up has not been told apart.  So the reduction is split over
 // sets of waves (KG) where there are few workgroups.  us, E4M3, best tile here, 4096 x 11008: 128 rows 20, 333 rows 33, 1024 rows 54; 8192 x 2048: 128 rows
-// 7.0, 1024 rows 18.4 (128 x 256).  Splitting it over workgroups whose FP32 sums another launch adds up gained in 5 of 54 sizes, 9 % at most.
+// 7.0, 1024 rows 18.4 (128 x 256).  Splitting it over workgroups whose FP32 sums another launch adds up gained in 5 of 54 sizes, 9 % at most, for E4M3; for FP16
+// operands with adapters it has not been tried.
 #pragma once
 #include "routed_rows.hpp"
 
